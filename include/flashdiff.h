@@ -45,7 +45,8 @@ typedef enum {
     FD_ERR_TIMEOUT = 7      /* a bounded device-side wait expired                           */
 } fd_status;
 
-typedef enum { FD_F32 = 0, FD_BF16 = 1 } fd_dtype;
+/* FD_E4M3 is an output type of fd_matmul_fp8_blocks only; a context's storage type is one of the first two. */
+typedef enum { FD_F32 = 0, FD_BF16 = 1, FD_E4M3 = 2 } fd_dtype;
 
 /* Which kernels run the dense contractions. */
 typedef enum {
@@ -358,6 +359,117 @@ fd_status fd_region_activity_noalloc(const float* z_cur, const float* z_prev, co
                                      float* delta_state, int32_t* skip_count, uint8_t* prev_active,
                                      float* score_out, float* weight_out, uint8_t* mask_out,
                                      int32_t* status_out, void* cuda_stream);
+
+/*
+ * Row operators next to the step.  They need neither a context nor a workspace, keep no state between calls and
+ * allocate nothing, so calls on different streams, devices and host threads are independent, and a call can be captured
+ * into a CUDA graph like any other launch.  Each works on the current CUDA device, which has to be the one the
+ * pointers and the stream belong to.  Errors go to fd_last_error(NULL) of the calling thread.  Strides are counted in
+ * elements of the tensor they belong to; a row count of zero is a valid call that launches nothing.  Outputs must not
+ * overlap inputs except where that is said; elements of a strided output that belong to no row are left as they were.
+ *
+ * Rotary positions with several axes (time, height, width of a video token, height and width of an image token).
+ * The paper does not define rotary embedding; the convention is the one of fd_set_block_variants with the angle of a
+ * channel pair taken from one coordinate of the token's position:
+ *   axis a owns axis_dim[a] channels of every head, i.e. axis_dim[a] / 2 channel pairs; the axes' pairs follow one
+ *   another in the order of the axes, and pair i of axis a turns by  pos[t, a] * theta[a]^(-2 i / axis_dim[a]);
+ *   FD_ROPE_INTERLEAVED: pair p is the channels (2p, 2p + 1);  FD_ROPE_HALVES: pair p is (p, p + rot / 2), where
+ *   rot = the sum of axis_dim;  (a, b) -> (a cos - b sin, a sin + b cos);  channels from rot on are copied.
+ * Angles are formed and reduced in 64 bits, so positions far from the origin keep their accuracy; the rotation is fp32
+ * with one rounding to the storage type.
+ *   spec (HOST)  n_axes in 1..4, axis_dim positive and even with a sum of at most head_dim, theta positive and finite
+ *   pos          [tokens, n_axes] f32, contiguous (fractional and negative positions are fine)
+ *   head_dim     even, at most 256
+ *
+ * fd_rope_axes rotates one or two sets of rows (HOST array; queries and keys), element type dtype (FD_F32 / FD_BF16):
+ * row (t, h) of a set is at in + t * in_token_stride + h * in_head_stride, so slices of a fused projection's output need
+ * no copy.  out may be in with the same strides (in place).  inverse != 0 turns by the negative angles: the inverse
+ * map, which is also the gradient of the forward one.  An output's rows must not overlap one another: FD_ERR_SHAPE.
+ *
+ * fd_rope_axes_tables writes the tables fd_set_block_variants takes: cos_out, sin_out [tokens, head_dim / 2] f32, pair p
+ * of the interleaved pairing in column p (FD_ROPE_HALVES is refused: the step pairs neighbours), 1 and 0 behind rot / 2.
+ */
+typedef enum { FD_ROPE_INTERLEAVED = 0, FD_ROPE_HALVES = 1 } fd_rope_pairing;
+typedef struct {
+    double theta[4];
+    int32_t axis_dim[4];
+    int32_t n_axes;
+    int32_t pairing; /* fd_rope_pairing */
+} fd_rope_spec;
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
+    int32_t heads;
+} fd_rope_rows;
+fd_status fd_rope_axes(const fd_rope_spec* spec, const float* pos, int64_t tokens, int head_dim, int dtype,
+                       const fd_rope_rows* sets, int n_sets, int inverse, void* cuda_stream);
+fd_status fd_rope_axes_tables(const fd_rope_spec* spec, const float* pos, int64_t tokens, int head_dim, float* cos_out,
+                              float* sin_out, void* cuda_stream);
+
+/*
+ * 8-bit rows with a scale for every block of 128 columns (no counterpart in the paper; the finer-grained relative of
+ * fd_set_fp8_operands, whose activation scales are fixed numbers per tensor: here they follow the data).  Block b of a
+ * row is its columns 128 b .. 128 b + 127 (the last one may be shorter) and is stored as
+ *   scale[row, b] = max(amax, 2^-100) / 448,   amax the block's largest magnitude,
+ *   code[row, c]  = E4M3(v[row, c] * (448 / max(amax, 2^-100)))     round to nearest even,
+ * so that code * scale stands for v.  A NaN becomes the NaN code and does not count for amax; a block that holds an
+ * infinity has an infinite scale and stands for NaN.
+ *
+ * fd_add_rmsnorm: residual addition and root-mean-square norm in one pass over the rows,
+ *   r = x + residual,   y = r / sqrt(mean(r^2) + eps) * weight,
+ * sums and norm in fp32; r is rounded only where it is stored (the norm reads the unrounded sum).
+ *   x [rows, cols] of x_dtype;  residual, residual_out of residual_dtype, or NULL (no addition / sum not kept; without a
+ *   residual, residual_out receives x);  weight [cols] of x_dtype or NULL (ones);  eps >= 0;
+ *   y [rows, cols] of x_dtype or NULL;  y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)] f32, or both NULL; at
+ *   least one of y, y8 is given.  residual_out may be residual, y may be x (same strides).
+ * fd_quantize_fp8_blocks: the block form of a tensor as it is (an attention output, a weight's rows).
+ * Any width, any row stride of at least the width; 16-byte aligned rows of a multiple of 8 columns take the fast path.
+ */
+typedef struct {
+    const void* x;
+    const void* residual;
+    void* residual_out;
+    const void* weight;
+    void* y;
+    void* y8;
+    float* y8_scale;
+    int64_t x_stride, residual_stride, residual_out_stride, y_stride, y8_stride, y8_scale_stride;
+    int32_t x_dtype, residual_dtype; /* FD_F32 / FD_BF16 */
+    float eps;
+} fd_rmsnorm_args;
+fd_status fd_add_rmsnorm(const fd_rmsnorm_args* args, int64_t rows, int cols, void* cuda_stream);
+fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, int64_t rows, int cols, void* y8,
+                                 int64_t y8_stride, float* y8_scale, int64_t y8_scale_stride, void* cuda_stream);
+
+/*
+ * Matrix product of two E4M3 operands with block scales:
+ *   v[i, j] = sum_b a_scale[i, b] * w_scale[j / 128, b] * (sum over the k of block b of a8[i, k] * w8[j, k]) + bias[j]
+ *   out[i, j] = v, or tanh-GELU(v) with gelu != 0
+ * The inner sums and the sum over blocks are fp32; the bias and the GELU are applied to the fp32 value, which is rounded
+ * once to out_dtype.  FD_E4M3 writes codes with a scale per 128 columns in out_scale [m, ceil(n / 128)], by the rule above:
+ * the a8 / a_scale of the next product.
+ *   a8 [m, k], w8 [n, k]: codes, k contiguous; base addresses 16-byte aligned, row strides multiples of 16 bytes
+ *   a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] f32 (columns contiguous); the product of an a_scale
+ *   and a w_scale has to be finite
+ *   bias [n] of bias_dtype (FD_F32 / FD_BF16) or NULL;  out [m, n], columns contiguous
+ * Any m >= 0, n >= 1, k >= 1.
+ *   status_out: optional DEVICE int32 that receives, in stream order, 0 or FD_ERR_TIMEOUT if a bounded wait of the kernel
+ *   ran out (the result is then incomplete); may be NULL.
+ */
+typedef struct {
+    const void* a8;
+    const float* a_scale;
+    const void* w8;
+    const float* w_scale;
+    const void* bias;
+    void* out;
+    float* out_scale;
+    int32_t* status_out;
+    int64_t a8_stride, a_scale_stride, w8_stride, w_scale_stride, out_stride, out_scale_stride;
+    int32_t bias_dtype, out_dtype, gelu;
+} fd_matmul_fp8_args;
+fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* args, int m, int n, int k, void* cuda_stream);
 
 /*
  * Reads the device-side status word (synchronises `cuda_stream`).  Returns FD_OK, or the first

@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libflashdiff.so")
 FD_OK = 0
 FD_ERR_INVALID_ARG, FD_ERR_SHAPE, FD_ERR_STATE, FD_ERR_WORKSPACE = 1, 2, 3, 4
 FD_ERR_UNSUPPORTED, FD_ERR_CUDA, FD_ERR_TIMEOUT = 5, 6, 7
-FD_F32, FD_BF16 = 0, 1
+FD_F32, FD_BF16, FD_E4M3 = 0, 1, 2
+FD_ROPE_INTERLEAVED, FD_ROPE_HALVES = 0, 1
 FD_ENGINE_AUTO, FD_ENGINE_SIMT, FD_ENGINE_TC = 0, 1, 2
 
 EXPORTS = ["fd_workspace_bytes", "fd_create", "fd_partition_regions", "fd_region_activity",
@@ -24,7 +25,8 @@ EXPORTS = ["fd_workspace_bytes", "fd_create", "fd_partition_regions", "fd_region
            "fd_profile_enable", "fd_profile_read", "fd_region_activity_noalloc", "fd_selftest_bounded_wait",
            "fd_embed_latent", "fd_update_latent", "fd_regional_step_mass", "fd_region_activity_attn",
            "fd_sched_pack", "fd_sched_form_batch", "fd_rsearch_init", "fd_rsearch_update", "fd_set_block_variants",
-           "fd_set_text_stream", "fd_set_cross_attention", "fd_set_fp8_operands", "fd_debug_buffer", "fd_set_fp8_text_stream"]
+           "fd_set_text_stream", "fd_set_cross_attention", "fd_set_fp8_operands", "fd_debug_buffer", "fd_set_fp8_text_stream",
+           "fd_rope_axes", "fd_rope_axes_tables", "fd_add_rmsnorm", "fd_quantize_fp8_blocks", "fd_matmul_fp8_blocks"]
 FD_NOALLOC_MAX_REGION_SLOTS = 16384
 PROF_GROUPS = ["activity", "compact", "adaln", "ln_modulate", "gemm_qkv", "attention", "gemm_out", "gemm_fc1",
                "gemm_fc2", "partition", "sampler", "qk_variants", "cross_attention"]
@@ -64,6 +66,31 @@ class FdFp8Operands(ctypes.Structure):
 class FdRSearch(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("r_min", "r_max", "accepted", "candidate", "step", "dir", "have_ref",
                                               "fails_at_one", "converged")] + [("ref_perf", ctypes.c_double)]
+
+
+class FdRopeSpec(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double * 4), ("axis_dim", ctypes.c_int32 * 4), ("n_axes", ctypes.c_int32),
+                ("pairing", ctypes.c_int32)]
+
+
+class FdRopeRows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("in_token_stride", "in_head_stride", "out_token_stride", "out_head_stride")] + \
+               [("heads", ctypes.c_int32)]
+
+
+class FdRmsnormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "residual_out", "weight", "y", "y8", "y8_scale")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "y_stride", "y8_stride",
+                                              "y8_scale_stride")] + \
+               [("x_dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class FdMatmulFp8Args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("a8", "a_scale", "w8", "w_scale", "bias", "out", "out_scale", "status_out")] + \
+               [(n, ctypes.c_int64) for n in ("a8_stride", "a_scale_stride", "w8_stride", "w_scale_stride", "out_stride",
+                                              "out_scale_stride")] + \
+               [(n, ctypes.c_int32) for n in ("bias_dtype", "out_dtype", "gelu")]
 
 
 class FlashDiffError(RuntimeError):
@@ -127,6 +154,17 @@ def _load() -> ctypes.CDLL:
     lib.fd_set_fp8_text_stream.argtypes = [vp, ctypes.POINTER(FdFp8Operands)]
     lib.fd_set_cross_attention.restype = i32
     lib.fd_set_cross_attention.argtypes = [vp, ctypes.POINTER(FdCrossAttention)]
+    i64 = ctypes.c_int64
+    lib.fd_rope_axes.restype = i32
+    lib.fd_rope_axes.argtypes = [ctypes.POINTER(FdRopeSpec), vp, i64, i32, i32, ctypes.POINTER(FdRopeRows), i32, i32, vp]
+    lib.fd_rope_axes_tables.restype = i32
+    lib.fd_rope_axes_tables.argtypes = [ctypes.POINTER(FdRopeSpec), vp, i64, i32, vp, vp, vp]
+    lib.fd_add_rmsnorm.restype = i32
+    lib.fd_add_rmsnorm.argtypes = [ctypes.POINTER(FdRmsnormArgs), i64, i32, vp]
+    lib.fd_quantize_fp8_blocks.restype = i32
+    lib.fd_quantize_fp8_blocks.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, i64, vp]
+    lib.fd_matmul_fp8_blocks.restype = i32
+    lib.fd_matmul_fp8_blocks.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
     lib.fd_launch_count.restype = ctypes.c_int64
     lib.fd_launch_count.argtypes = [vp]
     lib.fd_destroy.restype = i32
@@ -359,6 +397,199 @@ def fd_set_fp8_operands(ctx: Context, fp8: Optional[Dict[str, "object"]], text_s
     a = np.ascontiguousarray(fp8["a_scale"], dtype=np.float32)
     f = FdFp8Operands(*(fp8[k].data_ptr() for k in ("w8_qkv", "s_qkv", "w8_fc1", "s_fc1", "w8_fc2", "s_fc2")), a.ctypes.data)
     _check(ctx.handle, call(ctx.handle, ctypes.byref(f)))
+
+
+# ---- row operators next to the step (no context; work on the tensors' device) ------------------------------------
+
+def _op_fail(text: str):
+    raise FlashDiffError(FD_ERR_INVALID_ARG, text)
+
+
+def _codes_type(t) -> bool:
+    return t.element_size() == 1 and str(t.dtype) in ("torch.uint8", "torch.float8_e4m3fn")
+
+
+def _type_code(t, name: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return FD_BF16
+    if t.dtype == torch.float32:
+        return FD_F32
+    _op_fail("%s must be float32 or bfloat16, not %s" % (name, t.dtype))
+
+
+def _rows(t, name: str, rows: int, cols: int, device, code=None, f32=False) -> int:
+    """Row stride of the 2-D device tensor ``t`` of the wanted shape, columns contiguous."""
+    import torch
+    if t.device != device or tuple(t.shape) != (rows, cols):
+        _op_fail("%s must be [%d, %d] on %s, not %s on %s" % (name, rows, cols, device, list(t.shape), t.device))
+    if cols > 1 and t.stride(1) != 1:
+        _op_fail("%s must have contiguous columns" % name)
+    if code and not _codes_type(t):
+        _op_fail("%s must hold E4M3 codes (uint8 or float8_e4m3fn), not %s" % (name, t.dtype))
+    if f32 and t.dtype != torch.float32:
+        _op_fail("%s must be float32, not %s" % (name, t.dtype))
+    return max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+
+
+class _on_device:
+    """The tensors' device made current for a call (nothing to do where it already is)."""
+
+    def __init__(self, t):
+        import torch
+        if not t.is_cuda:
+            _op_fail("device tensors wanted, got one on %s" % t.device)
+        self.guard = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard:
+            self.guard.__exit__(*exc)
+
+
+def make_rope_axes(axis_dims, theta=10000.0, pairing: str = "interleaved") -> FdRopeSpec:
+    """fd_rope_spec: channels per axis, base per axis (or one for all), "interleaved" or "halves"."""
+    axis_dims = [int(d) for d in axis_dims]
+    thetas = [float(theta)] * len(axis_dims) if isinstance(theta, (int, float)) else [float(v) for v in theta]
+    if not 1 <= len(axis_dims) <= 4 or len(thetas) != len(axis_dims):
+        _op_fail("one to four axes, with one base each")
+    if pairing not in ("interleaved", "halves"):
+        _op_fail("unknown pairing %r" % (pairing,))
+    return FdRopeSpec((ctypes.c_double * 4)(*thetas), (ctypes.c_int32 * 4)(*axis_dims), len(axis_dims),
+                      FD_ROPE_INTERLEAVED if pairing == "interleaved" else FD_ROPE_HALVES)
+
+
+def _rope_pos(spec: FdRopeSpec, pos) -> int:
+    import torch
+    if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape[1] != spec.n_axes or not pos.is_contiguous():
+        _op_fail("pos must be a contiguous float32 tensor [tokens, %d]" % spec.n_axes)
+    return int(pos.shape[0])
+
+
+def fd_rope_axes(spec: FdRopeSpec, pos, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
+    """Rotates q (and k) [tokens, heads, head_dim] by the tokens' positions pos [tokens, n_axes] into q_out (k_out);
+    any token and head strides, the same tensor twice rotates in place.  ``inverse``: the inverse map, also the gradient."""
+    tokens = _rope_pos(spec, pos)
+    sets = [(q, q_out)] + ([(k, k_out)] if k is not None else [])
+    if (k is None) != (k_out is None):
+        _op_fail("k and k_out come together")
+    code, dh = _type_code(q, "q"), int(q.shape[-1])
+    rows = (FdRopeRows * len(sets))()
+    for i, (a, b) in enumerate(sets):
+        if a.dim() != 3 or a.shape[0] != tokens or a.shape[2] != dh or a.shape != b.shape:
+            _op_fail("rows must be [tokens, heads, head_dim], inputs and outputs alike")
+        if a.dtype != q.dtype or b.dtype != q.dtype or a.device != pos.device or b.device != pos.device:
+            _op_fail("rows must share one type and the device of pos")
+        if a.stride(2) != 1 or b.stride(2) != 1:
+            _op_fail("channels must be contiguous")
+        rows[i] = FdRopeRows(a.data_ptr(), b.data_ptr(), a.stride(0), a.stride(1), b.stride(0), b.stride(1), a.shape[1])
+    if tokens == 0:
+        return
+    with _on_device(pos):
+        _check(None, lib.fd_rope_axes(ctypes.byref(spec), pos.data_ptr(), tokens, dh, code, rows, len(sets), 1 if inverse else 0,
+                                      _stream(stream)))
+
+
+def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) -> None:
+    """The rotary tables [tokens, head_dim / 2] float32 that fd_set_block_variants takes, from positions [tokens, n_axes]."""
+    tokens = _rope_pos(spec, pos)
+    half = int(cos_out.shape[-1])
+    for t, name in ((cos_out, "cos_out"), (sin_out, "sin_out")):
+        _rows(t, name, tokens, half, pos.device, f32=True)
+        if not t.is_contiguous():
+            _op_fail("%s must be contiguous" % name)
+    if tokens == 0:
+        return
+    with _on_device(pos):
+        _check(None, lib.fd_rope_axes_tables(ctypes.byref(spec), pos.data_ptr(), tokens, 2 * half, cos_out.data_ptr(), sin_out.data_ptr(),
+                                             _stream(stream)))
+
+
+def fd_add_rmsnorm(x, weight, eps: float, residual=None, residual_out=None, y=None, y8=None, y8_scale=None, stream=None) -> None:
+    """r = x + residual (kept in residual_out if given), y = r / sqrt(mean(r^2) + eps) * weight; outputs y in x's type and / or
+    y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)].  residual_out may be residual, y may be x."""
+    rows, cols = x.shape
+    dev = x.device
+    a = FdRmsnormArgs(eps=float(eps), x_dtype=_type_code(x, "x"))
+    a.x, a.x_stride = x.data_ptr(), _rows(x, "x", rows, cols, dev)
+    if weight is not None:
+        if weight.dtype != x.dtype or weight.device != dev or tuple(weight.shape) != (cols,) or not weight.is_contiguous():
+            _op_fail("weight must be a contiguous [%d] tensor of x's type and device" % cols)
+        a.weight = weight.data_ptr()
+    if residual is not None and residual_out is not None and residual.dtype != residual_out.dtype:
+        _op_fail("residual and residual_out must share one type")
+    for t, name in ((residual, "residual"), (residual_out, "residual_out")):
+        if t is not None:
+            a.residual_dtype = _type_code(t, name)
+            setattr(a, name, t.data_ptr())
+            setattr(a, name + "_stride", _rows(t, name, rows, cols, dev))
+    if y is not None:
+        if y.dtype != x.dtype:
+            _op_fail("y must have x's type")
+        a.y, a.y_stride = y.data_ptr(), _rows(y, "y", rows, cols, dev)
+    if y8 is not None:
+        a.y8, a.y8_stride = y8.data_ptr(), _rows(y8, "y8", rows, cols, dev, code=True)
+    if y8_scale is not None:
+        a.y8_scale, a.y8_scale_stride = y8_scale.data_ptr(), _rows(y8_scale, "y8_scale", rows, (cols + 127) // 128, dev, f32=True)
+    if rows == 0:
+        return
+    with _on_device(x):
+        _check(None, lib.fd_add_rmsnorm(ctypes.byref(a), rows, cols, _stream(stream)))
+
+
+def fd_quantize_fp8_blocks(x, y8, y8_scale, stream=None) -> None:
+    """E4M3 codes y8 and scales y8_scale [rows, ceil(cols / 128)] of x [rows, cols] (float32 or bfloat16)."""
+    rows, cols = x.shape
+    dev = x.device
+    args = (_rows(x, "x", rows, cols, dev), _type_code(x, "x"), rows, cols, y8.data_ptr(), _rows(y8, "y8", rows, cols, dev, code=True),
+            y8_scale.data_ptr(), _rows(y8_scale, "y8_scale", rows, (cols + 127) // 128, dev, f32=True))
+    if rows == 0:
+        return
+    with _on_device(x):
+        _check(None, lib.fd_quantize_fp8_blocks(x.data_ptr(), *args, _stream(stream)))
+
+
+def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = False, out_scale=None, status_out=None,
+                         stream=None) -> None:
+    """out [m, n] = sum over the 128-blocks of k of a_scale * w_scale * (a8 w8^T) + bias, then tanh-GELU if asked.  a8 [m, k],
+    w8 [n, k]: E4M3 codes; a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] float32; out float32, bfloat16,
+    or codes with out_scale [m, ceil(n / 128)]; status_out: optional int32 device scalar."""
+    import torch
+    (m, k), n, dev = a8.shape, w8.shape[0], a8.device
+    kb, nb = (k + 127) // 128, (n + 127) // 128
+    f = FdMatmulFp8Args(gelu=1 if gelu else 0)
+    f.a8, f.a8_stride = a8.data_ptr(), _rows(a8, "a8", m, k, dev, code=True)
+    f.w8, f.w8_stride = w8.data_ptr(), _rows(w8, "w8", n, k, dev, code=True)
+    if m <= 1:                                          # the stride of a single row is free: round it up to what is asked for
+        f.a8_stride = (f.a8_stride + 15) // 16 * 16
+    if n <= 1:
+        f.w8_stride = (f.w8_stride + 15) // 16 * 16
+    f.a_scale, f.a_scale_stride = a_scale.data_ptr(), _rows(a_scale, "a_scale", m, kb, dev, f32=True)
+    f.w_scale, f.w_scale_stride = w_scale.data_ptr(), _rows(w_scale, "w_scale", nb, kb, dev, f32=True)
+    if bias is not None:
+        if bias.device != dev or tuple(bias.shape) != (n,) or (n > 1 and bias.stride(0) != 1):
+            _op_fail("bias must be a contiguous [%d] tensor on %s" % (n, dev))
+        f.bias, f.bias_dtype = bias.data_ptr(), _type_code(bias, "bias")
+    if _codes_type(out):
+        f.out_dtype = FD_E4M3
+        if out_scale is None:
+            _op_fail("codes in out need out_scale")
+    else:
+        f.out_dtype = _type_code(out, "out")
+    f.out, f.out_stride = out.data_ptr(), _rows(out, "out", m, n, dev)
+    if out_scale is not None:
+        f.out_scale, f.out_scale_stride = out_scale.data_ptr(), _rows(out_scale, "out_scale", m, nb, dev, f32=True)
+    if status_out is not None:
+        if status_out.dtype != torch.int32 or status_out.device != dev or status_out.numel() < 1:
+            _op_fail("status_out must be an int32 tensor on %s" % dev)
+        f.status_out = status_out.data_ptr()
+    if m == 0:
+        return
+    with _on_device(a8):
+        _check(None, lib.fd_matmul_fp8_blocks(ctypes.byref(f), m, n, k, _stream(stream)))
 
 
 def fd_sched_pack(load, cost, home):

@@ -813,6 +813,173 @@ fd_status fd_set_fp8_text_stream(fd_ctx* c, const fd_fp8_operands* f) {
     return set_fp8(c, f, true);
 }
 
+// ---- row operators next to the step: no context, errors to the calling thread's text ---------------------------------
+namespace {
+fd_status op_fail(fd_status s, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    try {
+        g_create_error = buf;
+    } catch (...) {                              // out of host memory: the status has to do
+    }
+    return s;
+}
+fd_status op_launched(const char* who, cudaError_t e, const std::string& why = std::string()) {
+    if (e == cudaSuccess) return FD_OK;
+    return op_fail(FD_ERR_CUDA, "%s: %s", who, why.empty() ? cudaGetErrorString(e) : why.c_str());
+}
+bool storage_type(int dtype) { return dtype == FD_F32 || dtype == FD_BF16; }
+bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+size_t type_bytes(int dtype) { return dtype == FD_F32 ? 4 : 2; }
+constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
+constexpr int64_t MAX_ROWS = int64_t(1) << 31;
+
+fd_status rope_spec_ok(const char* who, const fd_rope_spec* s, const float* pos, int64_t tokens, int head_dim) {
+    if (!s || !pos) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
+    if (!aligned4(pos)) return op_fail(FD_ERR_INVALID_ARG, "%s: pos must be 4-byte aligned", who);
+    if (tokens < 0 || tokens >= MAX_ROWS) return op_fail(FD_ERR_SHAPE, "%s: tokens must be in [0, 2^31)", who);
+    if (head_dim < 2 || head_dim > 256 || head_dim % 2) return op_fail(FD_ERR_SHAPE, "%s: head_dim must be even, 2 .. 256", who);
+    if (s->n_axes < 1 || s->n_axes > 4) return op_fail(FD_ERR_SHAPE, "%s: n_axes must be 1 .. 4", who);
+    int64_t rot = 0;
+    for (int a = 0; a < s->n_axes; ++a) {
+        if (s->axis_dim[a] < 2 || s->axis_dim[a] % 2) return op_fail(FD_ERR_SHAPE, "%s: axis_dim must be positive and even", who);
+        if (!(s->theta[a] > 0.0) || !(s->theta[a] < 1e300)) return op_fail(FD_ERR_INVALID_ARG, "%s: theta must be positive and finite", who);
+        rot += s->axis_dim[a];
+    }
+    if (rot > head_dim) return op_fail(FD_ERR_SHAPE, "%s: the axes' channels exceed head_dim", who);
+    if (s->pairing != FD_ROPE_INTERLEAVED && s->pairing != FD_ROPE_HALVES) return op_fail(FD_ERR_INVALID_ARG, "%s: unknown pairing", who);
+    return FD_OK;
+}
+}  // namespace
+
+fd_status fd_rope_axes(const fd_rope_spec* spec, const float* pos, int64_t tokens, int head_dim, int dtype,
+                       const fd_rope_rows* sets, int n_sets, int inverse, void* cuda_stream) {
+    const char* who = "fd_rope_axes";
+    fd_status s = rope_spec_ok(who, spec, pos, tokens, head_dim);
+    if (s != FD_OK) return s;
+    if (!storage_type(dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: dtype must be FD_F32 or FD_BF16", who);
+    if (!sets || n_sets < 1 || n_sets > 2) return op_fail(FD_ERR_INVALID_ARG, "%s: one or two sets of rows", who);
+    for (int i = 0; i < n_sets; ++i) {
+        const fd_rope_rows& r = sets[i];
+        if (!r.in || !r.out) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
+        if (!aligned_to(r.in, type_bytes(dtype)) || !aligned_to(r.out, type_bytes(dtype)))
+            return op_fail(FD_ERR_INVALID_ARG, "%s: rows must be aligned to their element type", who);
+        if (r.heads < 1 || r.heads > 65536) return op_fail(FD_ERR_SHAPE, "%s: heads must be 1 .. 65536", who);
+        const int64_t st[4] = {r.in_token_stride, r.in_head_stride, r.out_token_stride, r.out_head_stride};
+        for (int64_t v : st)
+            if (v < 0 || v > MAX_STRIDE) return op_fail(FD_ERR_SHAPE, "%s: strides must be in [0, 2^40]", who);
+        // rows of the output lie apart: heads inside a token's span, or tokens inside a head's
+        const int64_t ts = r.out_token_stride, hs = r.out_head_stride, T = tokens, h = r.heads;
+        const bool head_in = (h == 1 || hs >= head_dim) && (T <= 1 || ts >= (h - 1) * hs + head_dim);
+        const bool token_in = (T <= 1 || ts >= head_dim) && (h == 1 || hs >= (T - 1) * ts + head_dim);
+        if (!head_in && !token_in) return op_fail(FD_ERR_SHAPE, "%s: the output's rows overlap", who);
+        if (r.in == r.out && ((T > 1 && r.in_token_stride != ts) || (h > 1 && r.in_head_stride != hs)))
+            return op_fail(FD_ERR_SHAPE, "%s: in place needs equal strides", who);
+    }
+    if (tokens == 0) return FD_OK;
+    return op_launched(who, launch_rope_axes(*spec, pos, tokens, head_dim, dtype, sets, n_sets, inverse != 0, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+fd_status fd_rope_axes_tables(const fd_rope_spec* spec, const float* pos, int64_t tokens, int head_dim, float* cos_out,
+                              float* sin_out, void* cuda_stream) {
+    const char* who = "fd_rope_axes_tables";
+    fd_status s = rope_spec_ok(who, spec, pos, tokens, head_dim);
+    if (s != FD_OK) return s;
+    if (!cos_out || !sin_out || !aligned4(cos_out) || !aligned4(sin_out))
+        return op_fail(FD_ERR_INVALID_ARG, "%s: tables null or not 4-byte aligned", who);
+    if (spec->pairing != FD_ROPE_INTERLEAVED) return op_fail(FD_ERR_UNSUPPORTED, "%s: the step rotates neighbouring channels", who);
+    if (tokens == 0) return FD_OK;
+    return op_launched(who, launch_rope_tables(*spec, pos, tokens, head_dim, cos_out, sin_out, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+namespace {
+// pointer given: aligned to its element, rows at least `width` apart
+fd_status op_rows(const char* who, const char* name, const void* p, int64_t stride, size_t align, int64_t rows, int64_t width) {
+    if (!p) return FD_OK;
+    if (!aligned_to(p, align)) return op_fail(FD_ERR_INVALID_ARG, "%s: %s is misaligned", who, name);
+    if (stride < 0 || stride > MAX_STRIDE || (rows > 1 && stride < width)) return op_fail(FD_ERR_SHAPE, "%s: %s has a row stride below its width", who, name);
+    return FD_OK;
+}
+fd_status row_blocks_call(const char* who, const fd_rmsnorm_args& a, int64_t rows, int cols, bool norm, void* cuda_stream) {
+    if (!a.x) return op_fail(FD_ERR_INVALID_ARG, "%s: x is null", who);
+    if (!a.y && !a.y8) return op_fail(FD_ERR_INVALID_ARG, "%s: no output", who);
+    if ((a.y8 == nullptr) != (a.y8_scale == nullptr)) return op_fail(FD_ERR_INVALID_ARG, "%s: the codes and their scales come together", who);
+    if (!storage_type(a.x_dtype) || ((a.residual || a.residual_out) && !storage_type(a.residual_dtype)))
+        return op_fail(FD_ERR_UNSUPPORTED, "%s: dtypes must be FD_F32 or FD_BF16", who);
+    if (rows < 0 || rows >= MAX_ROWS || cols < 1 || cols > (1 << 30)) return op_fail(FD_ERR_SHAPE, "%s: rows in [0, 2^31), cols in [1, 2^30]", who);
+    if (!(a.eps >= 0.f) || !(a.eps < 3.0e38f)) return op_fail(FD_ERR_INVALID_ARG, "%s: eps must be non-negative and finite", who);
+    const size_t xs = type_bytes(a.x_dtype), rs = type_bytes(a.residual_dtype);
+    if (a.weight && !aligned_to(a.weight, xs)) return op_fail(FD_ERR_INVALID_ARG, "%s: weight is misaligned", who);
+    fd_status s = FD_OK;
+    if ((s = op_rows(who, "x", a.x, a.x_stride, xs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "residual", a.residual, a.residual_stride, rs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "residual_out", a.residual_out, a.residual_out_stride, rs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "y", a.y, a.y_stride, xs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "y8", a.y8, a.y8_stride, 1, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "y8_scale", a.y8_scale, a.y8_scale_stride, 4, rows, (cols + FP8_BLOCK - 1) / FP8_BLOCK)) != FD_OK) return s;
+    if (rows > 1 && ((a.residual_out && a.residual_out == a.residual && a.residual_out_stride != a.residual_stride) ||
+                     (a.y && a.y == a.x && a.y_stride != a.x_stride)))
+        return op_fail(FD_ERR_SHAPE, "%s: in place needs equal strides", who);
+    if (rows == 0) return FD_OK;
+    return op_launched(who, launch_row_blocks(a, rows, cols, norm, static_cast<cudaStream_t>(cuda_stream)));
+}
+}  // namespace
+
+fd_status fd_add_rmsnorm(const fd_rmsnorm_args* args, int64_t rows, int cols, void* cuda_stream) {
+    if (!args) return op_fail(FD_ERR_INVALID_ARG, "fd_add_rmsnorm: args is null");
+    return row_blocks_call("fd_add_rmsnorm", *args, rows, cols, true, cuda_stream);
+}
+
+fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, int64_t rows, int cols, void* y8,
+                                 int64_t y8_stride, float* y8_scale, int64_t y8_scale_stride, void* cuda_stream) {
+    fd_rmsnorm_args a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.x_dtype = x_dtype;
+    a.y8 = y8;
+    a.y8_stride = y8_stride;
+    a.y8_scale = y8_scale;
+    a.y8_scale_stride = y8_scale_stride;
+    return row_blocks_call("fd_quantize_fp8_blocks", a, rows, cols, false, cuda_stream);
+}
+
+fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k, void* cuda_stream) {
+    const char* who = "fd_matmul_fp8_blocks";
+    if (!f) return op_fail(FD_ERR_INVALID_ARG, "%s: args is null", who);
+    if (!f->a8 || !f->a_scale || !f->w8 || !f->w_scale || !f->out) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
+    if (f->out_dtype != FD_F32 && f->out_dtype != FD_BF16 && f->out_dtype != FD_E4M3) return op_fail(FD_ERR_UNSUPPORTED, "%s: unknown out_dtype", who);
+    if (f->bias && !storage_type(f->bias_dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: bias_dtype must be FD_F32 or FD_BF16", who);
+    if ((f->out_dtype == FD_E4M3) != (f->out_scale != nullptr)) return op_fail(FD_ERR_INVALID_ARG, "%s: out_scale goes with an E4M3 output", who);
+    if (m < 0 || n < 1 || k < 1 || m > (1 << 30) || n > (1 << 30) || k > (1 << 30))
+        return op_fail(FD_ERR_SHAPE, "%s: m in [0, 2^30], n and k in [1, 2^30]", who);
+    if (!aligned16(f->a8) || !aligned16(f->w8)) return op_fail(FD_ERR_INVALID_ARG, "%s: a8 and w8 must be 16-byte aligned", who);
+    const int64_t kb = (k + FP8_BLOCK - 1) / FP8_BLOCK, nb = (n + FP8_BLOCK - 1) / FP8_BLOCK;
+    // the tensor maps take the strides of single rows too
+    if (f->a8_stride % 16 || f->w8_stride % 16 || f->a8_stride < k || f->w8_stride < k)
+        return op_fail(FD_ERR_SHAPE, "%s: the strides of a8 and w8 must be multiples of 16 and at least k", who);
+    const size_t es = f->out_dtype == FD_E4M3 ? 1 : type_bytes(f->out_dtype);
+    fd_status s = FD_OK;
+    if ((s = op_rows(who, "a8", f->a8, f->a8_stride, 16, m, k)) != FD_OK) return s;
+    if ((s = op_rows(who, "w8", f->w8, f->w8_stride, 16, n, k)) != FD_OK) return s;
+    if ((s = op_rows(who, "a_scale", f->a_scale, f->a_scale_stride, 4, m, kb)) != FD_OK) return s;
+    if ((s = op_rows(who, "w_scale", f->w_scale, f->w_scale_stride, 4, nb, kb)) != FD_OK) return s;
+    if ((s = op_rows(who, "out", f->out, f->out_stride, es, m, n)) != FD_OK) return s;
+    if ((s = op_rows(who, "out_scale", f->out_scale, f->out_scale_stride, 4, m, nb)) != FD_OK) return s;
+    if (f->bias && !aligned_to(f->bias, type_bytes(f->bias_dtype))) return op_fail(FD_ERR_INVALID_ARG, "%s: bias is misaligned", who);
+    if (f->status_out && !aligned4(f->status_out)) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is misaligned", who);
+    if (m == 0) return FD_OK;
+    try {
+        std::string why;
+        const cudaError_t e = launch_matmul_fp8_blocks(*f, m, n, k, static_cast<cudaStream_t>(cuda_stream), &why);
+        return op_launched(who, e, why);
+    } catch (...) {
+        return op_fail(FD_ERR_CUDA, "%s: out of host memory", who);
+    }
+}
+
 fd_status fd_poll_status(fd_ctx* c, void* cuda_stream) {
     if (!c) return FD_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

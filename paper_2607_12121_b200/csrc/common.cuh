@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <string>
+
 #include "../../include/flashdiff.h"
 
 namespace fd {
@@ -54,6 +56,11 @@ __device__ __forceinline__ float gelu_tanh(float a) {
     float u = c * (a + 0.044715f * a * a * a);
     return 0.5f * a * (1.0f + tanhf(u));
 }
+
+// E4M3 rows with a scale per 128 columns (FP8_BLOCK): the largest code, and the smallest amax a scale is made from
+constexpr int FP8_BLOCK = 128;
+constexpr float E4M3_MAX = 448.0f;
+constexpr float FP8_AMAX_FLOOR = 0x1p-100f;
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -198,6 +205,18 @@ template <typename T>
 cudaError_t launch_update(const float* z, const T* y, const int32_t* active_idx, const int32_t* cu_active, const float* h,
                           const T* w_out, const T* b_out, float* drift, float* z_next, int B, int N, int D, int H,
                           float ln_eps, cudaStream_t st, int* n_launch);
+
+// rope_axes.cu
+cudaError_t launch_rope_axes(const fd_rope_spec& spec, const float* pos, int64_t tokens, int dh, int dtype, const fd_rope_rows* sets,
+                             int n_sets, bool inverse, cudaStream_t st);
+cudaError_t launch_rope_tables(const fd_rope_spec& spec, const float* pos, int64_t tokens, int dh, float* cos_out, float* sin_out,
+                               cudaStream_t st);
+
+// row_blocks.cu: residual addition + RMS norm (norm = false: none of both), 8-bit output with block scales
+cudaError_t launch_row_blocks(const fd_rmsnorm_args& a, int64_t rows, int cols, bool norm, cudaStream_t st);
+
+// tc_gemm_blocks.cu
+cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& a, int m, int n, int k, cudaStream_t st, std::string* why);
 
 // partition.cu
 size_t partition_scratch_bytes(int max_batch, int max_tokens, int max_regions);

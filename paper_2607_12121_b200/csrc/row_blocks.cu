@@ -1,0 +1,284 @@
+// Residual addition, RMS norm and the 8-bit form with a scale for every 128 columns, in one pass over the rows:
+//   r = x + residual,  y = r / sqrt(mean(r^2) + eps) * weight,  code = E4M3(y * (448 / amax)),  scale = amax / 448.
+// Bound by memory: every input element is read once and every output element written once.  A row stays in the
+// registers of W warps between the sum of squares and the output (16 lanes hold one block of 128 columns, 8 columns
+// each, so a block's amax is four shuffles and its codes leave as one 128-byte segment).  Sums, the norm and the scales
+// are fp32; the stored residual is the only rounding besides the outputs themselves.
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace fd {
+
+namespace {
+
+// eight consecutive values as fp32, 16-byte accesses
+template <typename T> __device__ __forceinline__ void load8(const T* p, float* f);
+template <> __device__ __forceinline__ void load8<float>(const float* p, float* f) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float* f) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float* f);
+template <> __device__ __forceinline__ void store8<float>(float* p, const float* f) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+struct RowArgs {
+    const void* x;
+    const void* residual;
+    void* residual_out;
+    const void* weight;
+    void* y;
+    uint8_t* y8;
+    float* y8_scale;
+    long long x_ld, res_ld, res_out_ld, y_ld, y8_ld, sc_ld;
+    long long rows;
+    int cols;
+    float eps;
+};
+
+// W warps hold one row, NV vectors of 8 columns per lane (cols <= 256 W NV, a multiple of 8)
+template <typename TX, typename TR, int W, int NV, bool NORM>
+__global__ void __launch_bounds__(W < 4 ? 128 : 32 * W)
+row_blocks_kernel(RowArgs a) {
+    constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
+    __shared__ float s_part[THREADS / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int wr = warp % W, rc = warp / W;                 // warp within its row, row within the CTA
+    const int col0 = (wr * 2 + (lane >> 4)) * FP8_BLOCK + (lane & 15) * 8;
+    ptx::pdl_wait();
+    for (long long row0 = (long long)blockIdx.x * RPC; row0 < a.rows; row0 += (long long)gridDim.x * RPC) {
+        const long long row = row0 + rc;
+        const bool live = row < a.rows;
+        const TX* x = static_cast<const TX*>(a.x) + row * a.x_ld;
+        float v[NV][8];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = col0 + i * W * 256;
+            if (live && c < a.cols) load8<TX>(x + c, v[i]);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+        }
+        if constexpr (NORM) {
+            if (a.residual) {
+                const TR* res = static_cast<const TR*>(a.residual) + row * a.res_ld;
+                float t[NV][8];
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = col0 + i * W * 256;
+                    if (live && c < a.cols) load8<TR>(res + c, t[i]);
+                    else
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) t[i][k] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[i][k] += t[i][k];
+            }
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) ss = fmaf(v[i][k], v[i][k], ss);
+            if (a.residual_out && live) {
+                TR* out = static_cast<TR*>(a.residual_out) + row * a.res_out_ld;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = col0 + i * W * 256;
+                    if (c < a.cols) store8<TR>(out + c, v[i]);
+                }
+            }
+            ss = warp_sum(ss);
+            if constexpr (W > 1) {
+                __syncthreads();                            // the previous row's readers are done
+                if (lane == 0) s_part[warp] = ss;
+                __syncthreads();
+                ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) ss += s_part[rc * W + i];
+            }
+            const float rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = col0 + i * W * 256;
+                float w[8];
+                if (a.weight && c < a.cols) load8<TX>(static_cast<const TX*>(a.weight) + c, w);
+                else
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = 1.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * rstd * w[k];
+            }
+            if (a.y && live) {
+                TX* y = static_cast<TX*>(a.y) + row * a.y_ld;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = col0 + i * W * 256;
+                    if (c < a.cols) store8<TX>(y + c, v[i]);
+                }
+            }
+        }
+        if (a.y8) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = col0 + i * W * 256;
+                float amax = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) amax = fmaxf(amax, fabsf(v[i][k]));
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                amax = fmaxf(amax, FP8_AMAX_FLOOR);
+                const float inv = E4M3_MAX / amax;
+                if (live && c < a.cols) {
+                    uint2 q;
+                    q.x = pack4_e4m3(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+                    q.y = pack4_e4m3(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+                    *reinterpret_cast<uint2*>(a.y8 + row * a.y8_ld + c) = q;
+                    if ((lane & 15) == 0) a.y8_scale[row * a.sc_ld + c / FP8_BLOCK] = amax / E4M3_MAX;
+                }
+            }
+        }
+    }
+    ptx::pdl_trigger();
+}
+
+// Any width, stride and alignment: one CTA per row, element accesses, the row read a second time for the output (each
+// element is read and written by the same thread there, so the in-place forms hold).  A warp takes a block at a time,
+// each lane four columns 32 apart.
+constexpr int ROW_ANY_THREADS = 256;
+
+template <typename TX, typename TR, bool NORM>
+__global__ void __launch_bounds__(ROW_ANY_THREADS)
+row_blocks_any_kernel(RowArgs a) {
+    __shared__ float s_part[ROW_ANY_THREADS / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int blocks = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
+    ptx::pdl_wait();
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const TX* x = static_cast<const TX*>(a.x) + row * a.x_ld;
+        const TR* res = NORM && a.residual ? static_cast<const TR*>(a.residual) + row * a.res_ld : nullptr;
+        float rstd = 1.f;
+        if constexpr (NORM) {
+            float ss = 0.f;
+            for (int c = threadIdx.x; c < a.cols; c += ROW_ANY_THREADS) {
+                const float r = to_f<TX>(x[c]) + (res ? to_f<TR>(res[c]) : 0.f);
+                ss = fmaf(r, r, ss);
+            }
+            ss = warp_sum(ss);
+            __syncthreads();
+            if (lane == 0) s_part[warp] = ss;
+            __syncthreads();
+            ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < ROW_ANY_THREADS / 32; ++i) ss += s_part[i];
+            rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+        }
+        for (int b = warp; b < blocks; b += ROW_ANY_THREADS / 32) {
+            float v[4];
+            float amax = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = b * FP8_BLOCK + k * 32 + lane;
+                v[k] = 0.f;
+                if (c < a.cols) {
+                    v[k] = to_f<TX>(x[c]);
+                    if constexpr (NORM) {
+                        if (res) v[k] += to_f<TR>(res[c]);
+                        if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(v[k]);
+                        v[k] = v[k] * rstd * (a.weight ? to_f<TX>(static_cast<const TX*>(a.weight)[c]) : 1.f);
+                        if (a.y) static_cast<TX*>(a.y)[row * a.y_ld + c] = from_f<TX>(v[k]);
+                    }
+                    amax = fmaxf(amax, fabsf(v[k]));
+                }
+            }
+            if (a.y8) {
+                amax = fmaxf(warp_max(amax), FP8_AMAX_FLOOR);
+                const float inv = E4M3_MAX / amax;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = b * FP8_BLOCK + k * 32 + lane;
+                    if (c < a.cols) a.y8[row * a.y8_ld + c] = __nv_cvt_float_to_fp8(v[k] * inv, __NV_SATFINITE, __NV_E4M3);
+                }
+                if (lane == 0) a.y8_scale[row * a.sc_ld + b] = amax / E4M3_MAX;
+            }
+        }
+    }
+    ptx::pdl_trigger();
+}
+
+template <typename TX, typename TR, int W, int NV, bool NORM>
+cudaError_t launch_reg(const RowArgs& a, cudaStream_t st) {
+    constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
+    const int grid = (int)min((a.rows + RPC - 1) / RPC, 1LL << 20);
+    return ptx::launch_kernel(row_blocks_kernel<TX, TR, W, NV, NORM>, grid, THREADS, 0, st, true, a);
+}
+
+template <typename TX, typename TR, int W, bool NORM>
+cudaError_t launch_nv(const RowArgs& a, cudaStream_t st) {
+    switch ((a.cols + 256 * W - 1) / (256 * W)) {
+        case 1: return launch_reg<TX, TR, W, 1, NORM>(a, st);
+        case 2: return launch_reg<TX, TR, W, 2, NORM>(a, st);
+        case 3: return launch_reg<TX, TR, W, 3, NORM>(a, st);
+        case 4: return launch_reg<TX, TR, W, 4, NORM>(a, st);
+        case 5: return launch_reg<TX, TR, W, 5, NORM>(a, st);
+        default: return launch_reg<TX, TR, W, 6, NORM>(a, st);
+    }
+}
+
+constexpr int ROW_MAX_NV = 6, ROW_MAX_W = 8;
+
+template <typename TX, typename TR, bool NORM>
+cudaError_t launch_typed(const RowArgs& a, cudaStream_t st) {
+    auto ok = [](const void* p, long long ld, int es) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0); };
+    const bool fast = a.cols % 8 == 0 && a.cols <= 256 * ROW_MAX_W * ROW_MAX_NV && ok(a.x, a.x_ld, sizeof(TX)) &&
+                      ok(a.residual, a.res_ld, sizeof(TR)) && ok(a.residual_out, a.res_out_ld, sizeof(TR)) &&
+                      ok(a.weight, 16, 1) && ok(a.y, a.y_ld, sizeof(TX)) &&
+                      (!a.y8 || ((reinterpret_cast<uintptr_t>(a.y8) & 7) == 0 && a.y8_ld % 8 == 0));
+    if (!fast) {
+        const int grid = (int)min(a.rows, 1LL << 20);
+        return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM>, grid, ROW_ANY_THREADS, 0, st, true, a);
+    }
+    // as few warps per row as hold it in their registers; more when the rows alone would leave SMs idle
+    int w = 1;
+    while (w < ROW_MAX_W && (a.cols > 256 * w * ROW_MAX_NV || (a.cols > 256 * w && a.rows * w < 148 * 4))) w *= 2;
+    switch (w) {
+        case 1: return launch_nv<TX, TR, 1, NORM>(a, st);
+        case 2: return launch_nv<TX, TR, 2, NORM>(a, st);
+        case 4: return launch_nv<TX, TR, 4, NORM>(a, st);
+        default: return launch_nv<TX, TR, 8, NORM>(a, st);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_row_blocks(const fd_rmsnorm_args& f, int64_t rows, int cols, bool norm, cudaStream_t st) {
+    RowArgs a{f.x, f.residual, f.residual_out, f.weight, f.y, static_cast<uint8_t*>(f.y8), f.y8_scale, f.x_stride, f.residual_stride,
+              f.residual_out_stride, f.y_stride, f.y8_stride, f.y8_scale_stride, rows, cols, f.eps};
+    const bool xb = f.x_dtype == FD_BF16, rb = f.residual_dtype == FD_BF16;
+    using bf = __nv_bfloat16;
+    if (!norm) return xb ? launch_typed<bf, bf, false>(a, st) : launch_typed<float, float, false>(a, st);
+    if (xb) return rb ? launch_typed<bf, bf, true>(a, st) : launch_typed<bf, float, true>(a, st);
+    return rb ? launch_typed<float, bf, true>(a, st) : launch_typed<float, float, true>(a, st);
+}
+
+}  // namespace fd

@@ -413,6 +413,11 @@ bool encode_tmap_bf16(CUtensorMap* out, void* base, int rank, const uint64_t* di
     return encode_tmap(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rank, dims, strides_bytes, box, swizzle_bytes, err);
 }
 
+bool encode_tmap_u8(CUtensorMap* out, void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                    const uint32_t* box, int swizzle_bytes, std::string* err) {
+    return encode_tmap(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, rank, dims, strides_bytes, box, swizzle_bytes, err);
+}
+
 struct GemmSpec {
     CUtensorMap a;              // activation operand
     int n_out, k, bn;
