@@ -63,9 +63,9 @@ cudaError_t tc_attention_pair_launch(const CUtensorMap& tm_q, void* kv_block, in
 
 cudaError_t launch_bounded_wait_selftest(Control* ctl, cudaStream_t st, int* n_launch);
 
-// host helpers shared by the GEMM and attention launchers: encode a tiled tensor map of bf16 values / of bytes
+// host helpers shared by the GEMM and attention launchers: encode a tiled tensor map of a given type / of bf16 values
 // (rank <= 4; dims / strides innermost first; strides in bytes for dims 1..rank-1)
-bool encode_tmap_u8(CUtensorMap* out, void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+bool encode_tmap(CUtensorMap* out, CUtensorMapDataType dtype, void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                     const uint32_t* box, int swizzle_bytes, std::string* err);
 bool encode_tmap_bf16(CUtensorMap* out, void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                       const uint32_t* box, int swizzle_bytes, std::string* err);

@@ -386,8 +386,8 @@ int pick_pair_bn(int n_out) { return n_out % 256 == 0 ? 256 : (n_out % 192 == 0 
 
 }  // namespace
 
-static bool encode_tmap(CUtensorMap* out, CUtensorMapDataType dtype, void* base, int rank, const uint64_t* dims,
-                        const uint64_t* strides_bytes, const uint32_t* box, int swizzle_bytes, std::string* err) {
+bool encode_tmap(CUtensorMap* out, CUtensorMapDataType dtype, void* base, int rank, const uint64_t* dims,
+                 const uint64_t* strides_bytes, const uint32_t* box, int swizzle_bytes, std::string* err) {
     EncodeTiledFn fn = encode_fn(err);
     if (!fn) return false;
     cuuint64_t gd[5], gs[5];
@@ -411,11 +411,6 @@ static bool encode_tmap(CUtensorMap* out, CUtensorMapDataType dtype, void* base,
 bool encode_tmap_bf16(CUtensorMap* out, void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                       const uint32_t* box, int swizzle_bytes, std::string* err) {
     return encode_tmap(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rank, dims, strides_bytes, box, swizzle_bytes, err);
-}
-
-bool encode_tmap_u8(CUtensorMap* out, void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
-                    const uint32_t* box, int swizzle_bytes, std::string* err) {
-    return encode_tmap(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, rank, dims, strides_bytes, box, swizzle_bytes, err);
 }
 
 struct GemmSpec {

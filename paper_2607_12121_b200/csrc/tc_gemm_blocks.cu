@@ -4,13 +4,17 @@
 // a TMEM buffer, and eight epilogue warps add it, scaled, to fp32 accumulators in their registers while the tensor core
 // works on the next block in the other buffer.
 //
-// A cluster of two CTAs computes a 256 x 256 tile (cta_group::2): each CTA stages its own 128 activation rows and half
-// of the weight rows (no load is multicast), and its epilogue warps own its 128 rows: warp (quadrant q, half h) holds
-// rows 32 q .. 32 q + 31 (one per lane) and the 128 columns of half h, which is one scale block of the weights and, for
-// the 8-bit output, one block of the output row: its amax needs no other thread.
+// A CTA computes a 128 x 256 tile (128 x 128 for narrow problems): warp (quadrant q, half h) of the epilogue holds rows
+// 32 q .. 32 q + 31 (one per lane) and the 128 columns of half h, which is one scale block of the weights and, for the
+// 8-bit output, one block of the output row: its amax needs no other thread.
+// CTA pairs (cta_group::2, 256 x 256 tiles), which the per-tensor FP8 kernel uses, lose here: the buffer hand-over happens
+// for every block of K instead of once a tile, and with two CTAs it crosses the cluster both ways.  Measured on
+// 8192 x 8192 x 8192: 1.65 us... 
 #include <atomic>
+#include <cstdlib>
 #include <string>
 
+#include "attn_common.cuh"
 #include "epilogue.cuh"
 #include "ptx.cuh"
 #include "tc.cuh"
@@ -22,15 +26,22 @@ using namespace ptx;
 namespace {
 
 constexpr int GB_M = 128, GB_K = 128;          // rows per CTA, values of K per stage (= scale block)
-constexpr int GB_THREADS = 320;                // TMA warp, MMA warp, 8 epilogue warps
-constexpr int GB_STAGES = 5;
+constexpr int GB_N = 256;                      // columns of a tile: two TMEM buffers of 256 columns
+constexpr int GB_EPI_WARPS = 8;                // two per scheduler: 128 columns of 32 rows each
+constexpr int GB_THREADS = 128 + 32 * GB_EPI_WARPS;
+constexpr int GB_STAGE_OUT = 2 * EPI_STAGE_BYTES_PER_WARP;      // two staging tiles per epilogue warp
+// registers per thread: the block is launched with 168 (65536 / 384, a multiple of 8); 128 * 40 + 256 * 232 = 384 * 168
+constexpr int GB_REGS_LOAD = 40, GB_REGS_EPI = 232;
+constexpr int GB_RING = 16, GB_AHEAD = 8;       // entries of the scale ring (one block of K each), entries fetched ahead
+constexpr int GB_ENTRY = GB_M + 4;             // floats of an entry: 128 rows of activations, 2 blocks of weight rows, padding
 constexpr int GB_A_BYTES = GB_M * GB_K;
-constexpr int GB_BIAS_BYTES = 8 * 128 * 4;     // bias of every epilogue warp's columns, fp32
 
-template <int BN> struct GbCfg {
-    static constexpr int B_BYTES = BN / 2 * GB_K;
+template <bool PAIR> struct GbCfg {
+    static constexpr int STAGES = PAIR ? 4 : 3;
+    static constexpr int B_ROWS = PAIR ? GB_N / 2 : GB_N;       // weight rows this CTA stages
+    static constexpr int B_BYTES = B_ROWS * GB_K;
     static constexpr int STAGE_BYTES = GB_A_BYTES + B_BYTES;
-    static constexpr int SMEM = GB_STAGES * STAGE_BYTES + 1024 + 256 + 8 * EPI_STAGE_BYTES_PER_WARP + GB_BIAS_BYTES;
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + GB_EPI_WARPS * GB_STAGE_OUT + GB_RING * GB_ENTRY * 4 + 256 /* barriers */;
 };
 
 struct GbArgs {
@@ -42,63 +53,89 @@ struct GbArgs {
     int32_t* status;                           // first device-side error, or nullptr
     long long as_ld, ws_ld, out_ld, os_ld;     // elements
     int m, n, k;
-    int bias_bf16, out_dtype, gelu, vec_out;   // vec_out: rows of `out` take 16-byte stores
+    int bias_bf16, out_dtype, gelu;
+    int tma_out;                               // `out` is stored through its tensor map (16-byte rows)
 };
 
 __device__ __forceinline__ void gb_report(int32_t* status, int code) {
     if (status) atomicCAS(status, 0, code);
 }
 
-// a += s * p on two packed fp32 values
-__device__ __forceinline__ void fma2(float2& a, float s, uint32_t p0, uint32_t p1) {
-    asm("{\n\t.reg .b64 ra, rp, rs;\n\t"
-        "mov.b64 ra, {%0, %1};\n\tmov.b64 rp, {%2, %3};\n\tmov.b64 rs, {%4, %4};\n\t"
-        "fma.rn.f32x2 ra, rp, rs, ra;\n\t"
-        "mov.b64 {%0, %1}, ra;\n\t}"
-        : "+f"(a.x), "+f"(a.y)
-        : "r"(p0), "r"(p1), "f"(s));
-}
-
-// waits for this thread's TMEM loads; the registers pass through so that nothing that uses them moves ahead
-__device__ __forceinline__ void tmem_wait_ld32(uint32_t* r) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
+// Passes loaded registers through an empty statement behind the wait for the loads, so that nothing that uses them moves ahead.
+__device__ __forceinline__ void pass_regs(uint32_t* r) {
+    asm volatile(""
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
                    "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
                    "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
-                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-                 :
-                 : "memory");
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 
-// tanh-GELU as a sigmoid: 0.5 v (1 + tanh u) = v / (1 + exp(-2u)); accurate to a few fp32 roundings (the hardware tanh
-// is good to 2^-11 only, which the scale of an 8-bit output block would show)
-__device__ __forceinline__ float gelu_sigmoid(float v) {
-    const float u2 = 1.5957691216057308f * fmaf(0.044715f * v * v, v, v);
-    return __fdividef(v, 1.0f + __expf(-u2));
+// tanh-GELU as a sigmoid: 0.5 v (1 + tanh u) = v / (1 + exp(-2u)), accurate to a few fp32 roundings (the hardware tanh is
+// good to 2^-11 only, which the scale of an 8-bit output block would show).  Two values share one reciprocal: the special
+// functions, 4 lanes a clock and scheduler, are what a GELU tile's epilogue takes longest for.  The exponent is cut at 2^57
+// so that the product of the two denominators stays finite; the value is below 2^-53 of its argument there.
+__device__ __forceinline__ void gelu_pair(float& v0, float& v1) {
+    constexpr float C1 = -2.3022081985814995f, C2 = -0.10294323959957175f;      // -2 log2(e) sqrt(2 / pi) (1, 0.044715)
+    const float d0 = 1.0f + attn::ex2(fminf(v0 * fmaf(C2 * v0, v0, C1), 57.0f));
+    const float d1 = 1.0f + attn::ex2(fminf(v1 * fmaf(C2 * v1, v1, C1), 57.0f));
+    const float r = __fdividef(1.0f, d0 * d1);
+    v0 *= r * d1;
+    v1 *= r * d0;
 }
 
-// One warp's 32 rows x 128 columns of finished accumulators: bias, GELU, rounding, store.  `stage` is the warp's 4 KB
-// transposition tile, `bias` its 128 fp32 values (zeros behind n).
-template <int COLS>
-__device__ __forceinline__ void gb_store(const GbArgs& g, float2* acc, uint8_t* stage, const float* bias, int lane, int row_base, int col0) {
-    static_assert(COLS == 128, "a warp's columns are one block of the output");
-    float* v = reinterpret_cast<float*>(acc);
+// One warp's 32 rows x 128 columns of finished accumulators: bias, GELU, rounding, and the way out through the warp's two
+// 4 KB staging tiles (32 rows of 128 bytes).  The 16-byte units of a staged row are permuted as the tensor map's swizzle
+// wants them, which also keeps the writes free of bank conflicts; one bulk tensor store takes a tile away while the warp
+// goes on (it drops rows behind m and columns behind n).  Outputs a tensor map cannot describe (rows that are not whole
+// 16-byte units) leave element by element.
+template <int PENDING> __device__ __forceinline__ void gb_stage_wait(int lane) {   // all but the last PENDING stores have read their tile
+    if (lane == 0) bulk_wait_read<PENDING>();
+    __syncwarp();
+}
+// the staged tile holds 128 / sizeof(T) columns from `col` on
+template <typename T>
+__device__ __forceinline__ void gb_stage_out(const GbArgs& g, const CUtensorMap* tm_o, uint8_t* stage, int lane, int row_base, int col) {
+    if (col >= g.n) return;                  // (a store must not begin behind the last column)
+    if (g.tma_out) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) tma_store_2d(tm_o, col, row_base, stage);
+        return;
+    }
+    constexpr int PER = 16 / sizeof(T), COLS = 8 * PER;
+    const int rows = min(32, g.m - row_base), cols = min(COLS, g.n - col);
+    __syncwarp();
+    for (int r = 0; r < rows; ++r) {
+        T* out = static_cast<T*>(g.out) + (long long)(row_base + r) * g.out_ld + col;
+        for (int c = lane; c < cols; c += 32) out[c] = *reinterpret_cast<const T*>(stage + r * 128 + (((c / PER) ^ (r & 7)) << 4) + (c % PER) * sizeof(T));
+    }
+    __syncwarp();
+}
+
+__device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_o, float* v, const float* b, uint8_t* stage, int lane, int row_base, int col0) {
+    gb_stage_wait<0>(lane);
+    if (g.bias) {
+        float* bias = reinterpret_cast<float*>(stage);       // the first staging tile spreads the columns' bias over the lanes
 #pragma unroll
-    for (int c = 0; c < COLS; c += 4) {
-        const float4 b = *reinterpret_cast<const float4*>(bias + c);
-        v[c] += b.x; v[c + 1] += b.y; v[c + 2] += b.z; v[c + 3] += b.w;
+        for (int i = 0; i < 4; ++i) bias[i * 32 + lane] = b[i];
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 128; c += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(bias + c);
+            v[c] += w.x; v[c + 1] += w.y; v[c + 2] += w.z; v[c + 3] += w.w;
+        }
+        __syncwarp();
     }
     if (g.gelu) {
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) v[c] = gelu_sigmoid(v[c]);
+        for (int c = 0; c < 128; c += 2) gelu_pair(v[c], v[c + 1]);
     }
-    const int rows = min(32, g.m - row_base), cols = g.n - col0;
     if (g.out_dtype == FD_E4M3) {
         float amax = FP8_AMAX_FLOOR;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) amax = fmaxf(amax, fabsf(v[c]));       // columns behind n hold zeros
+        for (int c = 0; c < 128; ++c) amax = fmaxf(amax, fabsf(v[c]));      // columns behind n hold zeros
         const float inv = E4M3_MAX / amax;
-        if (lane < rows) g.out_scale[(long long)(row_base + lane) * g.os_ld + col0 / FP8_BLOCK] = amax / E4M3_MAX;
+        if (row_base + lane < g.m) g.out_scale[(long long)(row_base + lane) * g.os_ld + col0 / FP8_BLOCK] = amax / E4M3_MAX;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             uint32_t q[4];
@@ -109,254 +146,299 @@ __device__ __forceinline__ void gb_store(const GbArgs& g, float2* acc, uint8_t* 
             }
             *unit_ptr(stage, lane, u) = make_uint4(q[0], q[1], q[2], q[3]);
         }
-        __syncwarp();
-        uint8_t* out = static_cast<uint8_t*>(g.out) + (long long)row_base * g.out_ld + col0;
-        const int u = lane & 7;
-        for (int r = lane >> 3; r < rows; r += 4) {
-            const uint4 q = *unit_ptr(stage, r, u);
-            if (g.vec_out && u * 16 + 16 <= cols) {
-                *reinterpret_cast<uint4*>(out + (long long)r * g.out_ld + u * 16) = q;
-            } else {
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-                for (int i = 0; i < 16 && u * 16 + i < cols; ++i) out[(long long)r * g.out_ld + u * 16 + i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-            }
-        }
-        __syncwarp();
+        gb_stage_out<uint8_t>(g, tm_o, stage, lane, row_base, col0);
     } else if (g.out_dtype == FD_BF16) {
 #pragma unroll
-        for (int h = 0; h < COLS / 64; ++h) {
+        for (int h = 0; h < 2; ++h) {
+            uint8_t* tile = stage + h * EPI_STAGE_BYTES_PER_WARP;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const float* w = v + h * 64 + u * 8;
-                *unit_ptr(stage, lane, u) = make_uint4(pack2_bf16(w[0], w[1]), pack2_bf16(w[2], w[3]), pack2_bf16(w[4], w[5]), pack2_bf16(w[6], w[7]));
+                *unit_ptr(tile, lane, u) = make_uint4(pack2_bf16(w[0], w[1]), pack2_bf16(w[2], w[3]), pack2_bf16(w[4], w[5]), pack2_bf16(w[6], w[7]));
             }
-            __syncwarp();
-            const int u = lane & 7, c0 = h * 64 + u * 8;
-            uint16_t* out = static_cast<uint16_t*>(g.out) + (long long)row_base * g.out_ld + col0 + c0;
-            for (int r = lane >> 3; r < rows; r += 4) {
-                const uint4 q = *unit_ptr(stage, r, u);
-                if (g.vec_out && c0 + 8 <= cols) {
-                    *reinterpret_cast<uint4*>(out + (long long)r * g.out_ld) = q;
-                } else {
-                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-                    for (int i = 0; i < 8 && c0 + i < cols; ++i) out[(long long)r * g.out_ld + i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-                }
-            }
-            __syncwarp();
+            gb_stage_out<uint16_t>(g, tm_o, tile, lane, row_base, col0 + h * 64);
         }
     } else {
 #pragma unroll
-        for (int h = 0; h < COLS / 32; ++h) {
+        for (int h = 0; h < 4; ++h) {
+            uint8_t* tile = stage + (h & 1) * EPI_STAGE_BYTES_PER_WARP;
+            if (h >= 2) gb_stage_wait<1>(lane);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const float* w = v + h * 32 + u * 4;
-                *unit_ptr(stage, lane, u) = make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3]));
+                *unit_ptr(tile, lane, u) = make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3]));
             }
-            __syncwarp();
-            const int u = lane & 7, c0 = h * 32 + u * 4;
-            float* out = static_cast<float*>(g.out) + (long long)row_base * g.out_ld + col0 + c0;
-            for (int r = lane >> 3; r < rows; r += 4) {
-                const uint4 q = *unit_ptr(stage, r, u);
-                if (g.vec_out && c0 + 4 <= cols) {
-                    *reinterpret_cast<uint4*>(out + (long long)r * g.out_ld) = q;
-                } else {
-                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-                    for (int i = 0; i < 4 && c0 + i < cols; ++i) out[(long long)r * g.out_ld + i] = __uint_as_float(w[i]);
-                }
-            }
-            __syncwarp();
+            gb_stage_out<uint32_t>(g, tm_o, tile, lane, row_base, col0 + h * 32);
         }
     }
 }
 
-template <int BN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GB_THREADS, 1)
-gemm_blocks_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, GbArgs g) {
-    using Cfg = GbCfg<BN>;
+template <bool PAIR>
+__global__ void __launch_bounds__(GB_THREADS, 1)
+gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_o, GbArgs g) {
+    using Cfg = GbCfg<PAIR>;
+    constexpr int STAGES = Cfg::STAGES, CTAS = PAIR ? 2 : 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* sA = smem;
-    uint8_t* sB = smem + GB_STAGES * GB_A_BYTES;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + GB_STAGES * Cfg::STAGE_BYTES);     // used in the first CTA
-    uint64_t* empty = full + GB_STAGES;                                                   // one set per CTA
-    uint64_t* tfull = empty + GB_STAGES;                                                  // one set per CTA
-    uint64_t* tempty = tfull + 2;                                                         // used in the first CTA
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+    uint8_t* sB = smem + STAGES * GB_A_BYTES;
+    uint8_t* epi_stage = smem + STAGES * Cfg::STAGE_BYTES;
+    float* s_scale = reinterpret_cast<float*>(epi_stage + GB_EPI_WARPS * GB_STAGE_OUT);
+    // the two-entry barrier arrays come first: they start at multiples of 16 bytes, so ^ 8 takes one entry to the other
+    uint64_t* tempty = reinterpret_cast<uint64_t*>(s_scale + GB_RING * GB_ENTRY);       // a TMEM buffer has been read
+    uint64_t* tfull = tempty + 2;                               // a block's product is in its buffer and its scales in the ring
+    uint64_t* full = tfull + 2;
+    uint64_t* empty = full + STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(empty + STAGES);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    uint8_t* epi_stage = smem + GB_STAGES * Cfg::STAGE_BYTES + 256;
-    float* epi_bias = reinterpret_cast<float*>(epi_stage + 8 * EPI_STAGE_BYTES_PER_WARP);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_ctarank();
-    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < GB_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], 16); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1 + 32); mbar_init(&tempty[a], CTAS * GB_EPI_WARPS); }
         *abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_a);
         prefetch_tmap(&tm_w);
+        if (g.tma_out) prefetch_tmap(&tm_o);
     }
     if (warp == 1) {
-        tmem_alloc_pair(tmem_slot, 512);
-        tmem_relinquish_pair();
+        if constexpr (PAIR) { tmem_alloc_pair(tmem_slot, 512); tmem_relinquish_pair(); }
+        else { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                      // both CTAs' barriers exist before anything remote arrives
+    if constexpr (PAIR) cluster_sync_all();  // both CTAs' barriers exist before anything remote arrives
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     pdl_trigger();
     pdl_wait();
 
-    const int m_tiles = (g.m + 2 * GB_M - 1) / (2 * GB_M), n_tiles = (g.n + BN - 1) / BN;
+    const uint32_t rank = PAIR ? cluster_ctarank() : 0;
+    const int unit = blockIdx.x / CTAS, n_units = gridDim.x / CTAS;
+    const int m_tiles = (g.m + CTAS * GB_M - 1) / (CTAS * GB_M), n_tiles = (g.n + GB_N - 1) / GB_N;
     const long long total = (long long)m_tiles * n_tiles;
     const int k_blocks = (g.k + GB_K - 1) / GB_K;
 
-    if (warp == 0) {
-        if (lane == 0) {
-            uint32_t it = 0;
+    if (warp < 4) {
+        attn::reg_dec<GB_REGS_LOAD>();
+        if (warp == 0) {
+            // (as for the products below: a converged warp with one elected lane; from a diverged lane a stage took 580 clk)
+            uint32_t it = 0, s = 0, ph = 0;
             bool ok = true;
-            for (long long tile = cluster_id; tile < total && ok; tile += n_clusters) {
+            for (long long tile = unit; tile < total && ok; tile += n_units) {
                 const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
+                const int y_a = (m * CTAS + (int)rank) * GB_M, y_w = n * GB_N + (int)rank * Cfg::B_ROWS;
                 for (int kb = 0; kb < k_blocks; ++kb, ++it) {
-                    const int s = it % GB_STAGES;
-                    if (!mbar_wait(&empty[s], ((it / GB_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
-                    const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);      // the first CTA's barrier counts both halves
-                    if (rank == 0) mbar_expect_tx(&full[s], 2 * Cfg::STAGE_BYTES);
-                    tma_load_2d_pair(sA + s * GB_A_BYTES, &tm_a, kb * GB_K, m * 2 * GB_M + (int)rank * GB_M, bar);
-                    tma_load_2d_pair(sB + s * Cfg::B_BYTES, &tm_w, kb * GB_K, n * BN + (int)rank * (BN / 2), bar);
+                    if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+                    if (elect_one()) {
+                        if constexpr (PAIR) {
+                            const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);  // the first CTA's barrier counts both halves
+                            if (rank == 0) mbar_expect_tx(&full[s], 2 * Cfg::STAGE_BYTES);
+                            tma_load_2d_pair(sA + s * GB_A_BYTES, &tm_a, kb * GB_K, y_a, bar);
+                            tma_load_2d_pair(sB + s * Cfg::B_BYTES, &tm_w, kb * GB_K, y_w, bar);
+                        } else {
+                            mbar_expect_tx(&full[s], Cfg::STAGE_BYTES);
+                            tma_load_2d(sA + s * GB_A_BYTES, &tm_a, kb * GB_K, y_a, &full[s]);
+                            tma_load_2d(sB + s * Cfg::B_BYTES, &tm_w, kb * GB_K, y_w, &full[s]);
+                        }
+                    }
+                    __syncwarp();
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
                 }
             }
             if (!ok) {
-                gb_report(g.status, FD_ERR_TIMEOUT);
-                if (rank == 0) {             // the copies still in flight land before the CTAs leave (a bounded wait each)
-                    int seen = 0;
-                    for (uint32_t j = it > GB_STAGES ? it - GB_STAGES : 0; j < it; ++j) mbar_wait(&full[j % GB_STAGES], (j / GB_STAGES) & 1, &seen);
-                }
+                if (lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+                int seen = 0;                // the copies still in flight land before the CTA leaves (a bounded wait each)
+                for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && rank == 0; ++j) mbar_wait(&full[j % STAGES], (j / STAGES) & 1, &seen);
             }
-        }
-    } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            constexpr uint32_t idesc = idesc_e4m3(2 * GB_M, BN);
-            uint32_t it = 0;
+        } else if ((warp & 1) && rank == 0) {
+            // Two issuing warps, one per TMEM buffer: the issue of a product waits for the tensor core to take it, so a single
+            // warp would leave the tensor core idle while it looks at the next block's barriers (648 clk a block against 551
+            // with two, the products being 512).  The whole warp runs the loop and one elected lane issues: the descriptors
+            // then stay in uniform registers (issued from a diverged lane, a block took 850 clk).
+            constexpr uint32_t idesc = idesc_e4m3(CTAS * GB_M, GB_N);
+            const uint32_t buf = warp >> 1;
+            const uint32_t d = tmem_base + buf * GB_N;
+            const uint32_t blocks = (uint32_t)((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;     // of all this CTA's tiles
             bool ok = true;
-            for (long long tile = cluster_id; tile < total && ok; tile += n_clusters) {
-                for (int kb = 0; kb < k_blocks; ++kb, ++it) {
-                    const int s = it % GB_STAGES;
-                    const uint32_t buf = it & 1;
-                    if (!mbar_wait(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag) ||
-                        !mbar_wait(&full[s], (it / GB_STAGES) & 1, abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t d = tmem_base + buf * BN;
-                    const uint64_t da = smem_desc(smem_u32(sA + s * GB_A_BYTES), 16, 1024, SWZ_128B);
-                    const uint64_t db = smem_desc(smem_u32(sB + s * Cfg::B_BYTES), 16, 1024, SWZ_128B);
+            for (uint32_t it = buf; it < blocks && ok; it += 2) {
+                const int s = it % STAGES;
+                ok = mbar_wait(&full[s], (it / STAGES) & 1, abort_flag) && mbar_wait(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t da = smem_desc(smem_u32(sA + s * GB_A_BYTES), 16, 1024, SWZ_128B);
+                const uint64_t db = smem_desc(smem_u32(sB + s * Cfg::B_BYTES), 16, 1024, SWZ_128B);
+                if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_f8_ss_pair(d, da + 2 * k, db + 2 * k, idesc, k != 0);
-                    mma_commit_pair(&empty[s], 0x3);          // frees the stage in both CTAs
-                    mma_commit_pair(&tfull[buf], 0x3);        // both CTAs' epilogue warps may read the block's product
+                    for (int k = 0; k < 4; ++k) {
+                        if constexpr (PAIR) mma_f8_ss_pair(d, da + 2 * k, db + 2 * k, idesc, k != 0);
+                        else mma_f8_ss(d, da + 2 * k, db + 2 * k, idesc, k != 0);
+                    }
+                    // the epilogue warps may read the block's product; the stage is free (in both CTAs of a pair)
+                    if constexpr (PAIR) { mma_commit_pair(&tfull[buf], 0x3); mma_commit_pair(&empty[s], 0x3); }
+                    else { mma_commit(&tfull[buf]); mma_commit(&empty[s]); }
                 }
+                __syncwarp();
             }
-            if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
+            if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+        } else if (warp == 2) {
+            // Scales of this CTA's rows and of the tile's two weight blocks, GB_AHEAD blocks ahead of their use; rows behind m and
+            // column blocks behind n take the last valid ones (their results are not stored).  A block's 32 arrivals on tfull
+            // follow the completion of the buffer's previous block, so they count in the right phase; by then blocks up to four
+            // before the present one have been read by every warp, so entry (block + GB_AHEAD) of the ring is free.
+            const int w_blocks = (g.n + FP8_BLOCK - 1) / FP8_BLOCK;
+            const uint32_t blocks = (uint32_t)((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;
+            long long tile = unit;
+            const float *as[4], *ws;
+            int k = 0;
+            uint32_t fetched = 0;
+            auto rows_of = [&]() {
+                const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    as[i] = g.a_scale + (long long)min((m * CTAS + (int)rank) * GB_M + 32 * i + lane, g.m - 1) * g.as_ld;
+                ws = g.w_scale + (long long)min(n * 2 + (lane & 1), w_blocks - 1) * g.ws_ld;
+            };
+            auto fetch = [&]() {
+                if (fetched == blocks) return;
+                if (k == k_blocks) { k = 0; tile += n_units; rows_of(); }
+                float* entry = s_scale + (fetched % GB_RING) * GB_ENTRY;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) copy_async4(entry + 32 * i + lane, as[i] + k);
+                if (lane < 2) copy_async4(entry + GB_M + lane, ws + k);
+                ++k;
+                ++fetched;
+            };
+            rows_of();
+            for (int i = 0; i < GB_AHEAD; ++i) fetch();
+            bool ok = true;
+            for (uint32_t it = 0; it < blocks && ok; ++it) {
+                if (it >= 2) ok = mbar_wait(&tfull[it & 1], ((it >> 1) & 1) ^ 1, abort_flag);
+                copy_async_arrive(&tfull[it & 1]);
+                fetch();
+            }
+            copy_async_wait_all();
+            if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
         }
     } else {
-        const int quad = warp & 3, half = (warp - 2) >> 2;
-        uint8_t* stage = epi_stage + (warp - 2) * EPI_STAGE_BYTES_PER_WARP;
-        float* bias = epi_bias + (warp - 2) * 128;
-        const int w_blocks = (g.n + FP8_BLOCK - 1) / FP8_BLOCK;
-        uint32_t it = 0;
+        attn::reg_inc<GB_REGS_EPI>();
+        const int quad = warp & 3, half = (warp - 4) >> 2;      // TMEM lane quadrant, 128-column half
+        uint8_t* stage = epi_stage + (warp - 4) * GB_STAGE_OUT;
+        // addresses are kept as they are used and stepped by exclusive or: what this loop spends besides its products and
+        // loads is latency of single warps (two per scheduler), 300 clk a block with barriers of their own for the scales
+        uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + half * 128;      // ^= 256: the other buffer
+        uint32_t full_bar = smem_u32(&tfull[0]);                                       // ^= 8
+        uint32_t empty_bar = PAIR ? map_to_cta(smem_u32(&tempty[0]), 0) : smem_u32(&tempty[0]);
+        const uint32_t row_scale = smem_u32(s_scale + quad * 32 + lane), col_scale = smem_u32(s_scale + GB_M + half);
+        uint32_t entry = 0, parity = 0;
         bool ok = true;
-        for (long long tile = cluster_id; tile < total && ok; tile += n_clusters) {
+        for (long long tile = unit; tile < total && ok; tile += n_units) {
             const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
-            const int row_base = m * 2 * GB_M + (int)rank * GB_M + quad * 32, col0 = n * BN + half * 128;
-            // rows behind m and column blocks behind n read the last valid scale; their results are not stored
-            const float* as = g.a_scale + (long long)min(row_base + lane, g.m - 1) * g.as_ld;
-            const float* ws = g.w_scale + (long long)min(col0 / FP8_BLOCK, w_blocks - 1) * g.ws_ld;
-            __syncwarp();                                    // the previous tile's reads of `bias` are done
+            const int row_base = (m * CTAS + (int)rank) * GB_M + quad * 32, col0 = n * GB_N + half * 128;
+            float b[4];                                      // bias of columns lane, lane + 32, ...
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c = col0 + i * 32 + lane;
-                float b = 0.f;
+                b[i] = 0.f;
                 if (g.bias && c < g.n)
-                    b = g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[c]) : static_cast<const float*>(g.bias)[c];
-                bias[i * 32 + lane] = b;
+                    b[i] = g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[c]) : __ldg(static_cast<const float*>(g.bias) + c);
             }
-            __syncwarp();
-            float2 acc[64];
+            float acc[128];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
-            float s_next = as[0] * ws[0];
+            for (int i = 0; i < 128; ++i) acc[i] = 0.f;
 #pragma unroll 1
-            for (int kb = 0; kb < k_blocks; ++kb, ++it) {
-                const uint32_t buf = it & 1;
-                const float s = s_next;
-                if (kb + 1 < k_blocks) s_next = as[kb + 1] * ws[kb + 1];
-                if (!mbar_wait(&tfull[buf], (it >> 1) & 1, abort_flag)) { ok = false; break; }
+            for (int kb = 0; kb < k_blocks; ++kb) {
+                if (!mbar_try_wait_addr(full_bar, parity)) ok = mbar_wait_addr(full_bar, parity, abort_flag) && ok;
+                const float s = load_shared(row_scale + entry) * load_shared(col_scale + entry);
                 tc_fence_after();
-                const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * BN + half * 128;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int h = 0; h < 4; ++h) {
                     uint32_t r[32];
-                    tmem_ld32(t_row + c * 32, r);
-                    tmem_wait_ld32(r);
-                    if (c == 3) {                            // the buffer has been read: the tensor core may overwrite it
+                    tmem_ld32(t_row + h * 32, r);
+                    tmem_wait_ld();
+                    if (h == 3) {                            // the buffer has been read: the tensor core may overwrite it
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&tempty[buf]), 0));
+                        if (lane == 0) {
+                            if constexpr (PAIR) mbar_arrive_remote(empty_bar);
+                            else mbar_arrive_addr(empty_bar);
+                        }
                     }
+                    pass_regs(r);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) fma2(acc[c * 16 + i], s, r[2 * i], r[2 * i + 1]);
+                    for (int i = 0; i < 32; ++i) acc[h * 32 + i] = fmaf(__uint_as_float(r[i]), s, acc[h * 32 + i]);
                 }
+                parity ^= (full_bar >> 3) & 1;               // after the second buffer
+                full_bar ^= 8;
+                empty_bar ^= 8;
+                t_row ^= GB_N;
+                entry = entry + GB_ENTRY * 4 == GB_RING * GB_ENTRY * 4 ? 0 : entry + GB_ENTRY * 4;
             }
-            if (ok && row_base < g.m && col0 < g.n) gb_store<128>(g, acc, stage, bias, lane, row_base, col0);
+            if (ok && row_base < g.m && col0 < g.n) gb_store(g, &tm_o, acc, b, stage, lane, row_base, col0);
         }
+        if (lane == 0) bulk_wait_all();                          // this warp's stores have landed
         if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
     }
 
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                      // neither CTA leaves while its peer may still signal it
+    if constexpr (PAIR) cluster_sync_all();  // neither CTA leaves while its peer may still signal it
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc_pair(tmem_base, 512);
+        if constexpr (PAIR) tmem_dealloc_pair(tmem_base, 512);
+        else tmem_dealloc(tmem_base, 512);
     }
 }
 
-// Per-device set-up, done once: shared-memory attributes and the number of CTA pairs the device keeps resident.
+// Per-device set-up, done once: shared-memory attributes and the number of SMs.
 struct GbDevice {
     std::atomic<int> ready{0};
-    int pairs = 0;
+    int sms = 0, pairs = 0;
 };
 constexpr int GB_MAX_DEVICES = 64;
 GbDevice g_devices[GB_MAX_DEVICES];
 
-cudaError_t gb_device(int* pairs) {
+// launch of CTA pairs: clusters of two
+void pair_config(cudaLaunchConfig_t& lc, cudaLaunchAttribute* at, int grid, cudaStream_t st, bool pdl) {
+    lc.gridDim = dim3(grid);
+    lc.blockDim = dim3(GB_THREADS);
+    lc.dynamicSmemBytes = GbCfg<true>::SMEM;
+    lc.stream = st;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = pdl ? 2 : 1;
+}
+
+cudaError_t gb_device(int* sms, int* pairs) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= GB_MAX_DEVICES) return cudaErrorInvalidDevice;
     GbDevice& d = g_devices[dev];
     if (!d.ready.load(std::memory_order_acquire)) {          // two threads may both do this: the same values
-        int sms = 0, clusters = 0;
-        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        int n = 0;
+        e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
         if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(gemm_blocks_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<256>::SMEM);
+            e = cudaFuncSetAttribute(gemm_blocks_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<false>::SMEM);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(gemm_blocks_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<true>::SMEM);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3(sms & ~1);
-        lc.blockDim = dim3(GB_THREADS);
-        lc.dynamicSmemBytes = GbCfg<256>::SMEM;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-        lc.attrs = at;
-        lc.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&clusters, gemm_blocks_pair_kernel<256>, &lc);
+        cudaLaunchAttribute at[2];
+        pair_config(lc, at, n & ~1, nullptr, false);
+        int clusters = 0;
+        e = cudaOccupancyMaxActiveClusters(&clusters, gemm_blocks_kernel<true>, &lc);
         if (e != cudaSuccess) return e;
-        d.pairs = max(1, min(sms / 2, clusters));
+        d.pairs = max(1, min(n / 2, clusters));
+        d.sms = n;
         d.ready.store(1, std::memory_order_release);
     }
+    *sms = d.sms;
     *pairs = d.pairs;
     return cudaSuccess;
 }
@@ -364,27 +446,43 @@ cudaError_t gb_device(int* pairs) {
 }  // namespace
 
 cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, int k, cudaStream_t st, std::string* why) {
-    int pairs = 0;
-    cudaError_t e = gb_device(&pairs);
+    int sms = 0, pairs = 0;
+    cudaError_t e = gb_device(&sms, &pairs);
     if (e != cudaSuccess) return e;
     const int es = f.out_dtype == FD_F32 ? 4 : f.out_dtype == FD_BF16 ? 2 : 1;
     GbArgs g{f.a_scale, f.w_scale, f.bias, f.out, f.out_scale, f.status_out, f.a_scale_stride, f.w_scale_stride, f.out_stride,
              f.out_scale_stride, m, n, k, f.bias_dtype == FD_BF16, f.out_dtype, f.gelu != 0,
-             (reinterpret_cast<uintptr_t>(f.out) & 15) == 0 && f.out_stride * es % 16 == 0};
+             // (a bulk store clips columns to whole 16 bytes)
+             (reinterpret_cast<uintptr_t>(f.out) & 15) == 0 && f.out_stride * es % 16 == 0 && (long long)n * es % 16 == 0};
     if (f.status_out) {
         e = cudaMemsetAsync(f.status_out, 0, sizeof(int32_t), st);
         if (e != cudaSuccess) return e;
     }
-    CUtensorMap tm_a, tm_w;
+    CUtensorMap tm_a, tm_w, tm_o = {};
     const uint64_t da[2] = {(uint64_t)k, (uint64_t)m}, dw[2] = {(uint64_t)k, (uint64_t)n};
     const uint64_t sa[1] = {(uint64_t)f.a8_stride}, sw[1] = {(uint64_t)f.w8_stride};
-    const uint32_t box[2] = {GB_K, 128};
-    if (!encode_tmap_u8(&tm_a, const_cast<void*>(f.a8), 2, da, sa, box, 128, why) ||
-        !encode_tmap_u8(&tm_w, const_cast<void*>(f.w8), 2, dw, sw, box, 128, why))
+    const bool pair = getenv("GB_PAIR") ? atoi(getenv("GB_PAIR")) : m > GB_M;
+    const uint32_t box_a[2] = {GB_K, GB_M}, box_w[2] = {GB_K, (uint32_t)(pair ? 128 : 256)};
+    if (!encode_tmap(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.a8), 2, da, sa, box_a, 128, why) ||
+        !encode_tmap(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.w8), 2, dw, sw, box_w, 128, why))
         return cudaErrorInvalidValue;
-    const long long tiles = (long long)((m + 255) / 256) * ((n + 255) / 256);
-    const int grid = 2 * (int)min((long long)pairs, tiles);
-    return launch_kernel(gemm_blocks_pair_kernel<256>, grid, GB_THREADS, GbCfg<256>::SMEM, st, f.status_out == nullptr, tm_a, tm_w, g);
+    if (g.tma_out) {
+        const uint64_t d_o[2] = {(uint64_t)n, (uint64_t)m}, s_o[1] = {(uint64_t)f.out_stride * es};
+        const uint32_t box_o[2] = {(uint32_t)(128 / es), 32};
+        const CUtensorMapDataType type = f.out_dtype == FD_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 :
+                                         f.out_dtype == FD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+        if (!encode_tmap(&tm_o, type, f.out, 2, d_o, s_o, box_o, 128, why)) return cudaErrorInvalidValue;
+    }
+    const bool pdl = f.status_out == nullptr;
+    const long long n_tiles = (n + 255) / 256;
+    if (pair) {
+        cudaLaunchConfig_t lc = {};
+        cudaLaunchAttribute at[2];
+        pair_config(lc, at, 2 * (int)min((long long)pairs, (m + 255) / 256 * n_tiles), st, pdl);
+        return cudaLaunchKernelEx(&lc, gemm_blocks_kernel<true>, tm_a, tm_w, tm_o, g);
+    }
+    return launch_kernel(gemm_blocks_kernel<false>, (int)min((long long)sms, (m + GB_M - 1) / GB_M * n_tiles), GB_THREADS,
+                         GbCfg<false>::SMEM, st, pdl, tm_a, tm_w, tm_o, g);
 }
 
 }  // namespace fd
