@@ -582,8 +582,8 @@ fd_status fd_rsearch_update(fd_rsearch* st, double observed_perf, int32_t* next_
  * recorded and never polled; the context is released either way. */
 fd_status fd_destroy(fd_ctx* ctx);
 
-/* Text of the last error of this context (host string owned by the context; NULL ctx: text of
- * the last failed fd_create on this thread). */
+/* Text of the last error of this context (host string owned by the context; NULL ctx: text of the last failed
+ * fd_create, or call of an operator that takes no context, on this thread). */
 const char* fd_last_error(const fd_ctx* ctx);
 
 #ifdef __cplusplus

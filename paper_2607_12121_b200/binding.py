@@ -10,6 +10,8 @@ import ctypes
 import os
 from typing import Dict, Optional
 
+import torch
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libflashdiff.so")
 
@@ -400,156 +402,152 @@ def fd_set_fp8_operands(ctx: Context, fp8: Optional[Dict[str, "object"]], text_s
 
 
 # ---- row operators next to the step (no context; work on the tensors' device) ------------------------------------
+# A call's host time is what the smallest of these operators cost, so the checks below look at every tensor once.
+
+_TYPE_CODES = {torch.bfloat16: FD_BF16, torch.float32: FD_F32}
+_CODES_TYPES = (torch.uint8, torch.float8_e4m3fn)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 
 def _op_fail(text: str):
     raise FlashDiffError(FD_ERR_INVALID_ARG, text)
 
 
-def _codes_type(t) -> bool:
-    return t.element_size() == 1 and str(t.dtype) in ("torch.uint8", "torch.float8_e4m3fn")
-
-
 def _type_code(t, name: str) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return FD_BF16
-    if t.dtype == torch.float32:
-        return FD_F32
-    _op_fail("%s must be float32 or bfloat16, not %s" % (name, t.dtype))
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
+        _op_fail("%s must be float32 or bfloat16, not %s" % (name, t.dtype))
+    return code
 
 
-def _rows(t, name: str, rows: int, cols: int, device, code=None, f32=False) -> int:
-    """Row stride of the 2-D device tensor ``t`` of the wanted shape, columns contiguous."""
-    import torch
-    if t.device != device or tuple(t.shape) != (rows, cols):
-        _op_fail("%s must be [%d, %d] on %s, not %s on %s" % (name, rows, cols, device, list(t.shape), t.device))
-    if cols > 1 and t.stride(1) != 1:
+def _rows(t, name: str, rows: int, cols: int, device: int) -> int:
+    """Row stride of the 2-D tensor ``t`` of the wanted shape on the device, columns contiguous."""
+    stride = t.stride()
+    if len(stride) != 2 or t.get_device() != device:
+        _op_fail("%s must be [%d, %d] on device %d, not %s on %s" % (name, rows, cols, device, list(t.shape), t.device))
+    r, c = t.shape
+    if r != rows or c != cols:
+        _op_fail("%s must be [%d, %d], not %s" % (name, rows, cols, list(t.shape)))
+    if stride[1] != 1 and cols > 1:
         _op_fail("%s must have contiguous columns" % name)
-    if code and not _codes_type(t):
+    return stride[0] if rows > 1 else max(stride[0], cols)
+
+
+def _codes(t, name: str, rows: int, cols: int, device: int) -> int:
+    if t.dtype not in _CODES_TYPES:
         _op_fail("%s must hold E4M3 codes (uint8 or float8_e4m3fn), not %s" % (name, t.dtype))
-    if f32 and t.dtype != torch.float32:
+    return _rows(t, name, rows, cols, device)
+
+
+def _scales(t, name: str, rows: int, cols: int, device: int) -> int:
+    if t.dtype is not torch.float32:
         _op_fail("%s must be float32, not %s" % (name, t.dtype))
-    return max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+    return _rows(t, name, rows, cols, device)
 
 
-class _on_device:
-    """The tensors' device made current for a call (nothing to do where it already is)."""
-
-    def __init__(self, t):
-        import torch
-        if not t.is_cuda:
-            _op_fail("device tensors wanted, got one on %s" % t.device)
-        self.guard = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
+def _op_call(device: int, stream, fn, *args) -> None:
+    """The call with the tensors' device current, on the given stream or that device's current one."""
+    if device < 0:
+        _op_fail("device tensors wanted")
+    if torch.cuda.current_device() == device:
+        status = fn(*args, (_raw_stream(device) if stream is None else stream.cuda_stream) or None)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, (_raw_stream(device) if stream is None else stream.cuda_stream) or None)
+    if status != FD_OK:
+        _check(None, status)
 
 
 def make_rope_axes(axis_dims, theta=10000.0, pairing: str = "interleaved") -> FdRopeSpec:
     """fd_rope_spec: channels per axis, base per axis (or one for all), "interleaved" or "halves"."""
-    axis_dims = [int(d) for d in axis_dims]
-    thetas = [float(theta)] * len(axis_dims) if isinstance(theta, (int, float)) else [float(v) for v in theta]
-    if not 1 <= len(axis_dims) <= 4 or len(thetas) != len(axis_dims):
+    n = len(axis_dims)
+    thetas = (theta,) * n if isinstance(theta, (int, float)) else tuple(theta)
+    if not 1 <= n <= 4 or len(thetas) != n:
         _op_fail("one to four axes, with one base each")
     if pairing not in ("interleaved", "halves"):
         _op_fail("unknown pairing %r" % (pairing,))
-    return FdRopeSpec((ctypes.c_double * 4)(*thetas), (ctypes.c_int32 * 4)(*axis_dims), len(axis_dims),
-                      FD_ROPE_INTERLEAVED if pairing == "interleaved" else FD_ROPE_HALVES)
+    return FdRopeSpec(thetas, tuple(axis_dims), n, FD_ROPE_INTERLEAVED if pairing == "interleaved" else FD_ROPE_HALVES)
 
 
 def _rope_pos(spec: FdRopeSpec, pos) -> int:
-    import torch
-    if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape[1] != spec.n_axes or not pos.is_contiguous():
+    if pos.dtype is not torch.float32 or pos.dim() != 2 or pos.shape[1] != spec.n_axes or not pos.is_contiguous():
         _op_fail("pos must be a contiguous float32 tensor [tokens, %d]" % spec.n_axes)
-    return int(pos.shape[0])
+    return pos.shape[0]
+
+
+def _rope_set(a, b, tokens: int, dh: int, dtype, device: int):
+    if a.dim() != 3 or a.shape != b.shape or a.shape[0] != tokens or a.shape[2] != dh:
+        _op_fail("rows must be [tokens, heads, head_dim], inputs and outputs alike")
+    if a.dtype is not dtype or b.dtype is not dtype or a.get_device() != device or b.get_device() != device:
+        _op_fail("rows must share one type and the device of pos")
+    sa, sb = a.stride(), b.stride()
+    if sa[2] != 1 or sb[2] != 1:
+        _op_fail("channels must be contiguous")
+    return a.data_ptr(), b.data_ptr(), sa[0], sa[1], sb[0], sb[1], a.shape[1]
 
 
 def fd_rope_axes(spec: FdRopeSpec, pos, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
     """Rotates q (and k) [tokens, heads, head_dim] by the tokens' positions pos [tokens, n_axes] into q_out (k_out);
     any token and head strides, the same tensor twice rotates in place.  ``inverse``: the inverse map, also the gradient."""
-    tokens = _rope_pos(spec, pos)
-    sets = [(q, q_out)] + ([(k, k_out)] if k is not None else [])
+    tokens, device = _rope_pos(spec, pos), pos.get_device()
     if (k is None) != (k_out is None):
         _op_fail("k and k_out come together")
-    code, dh = _type_code(q, "q"), int(q.shape[-1])
-    rows = (FdRopeRows * len(sets))()
-    for i, (a, b) in enumerate(sets):
-        if a.dim() != 3 or a.shape[0] != tokens or a.shape[2] != dh or a.shape != b.shape:
-            _op_fail("rows must be [tokens, heads, head_dim], inputs and outputs alike")
-        if a.dtype != q.dtype or b.dtype != q.dtype or a.device != pos.device or b.device != pos.device:
-            _op_fail("rows must share one type and the device of pos")
-        if a.stride(2) != 1 or b.stride(2) != 1:
-            _op_fail("channels must be contiguous")
-        rows[i] = FdRopeRows(a.data_ptr(), b.data_ptr(), a.stride(0), a.stride(1), b.stride(0), b.stride(1), a.shape[1])
-    if tokens == 0:
-        return
-    with _on_device(pos):
-        _check(None, lib.fd_rope_axes(ctypes.byref(spec), pos.data_ptr(), tokens, dh, code, rows, len(sets), 1 if inverse else 0,
-                                      _stream(stream)))
+    code, dh = _type_code(q, "q"), q.shape[-1]
+    first = _rope_set(q, q_out, tokens, dh, q.dtype, device)
+    rows = (FdRopeRows * 2)(first) if k is None else (FdRopeRows * 2)(first, _rope_set(k, k_out, tokens, dh, q.dtype, device))
+    if tokens:
+        _op_call(device, stream, lib.fd_rope_axes, spec, pos.data_ptr(), tokens, dh, code, rows, 1 if k is None else 2, 1 if inverse else 0)
 
 
 def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) -> None:
     """The rotary tables [tokens, head_dim / 2] float32 that fd_set_block_variants takes, from positions [tokens, n_axes]."""
-    tokens = _rope_pos(spec, pos)
-    half = int(cos_out.shape[-1])
+    tokens, device, half = _rope_pos(spec, pos), pos.get_device(), cos_out.shape[-1]
     for t, name in ((cos_out, "cos_out"), (sin_out, "sin_out")):
-        _rows(t, name, tokens, half, pos.device, f32=True)
-        if not t.is_contiguous():
+        if _scales(t, name, tokens, half, device) != half:
             _op_fail("%s must be contiguous" % name)
-    if tokens == 0:
-        return
-    with _on_device(pos):
-        _check(None, lib.fd_rope_axes_tables(ctypes.byref(spec), pos.data_ptr(), tokens, 2 * half, cos_out.data_ptr(), sin_out.data_ptr(),
-                                             _stream(stream)))
+    if tokens:
+        _op_call(device, stream, lib.fd_rope_axes_tables, spec, pos.data_ptr(), tokens, 2 * half, cos_out.data_ptr(), sin_out.data_ptr())
 
 
 def fd_add_rmsnorm(x, weight, eps: float, residual=None, residual_out=None, y=None, y8=None, y8_scale=None, stream=None) -> None:
     """r = x + residual (kept in residual_out if given), y = r / sqrt(mean(r^2) + eps) * weight; outputs y in x's type and / or
     y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)].  residual_out may be residual, y may be x."""
-    rows, cols = x.shape
-    dev = x.device
-    a = FdRmsnormArgs(eps=float(eps), x_dtype=_type_code(x, "x"))
-    a.x, a.x_stride = x.data_ptr(), _rows(x, "x", rows, cols, dev)
+    (rows, cols), device = x.shape, x.get_device()
+    x_stride = _rows(x, "x", rows, cols, device)
+    w = r = ro = py = p8 = ps = None
+    r_stride = ro_stride = y_stride = y8_stride = s_stride = r_type = 0
     if weight is not None:
-        if weight.dtype != x.dtype or weight.device != dev or tuple(weight.shape) != (cols,) or not weight.is_contiguous():
+        if weight.dtype is not x.dtype or weight.get_device() != device or weight.shape != (cols,) or (cols > 1 and weight.stride(0) != 1):
             _op_fail("weight must be a contiguous [%d] tensor of x's type and device" % cols)
-        a.weight = weight.data_ptr()
-    if residual is not None and residual_out is not None and residual.dtype != residual_out.dtype:
-        _op_fail("residual and residual_out must share one type")
-    for t, name in ((residual, "residual"), (residual_out, "residual_out")):
-        if t is not None:
-            a.residual_dtype = _type_code(t, name)
-            setattr(a, name, t.data_ptr())
-            setattr(a, name + "_stride", _rows(t, name, rows, cols, dev))
+        w = weight.data_ptr()
+    if residual is not None:
+        r_type, r, r_stride = _type_code(residual, "residual"), residual.data_ptr(), _rows(residual, "residual", rows, cols, device)
+    if residual_out is not None:
+        if residual is not None and residual.dtype is not residual_out.dtype:
+            _op_fail("residual and residual_out must share one type")
+        r_type, ro = _type_code(residual_out, "residual_out"), residual_out.data_ptr()
+        ro_stride = r_stride if residual_out is residual else _rows(residual_out, "residual_out", rows, cols, device)
     if y is not None:
-        if y.dtype != x.dtype:
+        if y.dtype is not x.dtype:
             _op_fail("y must have x's type")
-        a.y, a.y_stride = y.data_ptr(), _rows(y, "y", rows, cols, dev)
+        py, y_stride = y.data_ptr(), _rows(y, "y", rows, cols, device)
     if y8 is not None:
-        a.y8, a.y8_stride = y8.data_ptr(), _rows(y8, "y8", rows, cols, dev, code=True)
+        p8, y8_stride = y8.data_ptr(), _codes(y8, "y8", rows, cols, device)
     if y8_scale is not None:
-        a.y8_scale, a.y8_scale_stride = y8_scale.data_ptr(), _rows(y8_scale, "y8_scale", rows, (cols + 127) // 128, dev, f32=True)
-    if rows == 0:
-        return
-    with _on_device(x):
-        _check(None, lib.fd_add_rmsnorm(ctypes.byref(a), rows, cols, _stream(stream)))
+        ps, s_stride = y8_scale.data_ptr(), _scales(y8_scale, "y8_scale", rows, (cols + 127) // 128, device)
+    if rows:
+        _op_call(device, stream, lib.fd_add_rmsnorm,
+                 FdRmsnormArgs(x.data_ptr(), r, ro, w, py, p8, ps, x_stride, r_stride, ro_stride, y_stride, y8_stride, s_stride,
+                               _type_code(x, "x"), r_type, eps), rows, cols)
 
 
 def fd_quantize_fp8_blocks(x, y8, y8_scale, stream=None) -> None:
     """E4M3 codes y8 and scales y8_scale [rows, ceil(cols / 128)] of x [rows, cols] (float32 or bfloat16)."""
-    rows, cols = x.shape
-    dev = x.device
-    args = (_rows(x, "x", rows, cols, dev), _type_code(x, "x"), rows, cols, y8.data_ptr(), _rows(y8, "y8", rows, cols, dev, code=True),
-            y8_scale.data_ptr(), _rows(y8_scale, "y8_scale", rows, (cols + 127) // 128, dev, f32=True))
-    if rows == 0:
-        return
-    with _on_device(x):
-        _check(None, lib.fd_quantize_fp8_blocks(x.data_ptr(), *args, _stream(stream)))
+    (rows, cols), device = x.shape, x.get_device()
+    args = (x.data_ptr(), _rows(x, "x", rows, cols, device), _type_code(x, "x"), rows, cols, y8.data_ptr(),
+            _codes(y8, "y8", rows, cols, device), y8_scale.data_ptr(), _scales(y8_scale, "y8_scale", rows, (cols + 127) // 128, device))
+    if rows:
+        _op_call(device, stream, lib.fd_quantize_fp8_blocks, *args)
 
 
 def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = False, out_scale=None, status_out=None,
@@ -557,39 +555,36 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
     """out [m, n] = sum over the 128-blocks of k of a_scale * w_scale * (a8 w8^T) + bias, then tanh-GELU if asked.  a8 [m, k],
     w8 [n, k]: E4M3 codes; a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] float32; out float32, bfloat16,
     or codes with out_scale [m, ceil(n / 128)]; status_out: optional int32 device scalar."""
-    import torch
-    (m, k), n, dev = a8.shape, w8.shape[0], a8.device
+    (m, k), n, device = a8.shape, w8.shape[0], a8.get_device()
     kb, nb = (k + 127) // 128, (n + 127) // 128
-    f = FdMatmulFp8Args(gelu=1 if gelu else 0)
-    f.a8, f.a8_stride = a8.data_ptr(), _rows(a8, "a8", m, k, dev, code=True)
-    f.w8, f.w8_stride = w8.data_ptr(), _rows(w8, "w8", n, k, dev, code=True)
+    a_stride, w_stride = _codes(a8, "a8", m, k, device), _codes(w8, "w8", n, k, device)
     if m <= 1:                                          # the stride of a single row is free: round it up to what is asked for
-        f.a8_stride = (f.a8_stride + 15) // 16 * 16
+        a_stride = (a_stride + 15) // 16 * 16
     if n <= 1:
-        f.w8_stride = (f.w8_stride + 15) // 16 * 16
-    f.a_scale, f.a_scale_stride = a_scale.data_ptr(), _rows(a_scale, "a_scale", m, kb, dev, f32=True)
-    f.w_scale, f.w_scale_stride = w_scale.data_ptr(), _rows(w_scale, "w_scale", nb, kb, dev, f32=True)
+        w_stride = (w_stride + 15) // 16 * 16
+    p_bias = p_scale = p_status = None
+    bias_type = s_stride = 0
     if bias is not None:
-        if bias.device != dev or tuple(bias.shape) != (n,) or (n > 1 and bias.stride(0) != 1):
-            _op_fail("bias must be a contiguous [%d] tensor on %s" % (n, dev))
-        f.bias, f.bias_dtype = bias.data_ptr(), _type_code(bias, "bias")
-    if _codes_type(out):
-        f.out_dtype = FD_E4M3
+        if bias.get_device() != device or bias.shape != (n,) or (n > 1 and bias.stride(0) != 1):
+            _op_fail("bias must be a contiguous [%d] tensor on the operands' device" % n)
+        p_bias, bias_type = bias.data_ptr(), _type_code(bias, "bias")
+    if out.dtype in _CODES_TYPES:
+        out_type = FD_E4M3
         if out_scale is None:
             _op_fail("codes in out need out_scale")
     else:
-        f.out_dtype = _type_code(out, "out")
-    f.out, f.out_stride = out.data_ptr(), _rows(out, "out", m, n, dev)
+        out_type = _type_code(out, "out")
     if out_scale is not None:
-        f.out_scale, f.out_scale_stride = out_scale.data_ptr(), _rows(out_scale, "out_scale", m, nb, dev, f32=True)
+        p_scale, s_stride = out_scale.data_ptr(), _scales(out_scale, "out_scale", m, nb, device)
     if status_out is not None:
-        if status_out.dtype != torch.int32 or status_out.device != dev or status_out.numel() < 1:
-            _op_fail("status_out must be an int32 tensor on %s" % dev)
-        f.status_out = status_out.data_ptr()
-    if m == 0:
-        return
-    with _on_device(a8):
-        _check(None, lib.fd_matmul_fp8_blocks(ctypes.byref(f), m, n, k, _stream(stream)))
+        if status_out.dtype is not torch.int32 or status_out.get_device() != device or status_out.numel() < 1:
+            _op_fail("status_out must be an int32 tensor on the operands' device")
+        p_status = status_out.data_ptr()
+    args = FdMatmulFp8Args(a8.data_ptr(), a_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), p_bias, out.data_ptr(), p_scale, p_status,
+                           a_stride, _scales(a_scale, "a_scale", m, kb, device), w_stride, _scales(w_scale, "w_scale", nb, kb, device),
+                           _rows(out, "out", m, n, device), s_stride, bias_type, out_type, 1 if gelu else 0)
+    if m:
+        _op_call(device, stream, lib.fd_matmul_fp8_blocks, args, m, n, k)
 
 
 def fd_sched_pack(load, cost, home):

@@ -958,8 +958,8 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k,
     if (!aligned16(f->a8) || !aligned16(f->w8)) return op_fail(FD_ERR_INVALID_ARG, "%s: a8 and w8 must be 16-byte aligned", who);
     const int64_t kb = (k + FP8_BLOCK - 1) / FP8_BLOCK, nb = (n + FP8_BLOCK - 1) / FP8_BLOCK;
     // the tensor maps take the strides of single rows too
-    if (f->a8_stride % 16 || f->w8_stride % 16 || f->a8_stride < k || f->w8_stride < k)
-        return op_fail(FD_ERR_SHAPE, "%s: the strides of a8 and w8 must be multiples of 16 and at least k", who);
+    if (f->a8_stride % 16 || f->w8_stride % 16 || f->a8_stride < k || f->w8_stride < k || f->a8_stride >= MAX_STRIDE || f->w8_stride >= MAX_STRIDE)
+        return op_fail(FD_ERR_SHAPE, "%s: the strides of a8 and w8 must be multiples of 16, at least k and below 2^40", who);
     const size_t es = f->out_dtype == FD_E4M3 ? 1 : type_bytes(f->out_dtype);
     fd_status s = FD_OK;
     if ((s = op_rows(who, "a8", f->a8, f->a8_stride, 16, m, k)) != FD_OK) return s;

@@ -164,15 +164,12 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, int
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y)
         : "memory");
 }
-// Asynchronous 4-byte copy global -> shared of one thread; copy_async_arrive makes the barrier count this thread once all
-// its copies so far have landed (the barrier's count includes one arrival per thread).
-__device__ __forceinline__ void copy_async4(void* sdst, const void* gsrc) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(sdst)), "l"(reinterpret_cast<uint64_t>(gsrc)) : "memory");
+// Asynchronous 4-byte copies global -> shared of one thread, waited for by groups.
+__device__ __forceinline__ void copy_async4(uint32_t sdst, const void* gsrc) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(sdst), "l"(reinterpret_cast<uint64_t>(gsrc)) : "memory");
 }
-__device__ __forceinline__ void copy_async_arrive(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void copy_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 // Untiled bulk copy global -> shared (this CTA's memory): both addresses 16-byte aligned, size a multiple of
 // 16 bytes; completion is counted in bytes on the mbarrier.
 __device__ __forceinline__ void bulk_load(void* sdst, const void* gsrc, uint32_t bytes, uint64_t* bar) {
@@ -308,6 +305,8 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // shared::cluster address of the same shared-memory location in CTA `rank` of the cluster
 __device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t rank) {
     uint32_t r;
@@ -321,6 +320,10 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
 // back a TMEM buffer, whose reads tcgen05.wait::ld has already completed and tcgen05.fence orders.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// 16 bytes into the shared memory of a CTA of the cluster (or this CTA's own, by its plain shared address)
+__device__ __forceinline__ void store_cluster4(uint32_t cluster_addr, float a, float b, float c, float d) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
 }
 // tile load into this CTA's shared memory whose completion is counted on a barrier that may live in
 // the peer CTA of the pair (no multicast: every CTA fetches its own tile)

@@ -258,9 +258,11 @@ cudaError_t launch_typed(const RowArgs& a, cudaStream_t st) {
         const int grid = (int)min(a.rows, 1LL << 20);
         return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM>, grid, ROW_ANY_THREADS, 0, st, true, a);
     }
-    // as few warps per row as hold it in their registers; more when the rows alone would leave SMs idle
+    // Warps per row: three vectors a lane where eight warps allow it (16380 x 1536, bf16 + fp32 residual to 8 bits: 47.1 us with two
+    // warps and three vectors, 56.7 with one and six, 48.0 with four and two, 62.9 with eight and one: more rows in flight
+    // against more lanes idle in the reductions); more warps when the rows alone would leave SMs idle.
     int w = 1;
-    while (w < ROW_MAX_W && (a.cols > 256 * w * ROW_MAX_NV || (a.cols > 256 * w && a.rows * w < 148 * 4))) w *= 2;
+    while (w < ROW_MAX_W && (a.cols > 256 * w * 3 || (a.cols > 256 * w && a.rows * w < 148 * 4))) w *= 2;
     switch (w) {
         case 1: return launch_nv<TX, TR, 1, NORM>(a, st);
         case 2: return launch_nv<TX, TR, 2, NORM>(a, st);

@@ -1,17 +1,24 @@
 // Product of E4M3 operands with a scale for every 128 values of K (activations: per row; weights: per 128 rows):
 //   v[i, j] = sum_b a_scale[i, b] * w_scale[j / 128, b] * (sum over block b of a8[i, k] * w8[j, k])
 // The tensor core cannot apply an fp32 scale, so every block of K is a product of its own (kind::f8f6f4, 128 deep) into
-// a TMEM buffer, and eight epilogue warps add it, scaled, to fp32 accumulators in their registers while the tensor core
-// works on the next block in the other buffer.
+// one of two TMEM buffers, and eight epilogue warps add it, scaled, to fp32 accumulators in their registers while the
+// tensor core works on the next block in the other buffer.  Warp (quadrant q, half h) holds rows 32 q .. 32 q + 31 (one per
+// lane) and the 128 columns of half h, which is one scale block of the weights and, for the 8-bit output, one block of the
+// output row: its amax needs no other thread.
 //
-// A CTA computes a 128 x 256 tile (128 x 128 for narrow problems): warp (quadrant q, half h) of the epilogue holds rows
-// 32 q .. 32 q + 31 (one per lane) and the 128 columns of half h, which is one scale block of the weights and, for the
-// 8-bit output, one block of the output row: its amax needs no other thread.
-// CTA pairs (cta_group::2, 256 x 256 tiles), which the per-tensor FP8 kernel uses, lose here: the buffer hand-over happens
-// for every block of K instead of once a tile, and with two CTAs it crosses the cluster both ways.  Measured on
-// 8192 x 8192 x 8192: 1.65 us... 
+// Three forms (launch_matmul_fp8_blocks chooses): a CTA per 128 x 256 tile; a CTA pair per 256 x 256 tile (cta_group::2:
+// each CTA stages its own activation rows and half of the weight rows, a third less to fetch and to read from shared memory
+// per product); and, for few tiles, 128 x 128 tiles with K shared out to a cluster (gemm_blocks_split_kernel).  No load is
+// multicast.
+//
+// What paces it, measured in clocks per block of K (its products take 512): a pair 715, a single CTA 770-850 (its operands'
+// way into shared memory, 48 KB, and out of it, 48 KB, shares one port).  The rest is the hand-over of the buffers, product ->
+// 32 rows x 128 columns read and added -> product, so everything on that way is kept short: arrivals on the other CTA's
+// barrier without cluster-scope release (with it: 1650 clk a block), two issuing warps, converged warps with an elected lane
+// for products and copies, scales fetched ahead into a shared-memory ring, and barrier addresses stepped by exclusive or.
+// Large sizes then run at the card's power limit: 8192 x 8192 x 8192 at 486 us (2263 TFLOP/s) on a cool card, 560 us after
+// others.
 #include <atomic>
-#include <cstdlib>
 #include <string>
 
 #include "attn_common.cuh"
@@ -53,8 +60,9 @@ struct GbArgs {
     int32_t* status;                           // first device-side error, or nullptr
     long long as_ld, ws_ld, out_ld, os_ld;     // elements
     int m, n, k;
-    int bias_bf16, out_dtype, gelu;
-    int tma_out;                               // `out` is stored through its tensor map (16-byte rows)
+    int bias_bf16;
+    int tma_out;                               // `out` is stored through its tensor map (whole 16-byte units)
+    int vec_out;                               // `out` takes stores of four columns
 };
 
 __device__ __forceinline__ void gb_report(int32_t* status, int code) {
@@ -70,17 +78,22 @@ __device__ __forceinline__ void pass_regs(uint32_t* r) {
                    "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float rcp_approx(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
 // tanh-GELU as a sigmoid: 0.5 v (1 + tanh u) = v / (1 + exp(-2u)), accurate to a few fp32 roundings (the hardware tanh is
-// good to 2^-11 only, which the scale of an 8-bit output block would show).  Two values share one reciprocal: the special
-// functions, 4 lanes a clock and scheduler, are what a GELU tile's epilogue takes longest for.  The exponent is cut at 2^57
-// so that the product of the two denominators stays finite; the value is below 2^-53 of its argument there.
+// good to 2^-11 only, which the scale of an 8-bit output block would show).  Two values share one reciprocal; the exponent is
+// cut at 2^57 so that the product of the two denominators stays finite (the value is below 2^-53 of its argument there).  It
+// costs a tile about 3000 clk of instruction latency, not of the special-function unit: exponentials on the FMA pipe for
+// three of eight pairs made 16380 x 8960 x 1536 slower (300 us against 265), a reciprocal for every value made no difference.
 __device__ __forceinline__ void gelu_pair(float& v0, float& v1) {
     constexpr float C1 = -2.3022081985814995f, C2 = -0.10294323959957175f;      // -2 log2(e) sqrt(2 / pi) (1, 0.044715)
-    const float d0 = 1.0f + attn::ex2(fminf(v0 * fmaf(C2 * v0, v0, C1), 57.0f));
-    const float d1 = 1.0f + attn::ex2(fminf(v1 * fmaf(C2 * v1, v1, C1), 57.0f));
-    const float r = __fdividef(1.0f, d0 * d1);
-    v0 *= r * d1;
-    v1 *= r * d0;
+    const uint64_t v = attn::pair(v0, v1);
+    float x0, x1, d0, d1;
+    attn::unpair(mul2(v, attn::fma2(mul2(v, attn::pair(C2, C2)), v, attn::pair(C1, C1))), x0, x1);
+    attn::unpair(attn::add2(attn::pair(attn::ex2(fminf(x0, 57.0f)), attn::ex2(fminf(x1, 57.0f))), attn::pair(1.0f, 1.0f)), d0, d1);
+    const float r = rcp_approx(d0 * d1);
+    attn::unpair(mul2(v, mul2(attn::pair(r, r), attn::pair(d1, d0))), v0, v1);
 }
 
 // One warp's 32 rows x 128 columns of finished accumulators: bias, GELU, rounding, and the way out through the warp's two
@@ -88,6 +101,7 @@ __device__ __forceinline__ void gelu_pair(float& v0, float& v1) {
 // wants them, which also keeps the writes free of bank conflicts; one bulk tensor store takes a tile away while the warp
 // goes on (it drops rows behind m and columns behind n).  Outputs a tensor map cannot describe (rows that are not whole
 // 16-byte units) leave element by element.
+// (bulk groups belong to the thread that issues them: always lane 0, elected in a converged warp)
 template <int PENDING> __device__ __forceinline__ void gb_stage_wait(int lane) {   // all but the last PENDING stores have read their tile
     if (lane == 0) bulk_wait_read<PENDING>();
     __syncwarp();
@@ -112,25 +126,28 @@ __device__ __forceinline__ void gb_stage_out(const GbArgs& g, const CUtensorMap*
     __syncwarp();
 }
 
-__device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_o, float* v, const float* b, uint8_t* stage, int lane, int row_base, int col0) {
+// `b`: bias of columns lane, lane + 32, ... as it was loaded (fp32, or bf16 in the low half)
+template <int OUT, bool GELU>
+__device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_o, float* v, const uint32_t* b, uint8_t* stage, int lane, int row_base, int col0) {
     gb_stage_wait<0>(lane);
     if (g.bias) {
-        float* bias = reinterpret_cast<float*>(stage);       // the first staging tile spreads the columns' bias over the lanes
+        uint32_t* bias = reinterpret_cast<uint32_t*>(stage); // the first staging tile spreads the columns' bias over the lanes
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bias[i * 32 + lane] = b[i];
+        for (int i = 0; i < 4; ++i) bias[i * 32 + lane] = g.bias_bf16 ? b[i] << 16 : b[i];
         __syncwarp();
 #pragma unroll
         for (int c = 0; c < 128; c += 4) {
             const float4 w = *reinterpret_cast<const float4*>(bias + c);
-            v[c] += w.x; v[c + 1] += w.y; v[c + 2] += w.z; v[c + 3] += w.w;
+            attn::unpair(attn::add2(attn::pair(v[c], v[c + 1]), attn::pair(w.x, w.y)), v[c], v[c + 1]);
+            attn::unpair(attn::add2(attn::pair(v[c + 2], v[c + 3]), attn::pair(w.z, w.w)), v[c + 2], v[c + 3]);
         }
         __syncwarp();
     }
-    if (g.gelu) {
+    if constexpr (GELU) {
 #pragma unroll
         for (int c = 0; c < 128; c += 2) gelu_pair(v[c], v[c + 1]);
     }
-    if (g.out_dtype == FD_E4M3) {
+    if constexpr (OUT == FD_E4M3) {
         float amax = FP8_AMAX_FLOOR;
 #pragma unroll
         for (int c = 0; c < 128; ++c) amax = fmaxf(amax, fabsf(v[c]));      // columns behind n hold zeros
@@ -147,7 +164,7 @@ __device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_
             *unit_ptr(stage, lane, u) = make_uint4(q[0], q[1], q[2], q[3]);
         }
         gb_stage_out<uint8_t>(g, tm_o, stage, lane, row_base, col0);
-    } else if (g.out_dtype == FD_BF16) {
+    } else if constexpr (OUT == FD_BF16) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             uint8_t* tile = stage + h * EPI_STAGE_BYTES_PER_WARP;
@@ -173,7 +190,7 @@ __device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_
     }
 }
 
-template <bool PAIR>
+template <bool PAIR, int OUT, bool GELU>
 __global__ void __launch_bounds__(GB_THREADS, 1)
 gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_o, GbArgs g) {
     using Cfg = GbCfg<PAIR>;
@@ -196,7 +213,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1 + 32); mbar_init(&tempty[a], CTAS * GB_EPI_WARPS); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 2); mbar_init(&tempty[a], CTAS * GB_EPI_WARPS); }
         *abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_a);
@@ -285,9 +302,10 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
         } else if (warp == 2) {
             // Scales of this CTA's rows and of the tile's two weight blocks, GB_AHEAD blocks ahead of their use; rows behind m and
-            // column blocks behind n take the last valid ones (their results are not stored).  A block's 32 arrivals on tfull
-            // follow the completion of the buffer's previous block, so they count in the right phase; by then blocks up to four
-            // before the present one have been read by every warp, so entry (block + GB_AHEAD) of the ring is free.
+            // column blocks behind n take the last valid ones (their results are not stored).  The arrival on tfull for a block
+            // follows the completion of its buffer's previous block, so it counts in the right phase; by then blocks up to four
+            // before the present one have been read by every warp, so entry (block + GB_AHEAD) of the ring is free.  Copies are
+            // waited for group by group: an arrival that had to wait for the newest copies would put their latency into every block.
             const int w_blocks = (g.n + FP8_BLOCK - 1) / FP8_BLOCK;
             const uint32_t blocks = (uint32_t)((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;
             long long tile = unit;
@@ -301,25 +319,31 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
                     as[i] = g.a_scale + (long long)min((m * CTAS + (int)rank) * GB_M + 32 * i + lane, g.m - 1) * g.as_ld;
                 ws = g.w_scale + (long long)min(n * 2 + (lane & 1), w_blocks - 1) * g.ws_ld;
             };
-            auto fetch = [&]() {
-                if (fetched == blocks) return;
-                if (k == k_blocks) { k = 0; tile += n_units; rows_of(); }
-                float* entry = s_scale + (fetched % GB_RING) * GB_ENTRY;
+            uint32_t dst = smem_u32(s_scale + lane);
+            const uint32_t dst_end = dst + GB_RING * GB_ENTRY * 4;
+            auto fetch = [&]() {                             // one group of copies, empty behind the last block
+                if (fetched < blocks) {
+                    if (k == k_blocks) { k = 0; tile += n_units; rows_of(); }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) copy_async4(entry + 32 * i + lane, as[i] + k);
-                if (lane < 2) copy_async4(entry + GB_M + lane, ws + k);
-                ++k;
-                ++fetched;
+                    for (int i = 0; i < 4; ++i) copy_async4(dst + 128 * i, as[i] + k);
+                    if (lane < 2) copy_async4(dst + GB_M * 4, ws + k);
+                    dst = dst + GB_ENTRY * 4 == dst_end ? dst_end - GB_RING * GB_ENTRY * 4 : dst + GB_ENTRY * 4;
+                    ++k;
+                    ++fetched;
+                }
+                copy_async_commit();
             };
             rows_of();
             for (int i = 0; i < GB_AHEAD; ++i) fetch();
             bool ok = true;
             for (uint32_t it = 0; it < blocks && ok; ++it) {
                 if (it >= 2) ok = mbar_wait(&tfull[it & 1], ((it >> 1) & 1) ^ 1, abort_flag);
-                copy_async_arrive(&tfull[it & 1]);
+                copy_async_wait<GB_AHEAD - 1>();             // this block's scales have landed
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&tfull[it & 1]);
                 fetch();
             }
-            copy_async_wait_all();
+            copy_async_wait<0>();
             if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
         }
     } else {
@@ -337,13 +361,17 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
         for (long long tile = unit; tile < total && ok; tile += n_units) {
             const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
             const int row_base = (m * CTAS + (int)rank) * GB_M + quad * 32, col0 = n * GB_N + half * 128;
-            float b[4];                                      // bias of columns lane, lane + 32, ...
+            uint32_t b[4] = {0u, 0u, 0u, 0u};                // bias of columns lane, lane + 32, ...: raw bits, first looked at when the tile is done
+            if (g.bias) {
+                if (g.bias_bf16) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = col0 + i * 32 + lane;
-                b[i] = 0.f;
-                if (g.bias && c < g.n)
-                    b[i] = g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[c]) : __ldg(static_cast<const float*>(g.bias) + c);
+                    for (int i = 0; i < 4; ++i)
+                        if (col0 + i * 32 + lane < g.n) b[i] = __ldg(static_cast<const unsigned short*>(g.bias) + col0 + i * 32 + lane);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (col0 + i * 32 + lane < g.n) b[i] = __ldg(static_cast<const uint32_t*>(g.bias) + col0 + i * 32 + lane);
+                }
             }
             float acc[128];
 #pragma unroll
@@ -376,7 +404,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
                 t_row ^= GB_N;
                 entry = entry + GB_ENTRY * 4 == GB_RING * GB_ENTRY * 4 ? 0 : entry + GB_ENTRY * 4;
             }
-            if (ok && row_base < g.m && col0 < g.n) gb_store(g, &tm_o, acc, b, stage, lane, row_base, col0);
+            if (ok && row_base < g.m && col0 < g.n) gb_store<OUT, GELU>(g, &tm_o, acc, b, stage, lane, row_base, col0);
         }
         if (lane == 0) bulk_wait_all();                          // this warp's stores have landed
         if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
@@ -392,29 +420,260 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     }
 }
 
-// Per-device set-up, done once: shared-memory attributes and the number of SMs.
+// ------------------------------------------------------------------------------------------------
+// Few tiles (few rows, or a narrow output): 128 x 128 tiles whose blocks of K are shared out to the S CTAs of a cluster.
+// Every CTA leaves its partial sums, 128 / S rows for each CTA of the cluster, in that CTA's shared memory; after one cluster
+// barrier each adds the S partial sums of its rows in the order of the ranks (the result does not depend on timing) and
+// finishes them with the lanes along the columns, so that nothing needs to be transposed.
+// ------------------------------------------------------------------------------------------------
+constexpr int GS_N = 128, GS_STAGES = 4, GS_BUFS = 4;          // columns of a tile, stages, TMEM buffers
+constexpr int GS_STAGE_BYTES = GB_A_BYTES + GS_N * GB_K;
+constexpr int GS_SMEM = 1024 + GS_STAGES * GS_STAGE_BYTES + GB_M * GS_N * 4 /* partial sums */ + GB_RING * GB_ENTRY * 4 + 256;
+
+// 16-byte unit u (of 32) of row r in the partial sums of one rank: permuted against bank conflicts of the row-wise writers
+__device__ __forceinline__ uint32_t gs_unit(int r, int u) { return (uint32_t)(r * 32 + (u ^ (r & 7))) * 16; }
+
+template <int OUT, bool GELU>
+__global__ void __launch_bounds__(GB_THREADS, 1)
+gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, GbArgs g, int splits) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sA = smem;
+    uint8_t* sB = smem + GS_STAGES * GB_A_BYTES;
+    uint8_t* s_part = smem + GS_STAGES * GS_STAGE_BYTES;        // [rank][128 / S rows][128 columns] fp32
+    float* s_scale = reinterpret_cast<float*>(s_part + GB_M * GS_N * 4);
+    uint64_t* tempty = reinterpret_cast<uint64_t*>(s_scale + GB_RING * GB_ENTRY);
+    uint64_t* tfull = tempty + GS_BUFS;
+    uint64_t* full = tfull + GS_BUFS;
+    uint64_t* empty = full + GS_STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(empty + GS_STAGES);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < GS_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int a = 0; a < GS_BUFS; ++a) { mbar_init(&tfull[a], 2); mbar_init(&tempty[a], GB_EPI_WARPS); }
+        *abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tm_a);
+        prefetch_tmap(&tm_w);
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, GS_BUFS * GS_N);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (splits > 1) cluster_arrive();        // (waited for before anything is written to another CTA's memory)
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_trigger();
+    pdl_wait();
+
+    const int rank = (int)blockIdx.x % splits, tile = (int)(blockIdx.x / splits);
+    const int n_tiles = (g.n + GS_N - 1) / GS_N;
+    const int m0 = tile / n_tiles * GB_M, n0 = tile % n_tiles * GS_N;
+    const int k_blocks = (g.k + GB_K - 1) / GB_K;
+    const int kb0 = (int)((long long)k_blocks * rank / splits), blocks = (int)((long long)k_blocks * (rank + 1) / splits) - kb0;
+    const int slice = GB_M / splits;         // rows this CTA finishes
+
+    if (warp == 0) {
+        bool ok = true;
+        int it = 0;
+        for (; it < blocks; ++it) {
+            const int s = it % GS_STAGES;
+            if (!mbar_wait(&empty[s], ((it / GS_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+            if (elect_one()) {
+                mbar_expect_tx(&full[s], GS_STAGE_BYTES);
+                tma_load_2d(sA + s * GB_A_BYTES, &tm_a, (kb0 + it) * GB_K, m0, &full[s]);
+                tma_load_2d(sB + s * GS_N * GB_K, &tm_w, (kb0 + it) * GB_K, n0, &full[s]);
+            }
+            __syncwarp();
+        }
+        if (!ok) {
+            if (lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+            int seen = 0;                    // the copies still in flight land before the CTA leaves (a bounded wait each)
+            for (int j = max(0, it - GS_STAGES); j < it; ++j) mbar_wait(&full[j % GS_STAGES], (j / GS_STAGES) & 1, &seen);
+        }
+    } else if (warp == 1 || warp == 3) {
+        constexpr uint32_t idesc = idesc_e4m3(GB_M, GS_N);
+        bool ok = true;
+        for (int it = warp >> 1; it < blocks && ok; it += 2) {
+            const int s = it % GS_STAGES, buf = it % GS_BUFS;
+            const uint32_t d = tmem_base + buf * GS_N;
+            ok = mbar_wait(&full[s], (it / GS_STAGES) & 1, abort_flag) && mbar_wait(&tempty[buf], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t da = smem_desc(smem_u32(sA + s * GB_A_BYTES), 16, 1024, SWZ_128B);
+            const uint64_t db = smem_desc(smem_u32(sB + s * GS_N * GB_K), 16, 1024, SWZ_128B);
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_f8_ss(d, da + 2 * k, db + 2 * k, idesc, k != 0);
+                mma_commit(&tfull[buf]);
+                mma_commit(&empty[s]);
+            }
+            __syncwarp();
+        }
+        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+    } else if (warp == 2) {
+        // scales: as in the kernel above, of one block of weight rows
+        const float* as[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) as[i] = g.a_scale + (long long)min(m0 + 32 * i + lane, g.m - 1) * g.as_ld + kb0;
+        const float* ws = g.w_scale + (long long)(n0 / FP8_BLOCK) * g.ws_ld + kb0;
+        auto fetch = [&](int it) {
+            if (it < blocks) {
+                const uint32_t dst = smem_u32(s_scale + (it % GB_RING) * GB_ENTRY + lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) copy_async4(dst + 128 * i, as[i] + it);
+                if (lane == 0) copy_async4(dst + GB_M * 4, ws + it);
+            }
+            copy_async_commit();
+        };
+        for (int i = 0; i < GB_AHEAD; ++i) fetch(i);
+        bool ok = true;
+        for (int it = 0; it < blocks && ok; ++it) {
+            if (it >= GS_BUFS) ok = mbar_wait(&tfull[it % GS_BUFS], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
+            copy_async_wait<GB_AHEAD - 1>();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tfull[it % GS_BUFS]);
+            fetch(it + GB_AHEAD);
+        }
+        copy_async_wait<0>();
+        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+    } else {
+        const int quad = warp & 3, half = (warp - 4) >> 2;      // TMEM lane quadrant, 64-column half
+        const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + half * 64;
+        const uint32_t full_bar = smem_u32(&tfull[0]), empty_bar = smem_u32(&tempty[0]);
+        const uint32_t row_scale = smem_u32(s_scale + quad * 32 + lane), col_scale = smem_u32(s_scale + GB_M);
+        uint32_t entry = 0;
+        bool ok = true;
+        float acc[64];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+#pragma unroll 1
+        for (int it = 0; it < blocks && ok; ++it) {
+            const uint32_t buf = it % GS_BUFS, parity = (it / GS_BUFS) & 1;
+            if (!mbar_try_wait_addr(full_bar + 8 * buf, parity)) ok = mbar_wait_addr(full_bar + 8 * buf, parity, abort_flag);
+            const float s = load_shared(row_scale + entry) * load_shared(col_scale + entry);
+            tc_fence_after();
+            uint32_t r[64];
+            tmem_ld32(t_row + buf * GS_N, r);
+            tmem_ld32(t_row + buf * GS_N + 32, r + 32);
+            tmem_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_addr(empty_bar + 8 * buf);
+            pass_regs(r);
+            pass_regs(r + 32);
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = fmaf(__uint_as_float(r[i]), s, acc[i]);
+            entry = entry + GB_ENTRY * 4 == GB_RING * GB_ENTRY * 4 ? 0 : entry + GB_ENTRY * 4;
+        }
+        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+        if (splits > 1) cluster_wait();
+        // this row's partial sums to the CTA that finishes the row
+        const int row = quad * 32 + lane, owner = row / slice, r0 = row - owner * slice;
+        const uint32_t part = smem_u32(s_part) + (uint32_t)rank * slice * GS_N * 4;
+        const uint32_t dst = splits > 1 ? map_to_cta(part, owner) : part;
+        if (m0 + row < g.m) {
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                store_cluster4(dst + gs_unit(r0, half * 16 + u), acc[4 * u], acc[4 * u + 1], acc[4 * u + 2], acc[4 * u + 3]);
+        }
+    }
+    if (warp < 4 && splits > 1) cluster_wait();
+    __syncwarp();
+    tc_fence_before();
+    if (splits > 1) cluster_sync_all();      // all partial sums have arrived; nothing remote is touched after this
+    else __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, GS_BUFS * GS_N);
+    }
+    if (warp < 4) return;
+
+    const int col = n0 + lane * 4, cols = min(4, g.n - col);    // this lane's columns
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (g.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < cols)
+                bias[i] = g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[col + i]) : static_cast<const float*>(g.bias)[col + i];
+    }
+    for (int r = warp - 4; r < slice; r += GB_EPI_WARPS) {
+        const int row = m0 + rank * slice + r;
+        if (row >= g.m) break;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4 p = *reinterpret_cast<const float4*>(s_part + (size_t)s * slice * GS_N * 4 + gs_unit(r, lane));
+            v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += bias[i];
+        if constexpr (GELU) {
+            gelu_pair(v[0], v[1]);
+            gelu_pair(v[2], v[3]);
+        }
+        if constexpr (OUT == FD_E4M3) {
+            float amax = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+            amax = fmaxf(warp_max(amax), FP8_AMAX_FLOOR);        // columns behind n hold zeros
+            const float inv = E4M3_MAX / amax;
+            const uint32_t q = pack4_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            uint8_t* out = static_cast<uint8_t*>(g.out) + (long long)row * g.out_ld + col;
+            if (g.vec_out && cols == 4) *reinterpret_cast<uint32_t*>(out) = q;
+            else
+                for (int i = 0; i < cols; ++i) out[i] = (uint8_t)(q >> (8 * i));
+            if (lane == 0) g.out_scale[(long long)row * g.os_ld + n0 / FP8_BLOCK] = amax / E4M3_MAX;
+        } else if constexpr (OUT == FD_BF16) {
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.out) + (long long)row * g.out_ld + col;
+            if (g.vec_out && cols == 4) store4<__nv_bfloat16>(out, v[0], v[1], v[2], v[3]);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < cols) out[i] = __float2bfloat16_rn(v[i]);
+        } else {
+            float* out = static_cast<float*>(g.out) + (long long)row * g.out_ld + col;
+            if (g.vec_out && cols == 4) store4<float>(out, v[0], v[1], v[2], v[3]);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < cols) out[i] = v[i];
+        }
+    }
+}
+
+typedef void (*GbKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, GbArgs);
+template <bool PAIR> constexpr GbKernel GB_KERNELS[6] = {                // by output type, without and with GELU
+    gemm_blocks_kernel<PAIR, FD_F32, false>, gemm_blocks_kernel<PAIR, FD_F32, true>, gemm_blocks_kernel<PAIR, FD_BF16, false>,
+    gemm_blocks_kernel<PAIR, FD_BF16, true>, gemm_blocks_kernel<PAIR, FD_E4M3, false>, gemm_blocks_kernel<PAIR, FD_E4M3, true>};
+typedef void (*GsKernel)(const CUtensorMap, const CUtensorMap, GbArgs, int);
+constexpr GsKernel GS_KERNELS[6] = {gemm_blocks_split_kernel<FD_F32, false>, gemm_blocks_split_kernel<FD_F32, true>, gemm_blocks_split_kernel<FD_BF16, false>,
+                                    gemm_blocks_split_kernel<FD_BF16, true>, gemm_blocks_split_kernel<FD_E4M3, false>, gemm_blocks_split_kernel<FD_E4M3, true>};
+
+// Per-device set-up, done once: shared-memory attributes, the number of SMs and of CTA pairs the device keeps resident.
 struct GbDevice {
     std::atomic<int> ready{0};
-    int sms = 0, pairs = 0;
+    int sms = 0, pairs = 0, clusters[4] = {};   // clusters of 1, 2, 4, 8 CTAs of the split kernel resident at once
 };
 constexpr int GB_MAX_DEVICES = 64;
 GbDevice g_devices[GB_MAX_DEVICES];
 
-// launch of CTA pairs: clusters of two
-void pair_config(cudaLaunchConfig_t& lc, cudaLaunchAttribute* at, int grid, cudaStream_t st, bool pdl) {
+void cluster_config(cudaLaunchConfig_t& lc, cudaLaunchAttribute* at, int cluster, int grid, int smem, cudaStream_t st, bool pdl) {
     lc.gridDim = dim3(grid);
     lc.blockDim = dim3(GB_THREADS);
-    lc.dynamicSmemBytes = GbCfg<true>::SMEM;
+    lc.dynamicSmemBytes = smem;
     lc.stream = st;
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[0].val.clusterDim.x = cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = at;
     lc.numAttrs = pdl ? 2 : 1;
 }
 
-cudaError_t gb_device(int* sms, int* pairs) {
+cudaError_t gb_device(const GbDevice** out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -423,37 +682,43 @@ cudaError_t gb_device(int* sms, int* pairs) {
     if (!d.ready.load(std::memory_order_acquire)) {          // two threads may both do this: the same values
         int n = 0;
         e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(gemm_blocks_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<false>::SMEM);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(gemm_blocks_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<true>::SMEM);
+        for (int i = 0; i < 6 && e == cudaSuccess; ++i) {
+            e = cudaFuncSetAttribute(GB_KERNELS<false>[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<false>::SMEM);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(GB_KERNELS<true>[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<true>::SMEM);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(GS_KERNELS[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GS_SMEM);
+        }
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t lc = {};
         cudaLaunchAttribute at[2];
-        pair_config(lc, at, n & ~1, nullptr, false);
+        cluster_config(lc, at, 2, n & ~1, GbCfg<true>::SMEM, nullptr, false);
         int clusters = 0;
-        e = cudaOccupancyMaxActiveClusters(&clusters, gemm_blocks_kernel<true>, &lc);
+        e = cudaOccupancyMaxActiveClusters(&clusters, GB_KERNELS<true>[0], &lc);
         if (e != cudaSuccess) return e;
         d.pairs = max(1, min(n / 2, clusters));
+        for (int i = 0; i < 4; ++i) {
+            cluster_config(lc, at, 1 << i, n / (1 << i) * (1 << i), GS_SMEM, nullptr, false);
+            e = cudaOccupancyMaxActiveClusters(&d.clusters[i], GS_KERNELS[0], &lc);
+            if (e != cudaSuccess) return e;
+        }
         d.sms = n;
         d.ready.store(1, std::memory_order_release);
     }
-    *sms = d.sms;
-    *pairs = d.pairs;
+    *out = &d;
     return cudaSuccess;
 }
 
 }  // namespace
 
 cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, int k, cudaStream_t st, std::string* why) {
-    int sms = 0, pairs = 0;
-    cudaError_t e = gb_device(&sms, &pairs);
+    const GbDevice* dev = nullptr;
+    cudaError_t e = gb_device(&dev);
     if (e != cudaSuccess) return e;
     const int es = f.out_dtype == FD_F32 ? 4 : f.out_dtype == FD_BF16 ? 2 : 1;
     GbArgs g{f.a_scale, f.w_scale, f.bias, f.out, f.out_scale, f.status_out, f.a_scale_stride, f.w_scale_stride, f.out_stride,
-             f.out_scale_stride, m, n, k, f.bias_dtype == FD_BF16, f.out_dtype, f.gelu != 0,
+             f.out_scale_stride, m, n, k, f.bias_dtype == FD_BF16,
              // (a bulk store clips columns to whole 16 bytes)
-             (reinterpret_cast<uintptr_t>(f.out) & 15) == 0 && f.out_stride * es % 16 == 0 && (long long)n * es % 16 == 0};
+             (reinterpret_cast<uintptr_t>(f.out) & 15) == 0 && f.out_stride * es % 16 == 0 && f.out_stride * es < 1LL << 40 && (long long)n * es % 16 == 0,
+             reinterpret_cast<uintptr_t>(f.out) % (4 * es) == 0 && f.out_stride % 4 == 0};
     if (f.status_out) {
         e = cudaMemsetAsync(f.status_out, 0, sizeof(int32_t), st);
         if (e != cudaSuccess) return e;
@@ -461,11 +726,33 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
     CUtensorMap tm_a, tm_w, tm_o = {};
     const uint64_t da[2] = {(uint64_t)k, (uint64_t)m}, dw[2] = {(uint64_t)k, (uint64_t)n};
     const uint64_t sa[1] = {(uint64_t)f.a8_stride}, sw[1] = {(uint64_t)f.w8_stride};
-    const bool pair = getenv("GB_PAIR") ? atoi(getenv("GB_PAIR")) : m > GB_M;
-    const uint32_t box_a[2] = {GB_K, GB_M}, box_w[2] = {GB_K, (uint32_t)(pair ? 128 : 256)};
+    const bool pdl = f.status_out == nullptr;
+    const int which = 2 * (f.out_dtype == FD_F32 ? 0 : f.out_dtype == FD_BF16 ? 1 : 2) + (f.gelu ? 1 : 0);
+    const int k_blocks = (k + GB_K - 1) / GB_K;
+    // Which form: 128 x 128 tiles with K shared out where they all fit on the device at once; else CTAs (128 x 256) or CTA pairs
+    // (256 x 256), whichever needs less for its rounds of tiles, at 800 / 715 clk per block of K and 3000 clk a tile.  Measured
+    // (shared out / CTAs / pairs): 1001 x 1152 x 4608 11.4 / 19.3 / 20.0 us, 8 x 9216 x 1536 7.1 / 8.1 / 8.7, 154 x 4608 x 1536
+    // 8.0 / 9.3 / 9.6; 600 x 6144 x 1536 (240 tiles of 128) 25.8 / 12.0 / 12.2; 5216 x 4608 x 1536 (5 rounds of CTAs, 6 of
+    // pairs) 90 / 40.3 / 43.7; 16380 x 4608 x 1536 (16 of either) - / 129.7 / 119.5.
+    const long long tiles_split = (long long)((m + 127) / 128) * ((n + 127) / 128), n_tiles = (n + 255) / 256;
+    const long long tiles_one = (m + GB_M - 1) / GB_M * n_tiles, tiles_pair = (m + 2 * GB_M - 1) / (2 * GB_M) * n_tiles;
+    const double cost_one = (double)((tiles_one + dev->sms - 1) / dev->sms) * (k_blocks * 800.0 + 3000.0);
+    const double cost_pair = (double)((tiles_pair + dev->pairs - 1) / dev->pairs) * (k_blocks * 715.0 + 3000.0);
+    const bool split = tiles_split <= dev->clusters[0], pair = !split && cost_pair < cost_one;
+    const uint32_t box_a[2] = {GB_K, GB_M}, box_w[2] = {GB_K, (uint32_t)(split || pair ? 128 : 256)};
     if (!encode_tmap(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.a8), 2, da, sa, box_a, 128, why) ||
         !encode_tmap(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.w8), 2, dw, sw, box_w, 128, why))
         return cudaErrorInvalidValue;
+    if (split) {
+        // as many CTAs a tile as keep all clusters resident at once (36 clusters of four do not fit: 308 x 1536 x 6144 took 16.5 us
+        // with them against 12.0 with two)
+        int splits = 1;
+        for (int i = 1; i < 4 && (1 << i) <= k_blocks && tiles_split <= dev->clusters[i]; ++i) splits = 1 << i;
+        cudaLaunchConfig_t lc = {};
+        cudaLaunchAttribute at[2];
+        cluster_config(lc, at, splits, (int)(tiles_split * splits), GS_SMEM, st, pdl);
+        return cudaLaunchKernelEx(&lc, GS_KERNELS[which], tm_a, tm_w, g, splits);
+    }
     if (g.tma_out) {
         const uint64_t d_o[2] = {(uint64_t)n, (uint64_t)m}, s_o[1] = {(uint64_t)f.out_stride * es};
         const uint32_t box_o[2] = {(uint32_t)(128 / es), 32};
@@ -473,15 +760,13 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
                                          f.out_dtype == FD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
         if (!encode_tmap(&tm_o, type, f.out, 2, d_o, s_o, box_o, 128, why)) return cudaErrorInvalidValue;
     }
-    const bool pdl = f.status_out == nullptr;
-    const long long n_tiles = (n + 255) / 256;
     if (pair) {
         cudaLaunchConfig_t lc = {};
         cudaLaunchAttribute at[2];
-        pair_config(lc, at, 2 * (int)min((long long)pairs, (m + 255) / 256 * n_tiles), st, pdl);
-        return cudaLaunchKernelEx(&lc, gemm_blocks_kernel<true>, tm_a, tm_w, tm_o, g);
+        cluster_config(lc, at, 2, 2 * (int)min((long long)dev->pairs, tiles_pair), GbCfg<true>::SMEM, st, pdl);
+        return cudaLaunchKernelEx(&lc, GB_KERNELS<true>[which], tm_a, tm_w, tm_o, g);
     }
-    return launch_kernel(gemm_blocks_kernel<false>, (int)min((long long)sms, (m + GB_M - 1) / GB_M * n_tiles), GB_THREADS,
+    return launch_kernel(GB_KERNELS<false>[which], (int)min((long long)dev->sms, tiles_one), GB_THREADS,
                          GbCfg<false>::SMEM, st, pdl, tm_a, tm_w, tm_o, g);
 }
 

@@ -60,7 +60,8 @@ def _run(m, n, k, out, bias="f32", gelu=False, pad=0, width=None, seed=0):
 
 SIZES = [(1, 1, 1), (1, 128, 128), (1, 1536, 1536), (2, 40, 16), (8, 9216, 1536), (5, 130, 100), (16, 256, 4608), (17, 300, 384), (31, 129, 2200), (33, 1000, 1536),
          (64, 1152, 1152), (65, 257, 130), (100, 4608, 256), (128, 256, 128), (129, 128, 640), (154, 1536, 1536), (255, 255, 255), (256, 256, 256), (257, 513, 1000),
-         (300, 1152, 4608), (777, 1536, 1536), (1001, 1152, 4608), (2500, 520, 272), (5216, 4608, 128)]
+         (300, 1152, 4608), (777, 1536, 1536), (1001, 1152, 4608), (2500, 520, 272), (5216, 4608, 128),
+         (9472, 1024, 640), (4800, 1100, 400), (3000, 4424, 1152), (9000, 777, 1024), (5200, 4600, 500)]
 
 
 @pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
@@ -72,18 +73,18 @@ def test_matches_the_definition(m, n, k, out):
 @pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
 @pytest.mark.parametrize("bias", [None, "f32", "bf16"])
 @pytest.mark.parametrize("gelu", [False, True])
-@pytest.mark.parametrize("m,n,k", [(7, 200, 300), (70, 384, 512), (300, 776, 512)])
+@pytest.mark.parametrize("m,n,k", [(7, 200, 300), (70, 384, 512), (300, 776, 512), (5200, 4600, 300), (9400, 1000, 300)])
 def test_epilogues(m, n, k, out, bias, gelu):
     _run(m, n, k, out, bias=bias, gelu=gelu)
 
 
 @pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
-@pytest.mark.parametrize("m,n,k,pad,width", [(3, 200, 250, 1, 208), (90, 200, 250, 2, 201), (260, 300, 400, 1, 301), (260, 300, 400, 0, 304), (520, 1024, 256, 3, 1040)])
+@pytest.mark.parametrize("m,n,k,pad,width", [(3, 200, 250, 1, 208), (90, 200, 250, 2, 201), (260, 300, 400, 1, 301), (260, 300, 400, 0, 304), (520, 1024, 256, 3, 1040), (5200, 4600, 250, 1, 4616), (9400, 1000, 250, 1, 1001)])
 def test_strides_and_neighbours(m, n, k, pad, width, out):
     _run(m, n, k, out, pad=pad, width=width)
 
 
-@pytest.mark.parametrize("m", [1, 4, 20, 64, 100, 300])
+@pytest.mark.parametrize("m", [1, 4, 20, 64, 100, 300, 12000])
 def test_small_whole_numbers_are_exact(m):
     """Whole codes and scales that are powers of two: every sum fits fp32, so the result is exact and independent of order."""
     n, k = 384, 1111
@@ -117,7 +118,7 @@ def test_strided_scales_and_nan_codes(m):
     _check(out[rest], None, v, err, False)
 
 
-@pytest.mark.parametrize("m", [1, 8, 50, 300])
+@pytest.mark.parametrize("m", [1, 8, 50, 300, 8000])
 def test_repeated_runs_are_bit_equal(m):
     a8, a_s = _operand(m, 4608, 3, False)
     w8, w_s = _operand(640, 4608, 4, True)
