@@ -148,10 +148,18 @@ __device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_
         for (int c = 0; c < 128; c += 2) gelu_pair(v[c], v[c + 1]);
     }
     if constexpr (OUT == FD_E4M3) {
-        float amax = FP8_AMAX_FLOOR;
+        float part[8];                                       // (eight short chains instead of one of 128; columns behind n hold zeros)
 #pragma unroll
-        for (int c = 0; c < 128; ++c) amax = fmaxf(amax, fabsf(v[c]));      // columns behind n hold zeros
+        for (int i = 0; i < 8; ++i) part[i] = FP8_AMAX_FLOOR;
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) part[(c >> 1) & 7] = attn::max3(part[(c >> 1) & 7], fabsf(v[c]), fabsf(v[c + 1]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i] = fmaxf(part[i], part[i + 4]);
+        const float amax = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
         const float inv = E4M3_MAX / amax;
+        const uint64_t inv2 = attn::pair(inv, inv);
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) attn::unpair(mul2(attn::pair(v[c], v[c + 1]), inv2), v[c], v[c + 1]);
         if (row_base + lane < g.m) g.out_scale[(long long)(row_base + lane) * g.os_ld + col0 / FP8_BLOCK] = amax / E4M3_MAX;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -159,7 +167,7 @@ __device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float* w = v + u * 16 + k * 4;
-                q[k] = pack4_e4m3(w[0] * inv, w[1] * inv, w[2] * inv, w[3] * inv);
+                q[k] = pack4_e4m3(w[0], w[1], w[2], w[3]);
             }
             *unit_ptr(stage, lane, u) = make_uint4(q[0], q[1], q[2], q[3]);
         }
@@ -233,9 +241,9 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     pdl_wait();
 
     const uint32_t rank = PAIR ? cluster_ctarank() : 0;
-    const int unit = blockIdx.x / CTAS, n_units = gridDim.x / CTAS;
-    const int m_tiles = (g.m + CTAS * GB_M - 1) / (CTAS * GB_M), n_tiles = (g.n + GB_N - 1) / GB_N;
-    const long long total = (long long)m_tiles * n_tiles;
+    const uint32_t unit = blockIdx.x / CTAS, n_units = gridDim.x / CTAS;
+    const uint32_t m_tiles = (uint32_t)(g.m + CTAS * GB_M - 1) / (CTAS * GB_M), n_tiles = (uint32_t)(g.n + GB_N - 1) / GB_N;
+    const uint32_t total = (uint32_t)m_tiles * (uint32_t)n_tiles;     // (the launcher has checked that it fits)
     const int k_blocks = (g.k + GB_K - 1) / GB_K;
 
     if (warp < 4) {
@@ -244,7 +252,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             // (as for the products below: a converged warp with one elected lane; from a diverged lane a stage took 580 clk)
             uint32_t it = 0, s = 0, ph = 0;
             bool ok = true;
-            for (long long tile = unit; tile < total && ok; tile += n_units) {
+            for (uint32_t tile = unit; tile < total && ok; tile += n_units) {
                 const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
                 const int y_a = (m * CTAS + (int)rank) * GB_M, y_w = n * GB_N + (int)rank * Cfg::B_ROWS;
                 for (int kb = 0; kb < k_blocks; ++kb, ++it) {
@@ -278,7 +286,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             constexpr uint32_t idesc = idesc_e4m3(CTAS * GB_M, GB_N);
             const uint32_t buf = warp >> 1;
             const uint32_t d = tmem_base + buf * GB_N;
-            const uint32_t blocks = (uint32_t)((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;     // of all this CTA's tiles
+            const uint32_t blocks = ((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;     // of all this CTA's tiles
             bool ok = true;
             for (uint32_t it = buf; it < blocks && ok; it += 2) {
                 const int s = it % STAGES;
@@ -307,8 +315,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             // before the present one have been read by every warp, so entry (block + GB_AHEAD) of the ring is free.  Copies are
             // waited for group by group: an arrival that had to wait for the newest copies would put their latency into every block.
             const int w_blocks = (g.n + FP8_BLOCK - 1) / FP8_BLOCK;
-            const uint32_t blocks = (uint32_t)((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;
-            long long tile = unit;
+            const uint32_t blocks = ((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;
+            uint32_t tile = unit;
             const float *as[4], *ws;
             int k = 0;
             uint32_t fetched = 0;
@@ -358,7 +366,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
         const uint32_t row_scale = smem_u32(s_scale + quad * 32 + lane), col_scale = smem_u32(s_scale + GB_M + half);
         uint32_t entry = 0, parity = 0;
         bool ok = true;
-        for (long long tile = unit; tile < total && ok; tile += n_units) {
+        for (uint32_t tile = unit; tile < total && ok; tile += n_units) {
             const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
             const int row_base = (m * CTAS + (int)rank) * GB_M + quad * 32, col0 = n * GB_N + half * 128;
             uint32_t b[4] = {0u, 0u, 0u, 0u};                // bias of columns lane, lane + 32, ...: raw bits, first looked at when the tile is done
@@ -422,16 +430,74 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 
 // ------------------------------------------------------------------------------------------------
 // Few tiles (few rows, or a narrow output): 128 x 128 tiles whose blocks of K are shared out to the S CTAs of a cluster.
-// Every CTA leaves its partial sums, 128 / S rows for each CTA of the cluster, in that CTA's shared memory; after one cluster
-// barrier each adds the S partial sums of its rows in the order of the ranks (the result does not depend on timing) and
-// finishes them with the lanes along the columns, so that nothing needs to be transposed.
+// Every CTA leaves its partial sums in its own shared memory; after a cluster barrier each finishes 128 / S rows: a warp
+// fetches 16 / S rows from all S CTAs, all loads in flight at once and the lanes along the columns (nothing needs to be
+// transposed), adds them in the order of the ranks (the result does not depend on timing), finishes and stores them.  Written
+// straight into the finishing CTA's memory by the warps that hold the sums (a row per lane), the same exchange took twice as
+// long: 16-byte packets.
 // ------------------------------------------------------------------------------------------------
 constexpr int GS_N = 128, GS_STAGES = 4, GS_BUFS = 4;          // columns of a tile, stages, TMEM buffers
 constexpr int GS_STAGE_BYTES = GB_A_BYTES + GS_N * GB_K;
 constexpr int GS_SMEM = 1024 + GS_STAGES * GS_STAGE_BYTES + GB_M * GS_N * 4 /* partial sums */ + GB_RING * GB_ENTRY * 4 + 256;
 
-// 16-byte unit u (of 32) of row r in the partial sums of one rank: permuted against bank conflicts of the row-wise writers
+// 16-byte unit u (of 32) of row r of the partial sums: permuted against bank conflicts of the writers (a row per lane)
 __device__ __forceinline__ uint32_t gs_unit(int r, int u) { return (uint32_t)(r * 32 + (u ^ (r & 7))) * 16; }
+
+// Rows w, w + 8, ... of this CTA's slice: `part` is the partial sums' address in shared memory, the same in every CTA
+template <int S, int OUT, bool GELU>
+__device__ __forceinline__ void gs_finish(const GbArgs& g, uint32_t part, int rank, int w, int lane, int m0, int n0, const float* bias) {
+    constexpr int ROWS = 16 / S;
+    const int col = n0 + lane * 4, cols = min(4, g.n - col);    // this lane's columns
+    uint32_t base[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) base[s] = S > 1 ? map_to_cta(part, s) : part;
+    float4 p[ROWS][S];
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        const int r = rank * (128 / S) + 8 * j + w;
+#pragma unroll
+        for (int s = 0; s < S; ++s) p[j][s] = m0 + r < g.m ? load_cluster4(base[s] + gs_unit(r, lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        const int row = m0 + rank * (128 / S) + 8 * j + w;
+        if (row >= g.m) break;
+        float v[4] = {p[j][0].x, p[j][0].y, p[j][0].z, p[j][0].w};
+#pragma unroll
+        for (int s = 1; s < S; ++s) { v[0] += p[j][s].x; v[1] += p[j][s].y; v[2] += p[j][s].z; v[3] += p[j][s].w; }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += bias[i];
+        if constexpr (GELU) {
+            gelu_pair(v[0], v[1]);
+            gelu_pair(v[2], v[3]);
+        }
+        if constexpr (OUT == FD_E4M3) {
+            float amax = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+            amax = fmaxf(warp_max(amax), FP8_AMAX_FLOOR);        // columns behind n hold zeros
+            const float inv = E4M3_MAX / amax;
+            const uint32_t q = pack4_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            uint8_t* out = static_cast<uint8_t*>(g.out) + (long long)row * g.out_ld + col;
+            if (g.vec_out && cols == 4) *reinterpret_cast<uint32_t*>(out) = q;
+            else
+                for (int i = 0; i < cols; ++i) out[i] = (uint8_t)(q >> (8 * i));
+            if (lane == 0) g.out_scale[(long long)row * g.os_ld + n0 / FP8_BLOCK] = amax / E4M3_MAX;
+        } else if constexpr (OUT == FD_BF16) {
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.out) + (long long)row * g.out_ld + col;
+            if (g.vec_out && cols == 4) store4<__nv_bfloat16>(out, v[0], v[1], v[2], v[3]);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < cols) out[i] = __float2bfloat16_rn(v[i]);
+        } else {
+            float* out = static_cast<float*>(g.out) + (long long)row * g.out_ld + col;
+            if (g.vec_out && cols == 4) store4<float>(out, v[0], v[1], v[2], v[3]);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < cols) out[i] = v[i];
+        }
+    }
+}
 
 template <int OUT, bool GELU>
 __global__ void __launch_bounds__(GB_THREADS, 1)
@@ -440,7 +506,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* sA = smem;
     uint8_t* sB = smem + GS_STAGES * GB_A_BYTES;
-    uint8_t* s_part = smem + GS_STAGES * GS_STAGE_BYTES;        // [rank][128 / S rows][128 columns] fp32
+    uint8_t* s_part = smem + GS_STAGES * GS_STAGE_BYTES;        // [128 rows][128 columns] fp32
     float* s_scale = reinterpret_cast<float*>(s_part + GB_M * GS_N * 4);
     uint64_t* tempty = reinterpret_cast<uint64_t*>(s_scale + GB_RING * GB_ENTRY);
     uint64_t* tfull = tempty + GS_BUFS;
@@ -450,45 +516,66 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < GS_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < GS_BUFS; ++a) { mbar_init(&tfull[a], 2); mbar_init(&tempty[a], GB_EPI_WARPS); }
-        *abort_flag = 0;
-        fence_barrier_init();
-        prefetch_tmap(&tm_a);
-        prefetch_tmap(&tm_w);
-    }
-    if (warp == 1) {
-        tmem_alloc(tmem_slot, GS_BUFS * GS_N);
-        tmem_relinquish();
-    }
-    tc_fence_before();
-    __syncthreads();
-    if (splits > 1) cluster_arrive();        // (waited for before anything is written to another CTA's memory)
-    tc_fence_after();
-    const uint32_t tmem_base = *tmem_slot;
-    pdl_trigger();
-    pdl_wait();
-
     const int rank = (int)blockIdx.x % splits, tile = (int)(blockIdx.x / splits);
     const int n_tiles = (g.n + GS_N - 1) / GS_N;
     const int m0 = tile / n_tiles * GB_M, n0 = tile % n_tiles * GS_N;
     const int k_blocks = (g.k + GB_K - 1) / GB_K;
     const int kb0 = (int)((long long)k_blocks * rank / splits), blocks = (int)((long long)k_blocks * (rank + 1) / splits) - kb0;
-    const int slice = GB_M / splits;         // rows this CTA finishes
+
+    auto load_stage = [&](int it) {          // whole warp 0
+        const int s = it % GS_STAGES;
+        if (elect_one()) {
+            mbar_expect_tx(&full[s], GS_STAGE_BYTES);
+            tma_load_2d(sA + s * GB_A_BYTES, &tm_a, (kb0 + it) * GB_K, m0, &full[s]);
+            tma_load_2d(sB + s * GS_N * GB_K, &tm_w, (kb0 + it) * GB_K, n0, &full[s]);
+        }
+        __syncwarp();
+    };
+    // scales: as in the kernel above, of one block of weight rows (warp 2)
+    const float* as[4];
+    const float* ws = g.w_scale + (long long)(n0 / FP8_BLOCK) * g.ws_ld + kb0;
+    auto fetch = [&](int it) {
+        if (it < blocks) {
+            const uint32_t dst = smem_u32(s_scale + (it % GB_RING) * GB_ENTRY + lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) copy_async4(dst + 128 * i, as[i] + it);
+            if (lane == 0) copy_async4(dst + GB_M * 4, ws + it);
+        }
+        copy_async_commit();
+    };
+    // what latency there is comes from the first loads: they leave before the rest of the set-up is done
+    if (warp == 0) {
+        if (lane == 0) {
+            for (int s = 0; s < GS_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+            for (int a = 0; a < GS_BUFS; ++a) { mbar_init(&tfull[a], 2); mbar_init(&tempty[a], GB_EPI_WARPS); }
+            *abort_flag = 0;
+            fence_barrier_init();
+        }
+        __syncwarp();
+        pdl_wait();
+        for (int it = 0; it < min(blocks, GS_STAGES); ++it) load_stage(it);
+    } else if (warp == 1) {
+        tmem_alloc(tmem_slot, GS_BUFS * GS_N);
+        tmem_relinquish();
+    } else if (warp == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) as[i] = g.a_scale + (long long)min(m0 + 32 * i + lane, g.m - 1) * g.as_ld + kb0;
+        pdl_wait();
+        for (int i = 0; i < GB_AHEAD; ++i) fetch(i);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_trigger();
+    pdl_wait();
 
     if (warp == 0) {
         bool ok = true;
-        int it = 0;
+        int it = min(blocks, GS_STAGES);
         for (; it < blocks; ++it) {
-            const int s = it % GS_STAGES;
-            if (!mbar_wait(&empty[s], ((it / GS_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
-            if (elect_one()) {
-                mbar_expect_tx(&full[s], GS_STAGE_BYTES);
-                tma_load_2d(sA + s * GB_A_BYTES, &tm_a, (kb0 + it) * GB_K, m0, &full[s]);
-                tma_load_2d(sB + s * GS_N * GB_K, &tm_w, (kb0 + it) * GB_K, n0, &full[s]);
-            }
-            __syncwarp();
+            if (!mbar_wait(&empty[it % GS_STAGES], ((it / GS_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+            load_stage(it);
         }
         if (!ok) {
             if (lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
@@ -516,21 +603,6 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
         }
         if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
     } else if (warp == 2) {
-        // scales: as in the kernel above, of one block of weight rows
-        const float* as[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) as[i] = g.a_scale + (long long)min(m0 + 32 * i + lane, g.m - 1) * g.as_ld + kb0;
-        const float* ws = g.w_scale + (long long)(n0 / FP8_BLOCK) * g.ws_ld + kb0;
-        auto fetch = [&](int it) {
-            if (it < blocks) {
-                const uint32_t dst = smem_u32(s_scale + (it % GB_RING) * GB_ENTRY + lane);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) copy_async4(dst + 128 * i, as[i] + it);
-                if (lane == 0) copy_async4(dst + GB_M * 4, ws + it);
-            }
-            copy_async_commit();
-        };
-        for (int i = 0; i < GB_AHEAD; ++i) fetch(i);
         bool ok = true;
         for (int it = 0; it < blocks && ok; ++it) {
             if (it >= GS_BUFS) ok = mbar_wait(&tfull[it % GS_BUFS], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
@@ -571,77 +643,40 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
             entry = entry + GB_ENTRY * 4 == GB_RING * GB_ENTRY * 4 ? 0 : entry + GB_ENTRY * 4;
         }
         if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
-        if (splits > 1) cluster_wait();
-        // this row's partial sums to the CTA that finishes the row
-        const int row = quad * 32 + lane, owner = row / slice, r0 = row - owner * slice;
-        const uint32_t part = smem_u32(s_part) + (uint32_t)rank * slice * GS_N * 4;
-        const uint32_t dst = splits > 1 ? map_to_cta(part, owner) : part;
+        const int row = quad * 32 + lane;
         if (m0 + row < g.m) {
 #pragma unroll
             for (int u = 0; u < 16; ++u)
-                store_cluster4(dst + gs_unit(r0, half * 16 + u), acc[4 * u], acc[4 * u + 1], acc[4 * u + 2], acc[4 * u + 3]);
+                *reinterpret_cast<float4*>(s_part + gs_unit(row, half * 16 + u)) = make_float4(acc[4 * u], acc[4 * u + 1], acc[4 * u + 2], acc[4 * u + 3]);
         }
     }
-    if (warp < 4 && splits > 1) cluster_wait();
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};    // of columns n0 + 4 lane ..: fetched before the barrier
+    if (warp >= 4 && g.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = n0 + lane * 4 + i;
+            if (c < g.n) bias[i] = g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[c]) : static_cast<const float*>(g.bias)[c];
+        }
+    }
     __syncwarp();
     tc_fence_before();
-    if (splits > 1) cluster_sync_all();      // all partial sums have arrived; nothing remote is touched after this
+    if (splits > 1) cluster_sync_all();      // all partial sums are there
     else __syncthreads();
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem_base, GS_BUFS * GS_N);
     }
-    if (warp < 4) return;
-
-    const int col = n0 + lane * 4, cols = min(4, g.n - col);    // this lane's columns
-    float bias[4] = {0.f, 0.f, 0.f, 0.f};
-    if (g.bias) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < cols)
-                bias[i] = g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[col + i]) : static_cast<const float*>(g.bias)[col + i];
-    }
-    for (int r = warp - 4; r < slice; r += GB_EPI_WARPS) {
-        const int row = m0 + rank * slice + r;
-        if (row >= g.m) break;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float4 p = *reinterpret_cast<const float4*>(s_part + (size_t)s * slice * GS_N * 4 + gs_unit(r, lane));
-            v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += bias[i];
-        if constexpr (GELU) {
-            gelu_pair(v[0], v[1]);
-            gelu_pair(v[2], v[3]);
-        }
-        if constexpr (OUT == FD_E4M3) {
-            float amax = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-            amax = fmaxf(warp_max(amax), FP8_AMAX_FLOOR);        // columns behind n hold zeros
-            const float inv = E4M3_MAX / amax;
-            const uint32_t q = pack4_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-            uint8_t* out = static_cast<uint8_t*>(g.out) + (long long)row * g.out_ld + col;
-            if (g.vec_out && cols == 4) *reinterpret_cast<uint32_t*>(out) = q;
-            else
-                for (int i = 0; i < cols; ++i) out[i] = (uint8_t)(q >> (8 * i));
-            if (lane == 0) g.out_scale[(long long)row * g.os_ld + n0 / FP8_BLOCK] = amax / E4M3_MAX;
-        } else if constexpr (OUT == FD_BF16) {
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.out) + (long long)row * g.out_ld + col;
-            if (g.vec_out && cols == 4) store4<__nv_bfloat16>(out, v[0], v[1], v[2], v[3]);
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < cols) out[i] = __float2bfloat16_rn(v[i]);
-        } else {
-            float* out = static_cast<float*>(g.out) + (long long)row * g.out_ld + col;
-            if (g.vec_out && cols == 4) store4<float>(out, v[0], v[1], v[2], v[3]);
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < cols) out[i] = v[i];
+    if (warp >= 4) {
+        const uint32_t part = smem_u32(s_part);
+        switch (splits) {
+            case 1: gs_finish<1, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            case 2: gs_finish<2, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            case 4: gs_finish<4, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            default: gs_finish<8, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
         }
     }
+    __syncwarp();
+    if (splits > 1) cluster_sync_all();      // no CTA leaves while another reads its memory
 }
 
 typedef void (*GbKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, GbArgs);
@@ -731,13 +766,17 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
     const int k_blocks = (k + GB_K - 1) / GB_K;
     // Which form: 128 x 128 tiles with K shared out where they all fit on the device at once; else CTAs (128 x 256) or CTA pairs
     // (256 x 256), whichever needs less for its rounds of tiles, at 800 / 715 clk per block of K and 3000 clk a tile.  Measured
-    // (shared out / CTAs / pairs): 1001 x 1152 x 4608 11.4 / 19.3 / 20.0 us, 8 x 9216 x 1536 7.1 / 8.1 / 8.7, 154 x 4608 x 1536
-    // 8.0 / 9.3 / 9.6; 600 x 6144 x 1536 (240 tiles of 128) 25.8 / 12.0 / 12.2; 5216 x 4608 x 1536 (5 rounds of CTAs, 6 of
-    // pairs) 90 / 40.3 / 43.7; 16380 x 4608 x 1536 (16 of either) - / 129.7 / 119.5.
+    // (shared out / CTAs / pairs): 1001 x 1152 x 4608 10.7 / 19.3 / 20.0 us, 8 x 9216 x 1536 7.1 / 8.1 / 8.7, 154 x 4608 x 1536
+    // 6.8 / 9.3 / 9.6; 600 x 6144 x 1536 (240 tiles of 128) 25.8 / 12.0 / 12.2; 5216 x 4608 x 1536 (5 rounds of CTAs, 6 of
+    // pairs) 90 / 40.3 / 43.7; 16380 x 4608 x 1536 (16 of either) - / 129.7 / 117.4.
     const long long tiles_split = (long long)((m + 127) / 128) * ((n + 127) / 128), n_tiles = (n + 255) / 256;
     const long long tiles_one = (m + GB_M - 1) / GB_M * n_tiles, tiles_pair = (m + 2 * GB_M - 1) / (2 * GB_M) * n_tiles;
     const double cost_one = (double)((tiles_one + dev->sms - 1) / dev->sms) * (k_blocks * 800.0 + 3000.0);
     const double cost_pair = (double)((tiles_pair + dev->pairs - 1) / dev->pairs) * (k_blocks * 715.0 + 3000.0);
+    if (tiles_one * k_blocks > 1LL << 30) {
+        if (why) *why = "more than 2^30 blocks of 128 x 256 x 128";
+        return cudaErrorInvalidValue;
+    }
     const bool split = tiles_split <= dev->clusters[0], pair = !split && cost_pair < cost_one;
     const uint32_t box_a[2] = {GB_K, GB_M}, box_w[2] = {GB_K, (uint32_t)(split || pair ? 128 : 256)};
     if (!encode_tmap(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.a8), 2, da, sa, box_a, 128, why) ||
@@ -745,7 +784,7 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
         return cudaErrorInvalidValue;
     if (split) {
         // as many CTAs a tile as keep all clusters resident at once (36 clusters of four do not fit: 308 x 1536 x 6144 took 16.5 us
-        // with them against 12.0 with two)
+        // with them against 12.0 with pairs)
         int splits = 1;
         for (int i = 1; i < 4 && (1 << i) <= k_blocks && tiles_split <= dev->clusters[i]; ++i) splits = 1 << i;
         cudaLaunchConfig_t lc = {};
