@@ -430,8 +430,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 
 // ------------------------------------------------------------------------------------------------
 // Few tiles (few rows, or a narrow output): 128 x 128 tiles whose blocks of K are shared out to the S CTAs of a cluster.
-// Every CTA leaves its partial sums in its own shared memory; after a cluster barrier each finishes 128 / S rows: a warp
-// fetches 16 / S rows from all S CTAs, all loads in flight at once and the lanes along the columns (nothing needs to be
+// Every CTA leaves its partial sums in its own shared memory; after a cluster barrier each finishes its share of the rows: a warp
+// fetches ceil(16 / S) rows from all S CTAs, all loads in flight at once and the lanes along the columns (nothing needs to be
 // transposed), adds them in the order of the ranks (the result does not depend on timing), finishes and stores them.  Written
 // straight into the finishing CTA's memory by the warps that hold the sums (a row per lane), the same exchange took twice as
 // long: 16-byte packets.
@@ -446,7 +446,7 @@ __device__ __forceinline__ uint32_t gs_unit(int r, int u) { return (uint32_t)(r 
 // Rows w, w + 8, ... of this CTA's slice: `part` is the partial sums' address in shared memory, the same in every CTA
 template <int S, int OUT, bool GELU>
 __device__ __forceinline__ void gs_finish(const GbArgs& g, uint32_t part, int rank, int w, int lane, int m0, int n0, const float* bias) {
-    constexpr int ROWS = 16 / S;
+    constexpr int ROWS = (16 + S - 1) / S, SLICE = 8 * ROWS;      // rows of a warp, of the CTA
     const int col = n0 + lane * 4, cols = min(4, g.n - col);    // this lane's columns
     uint32_t base[S];
 #pragma unroll
@@ -454,14 +454,14 @@ __device__ __forceinline__ void gs_finish(const GbArgs& g, uint32_t part, int ra
     float4 p[ROWS][S];
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
-        const int r = rank * (128 / S) + 8 * j + w;
+        const int r = rank * SLICE + 8 * j + w;
 #pragma unroll
-        for (int s = 0; s < S; ++s) p[j][s] = m0 + r < g.m ? load_cluster4(base[s] + gs_unit(r, lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < S; ++s) p[j][s] = r < GB_M && m0 + r < g.m ? load_cluster4(base[s] + gs_unit(r, lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
-        const int row = m0 + rank * (128 / S) + 8 * j + w;
-        if (row >= g.m) break;
+        const int r = rank * SLICE + 8 * j + w, row = m0 + r;
+        if (r >= GB_M || row >= g.m) break;
         float v[4] = {p[j][0].x, p[j][0].y, p[j][0].z, p[j][0].w};
 #pragma unroll
         for (int s = 1; s < S; ++s) { v[0] += p[j][s].x; v[1] += p[j][s].y; v[2] += p[j][s].z; v[3] += p[j][s].w; }
@@ -501,7 +501,7 @@ __device__ __forceinline__ void gs_finish(const GbArgs& g, uint32_t part, int ra
 
 template <int OUT, bool GELU>
 __global__ void __launch_bounds__(GB_THREADS, 1)
-gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, GbArgs g, int splits) {
+gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, GbArgs g, int splits, int a_rows) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* sA = smem;
@@ -525,7 +525,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     auto load_stage = [&](int it) {          // whole warp 0
         const int s = it % GS_STAGES;
         if (elect_one()) {
-            mbar_expect_tx(&full[s], GS_STAGE_BYTES);
+            mbar_expect_tx(&full[s], a_rows * GB_K + GS_N * GB_K);
             tma_load_2d(sA + s * GB_A_BYTES, &tm_a, (kb0 + it) * GB_K, m0, &full[s]);
             tma_load_2d(sB + s * GS_N * GB_K, &tm_w, (kb0 + it) * GB_K, n0, &full[s]);
         }
@@ -671,7 +671,11 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
         switch (splits) {
             case 1: gs_finish<1, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
             case 2: gs_finish<2, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            case 3: gs_finish<3, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
             case 4: gs_finish<4, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            case 5: gs_finish<5, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            case 6: gs_finish<6, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
+            case 7: gs_finish<7, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
             default: gs_finish<8, OUT, GELU>(g, part, rank, warp - 4, lane, m0, n0, bias); break;
         }
     }
@@ -683,14 +687,14 @@ typedef void (*GbKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap
 template <bool PAIR> constexpr GbKernel GB_KERNELS[6] = {                // by output type, without and with GELU
     gemm_blocks_kernel<PAIR, FD_F32, false>, gemm_blocks_kernel<PAIR, FD_F32, true>, gemm_blocks_kernel<PAIR, FD_BF16, false>,
     gemm_blocks_kernel<PAIR, FD_BF16, true>, gemm_blocks_kernel<PAIR, FD_E4M3, false>, gemm_blocks_kernel<PAIR, FD_E4M3, true>};
-typedef void (*GsKernel)(const CUtensorMap, const CUtensorMap, GbArgs, int);
+typedef void (*GsKernel)(const CUtensorMap, const CUtensorMap, GbArgs, int, int);
 constexpr GsKernel GS_KERNELS[6] = {gemm_blocks_split_kernel<FD_F32, false>, gemm_blocks_split_kernel<FD_F32, true>, gemm_blocks_split_kernel<FD_BF16, false>,
                                     gemm_blocks_split_kernel<FD_BF16, true>, gemm_blocks_split_kernel<FD_E4M3, false>, gemm_blocks_split_kernel<FD_E4M3, true>};
 
 // Per-device set-up, done once: shared-memory attributes, the number of SMs and of CTA pairs the device keeps resident.
 struct GbDevice {
     std::atomic<int> ready{0};
-    int sms = 0, pairs = 0, clusters[4] = {};   // clusters of 1, 2, 4, 8 CTAs of the split kernel resident at once
+    int sms = 0, pairs = 0, clusters[8] = {};   // clusters of 1 .. 8 CTAs of the split kernel resident at once
 };
 constexpr int GB_MAX_DEVICES = 64;
 GbDevice g_devices[GB_MAX_DEVICES];
@@ -730,8 +734,8 @@ cudaError_t gb_device(const GbDevice** out) {
         e = cudaOccupancyMaxActiveClusters(&clusters, GB_KERNELS<true>[0], &lc);
         if (e != cudaSuccess) return e;
         d.pairs = max(1, min(n / 2, clusters));
-        for (int i = 0; i < 4; ++i) {
-            cluster_config(lc, at, 1 << i, n / (1 << i) * (1 << i), GS_SMEM, nullptr, false);
+        for (int i = 0; i < 8; ++i) {
+            cluster_config(lc, at, i + 1, n / (i + 1) * (i + 1), GS_SMEM, nullptr, false);
             e = cudaOccupancyMaxActiveClusters(&d.clusters[i], GS_KERNELS[0], &lc);
             if (e != cudaSuccess) return e;
         }
@@ -766,7 +770,7 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
     const int k_blocks = (k + GB_K - 1) / GB_K;
     // Which form: 128 x 128 tiles with K shared out where they all fit on the device at once; else CTAs (128 x 256) or CTA pairs
     // (256 x 256), whichever needs less for its rounds of tiles, at 800 / 715 clk per block of K and 3000 clk a tile.  Measured
-    // (shared out / CTAs / pairs): 1001 x 1152 x 4608 10.7 / 19.3 / 20.0 us, 8 x 9216 x 1536 7.1 / 8.1 / 8.7, 154 x 4608 x 1536
+    // (shared out / CTAs / pairs): 1001 x 1152 x 4608 10.6 / 19.3 / 20.0 us, 8 x 9216 x 1536 5.7 / 8.1 / 8.7, 154 x 4608 x 1536
     // 6.8 / 9.3 / 9.6; 600 x 6144 x 1536 (240 tiles of 128) 25.8 / 12.0 / 12.2; 5216 x 4608 x 1536 (5 rounds of CTAs, 6 of
     // pairs) 90 / 40.3 / 43.7; 16380 x 4608 x 1536 (16 of either) - / 129.7 / 117.4.
     const long long tiles_split = (long long)((m + 127) / 128) * ((n + 127) / 128), n_tiles = (n + 255) / 256;
@@ -778,19 +782,24 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
         return cudaErrorInvalidValue;
     }
     const bool split = tiles_split <= dev->clusters[0], pair = !split && cost_pair < cost_one;
-    const uint32_t box_a[2] = {GB_K, GB_M}, box_w[2] = {GB_K, (uint32_t)(split || pair ? 128 : 256)};
+    // With few rows the box ends with them: rows of a box that lie behind the tensor are filled with zeros at a cost (9 x 6144 x
+    // 6144: 15.3 us with boxes of 128 rows, 9.9 so; eight rows x 9216 x 1536: 7.2 and 5.7).  What the products then read in the
+    // rows behind the box is not stored.
+    const int a_rows = split ? min(GB_M, (m + 7) / 8 * 8) : GB_M;
+    const uint32_t box_a[2] = {GB_K, (uint32_t)a_rows}, box_w[2] = {GB_K, (uint32_t)(split || pair ? 128 : 256)};
     if (!encode_tmap(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.a8), 2, da, sa, box_a, 128, why) ||
         !encode_tmap(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.w8), 2, dw, sw, box_w, 128, why))
         return cudaErrorInvalidValue;
     if (split) {
-        // as many CTAs a tile as keep all clusters resident at once (36 clusters of four do not fit: 308 x 1536 x 6144 took 16.5 us
-        // with them against 12.0 with pairs)
+        // as many CTAs a tile as leave each six blocks of K (1 x 4608 x 1536: 5.4 us with two CTAs, 5.75 with three) and keep all
+        // clusters resident at once (36 clusters of four do not fit: 308 x 1536 x 6144 took 16.5 us
+        // with them against 12.0 with clusters of two)
         int splits = 1;
-        for (int i = 1; i < 4 && (1 << i) <= k_blocks && tiles_split <= dev->clusters[i]; ++i) splits = 1 << i;
+        while (splits < 8 && k_blocks / (splits + 1) >= 6 && tiles_split <= dev->clusters[splits]) ++splits;
         cudaLaunchConfig_t lc = {};
         cudaLaunchAttribute at[2];
         cluster_config(lc, at, splits, (int)(tiles_split * splits), GS_SMEM, st, pdl);
-        return cudaLaunchKernelEx(&lc, GS_KERNELS[which], tm_a, tm_w, g, splits);
+        return cudaLaunchKernelEx(&lc, GS_KERNELS[which], tm_a, tm_w, g, splits, a_rows);
     }
     if (g.tma_out) {
         const uint64_t d_o[2] = {(uint64_t)n, (uint64_t)m}, s_o[1] = {(uint64_t)f.out_stride * es};
