@@ -4,6 +4,8 @@
 // registers of W warps between the sum of squares and the output (16 lanes hold one block of 128 columns, 8 columns
 // each, so a block's amax is four shuffles and its codes leave as one 128-byte segment).  Sums, the norm and the scales
 // are fp32; the stored residual is the only rounding besides the outputs themselves.
+// Measured: 16380 x 1536, bf16 + fp32 residual to 8 bits (278 MB): 45.5 us, 6.1 TB/s; 3997 x 1152, all bf16 (37 MB): 8.6 us; 8192 x
+// 1536 quantised alone (38 MB): 7.8 us; one token 1.9 us; 5000 x 1333 (element accesses, 86 MB): 34 us.
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -11,21 +13,35 @@ namespace fd {
 
 namespace {
 
-// eight consecutive values as fp32, 16-byte accesses
-template <typename T> __device__ __forceinline__ void load8(const T* p, float* f);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float* f) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float* f) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// eight consecutive values, 16-byte accesses: as they lie in memory, and as fp32
+template <typename T> struct Raw8;
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
+    __device__ __forceinline__ void set(float v) { a = b = make_float4(v, v, v, v); }
+    __device__ __forceinline__ void get(float* f) const {
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
     }
-}
+};
+template <> struct Raw8<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    }
+    __device__ __forceinline__ void set(float v) {
+        const uint32_t h = __float_as_uint(v) >> 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = h | (h << 16);
+    }
+    __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
 template <typename T> __device__ __forceinline__ void store8(T* p, const float* f);
 template <> __device__ __forceinline__ void store8<float>(float* p, const float* f) {
     reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
@@ -55,46 +71,72 @@ struct RowArgs {
     float eps;
 };
 
-// W warps hold one row, NV vectors of 8 columns per lane (cols <= 256 W NV, a multiple of 8)
+template <typename TX, typename TR, bool NORM> constexpr bool row_ahead = !NORM || sizeof(TX) + sizeof(TR) <= 6;
+
+// W warps hold one row, NV vectors of 8 columns per lane (cols <= 256 W NV, a multiple of 8).  CTAs stay and walk the rows: the
+// weights are fetched once, and the next row is requested before the present one is reduced.  (AHEAD; not with fp32 rows and
+// an fp32 residual, where its registers cost more warps than it gives: there a CTA takes one row, 4000 x 4608 in 45.9 us
+// against 51.5.)
 template <typename TX, typename TR, int W, int NV, bool NORM>
 __global__ void __launch_bounds__(W < 4 ? 128 : 32 * W)
 row_blocks_kernel(RowArgs a) {
     constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
-    __shared__ float s_part[THREADS / 32];
+    __shared__ float s_part[2][THREADS / 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wr = warp % W, rc = warp / W;                 // warp within its row, row within the CTA
     const int col0 = (wr * 2 + (lane >> 4)) * FP8_BLOCK + (lane & 15) * 8;
+    constexpr bool AHEAD = row_ahead<TX, TR, NORM>;
+    const float inv_cols = 1.0f / (float)a.cols;
     ptx::pdl_wait();
-    for (long long row0 = (long long)blockIdx.x * RPC; row0 < a.rows; row0 += (long long)gridDim.x * RPC) {
+    Raw8<TX> x[NV], w[NORM ? NV : 1];
+    Raw8<TR> t[NORM ? NV : 1];
+    auto request = [&](long long row) {
+        const TX* px = static_cast<const TX*>(a.x) + row * a.x_ld + col0;
+        const TR* pt = static_cast<const TR*>(a.residual) + row * a.res_ld + col0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (col0 + i * W * 256 < a.cols) {
+                x[i].load(px + i * W * 256);
+                if constexpr (NORM)
+                    if (a.residual) t[i].load(pt + i * W * 256);
+            }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        x[i].set(0.f);
+        if constexpr (NORM) {
+            t[i].set(0.f);
+            w[i].set(1.f);
+        }
+    }
+    const long long step = (long long)gridDim.x * RPC;
+    long long row0 = (long long)blockIdx.x * RPC;
+    if (AHEAD && row0 + rc < a.rows) request(row0 + rc);
+    if constexpr (NORM)
+        if (a.weight)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (col0 + i * W * 256 < a.cols) w[i].load(static_cast<const TX*>(a.weight) + col0 + i * W * 256);
+    int turn = 0;
+    for (; row0 < a.rows; row0 += step, turn ^= 1) {
         const long long row = row0 + rc;
         const bool live = row < a.rows;
-        const TX* x = static_cast<const TX*>(a.x) + row * a.x_ld;
+        if (!AHEAD && live) request(row);
         float v[NV][8];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = col0 + i * W * 256;
-            if (live && c < a.cols) load8<TX>(x + c, v[i]);
-            else
+            x[i].get(v[i]);
+            if constexpr (NORM) {
+                if (a.residual) {
+                    float r[8];
+                    t[i].get(r);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
-        }
-        if constexpr (NORM) {
-            if (a.residual) {
-                const TR* res = static_cast<const TR*>(a.residual) + row * a.res_ld;
-                float t[NV][8];
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c = col0 + i * W * 256;
-                    if (live && c < a.cols) load8<TR>(res + c, t[i]);
-                    else
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) t[i][k] = 0.f;
+                    for (int k = 0; k < 8; ++k) v[i][k] += r[k];
                 }
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] += t[i][k];
             }
+        }
+        if (AHEAD && row + step < a.rows) request(row + step);
+        if constexpr (NORM) {
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
@@ -110,24 +152,19 @@ row_blocks_kernel(RowArgs a) {
             }
             ss = warp_sum(ss);
             if constexpr (W > 1) {
-                __syncthreads();                            // the previous row's readers are done
-                if (lane == 0) s_part[warp] = ss;
+                if (lane == 0) s_part[turn][warp] = ss;     // (two turns: a row's sums are read before the row after next is written)
                 __syncthreads();
                 ss = 0.f;
 #pragma unroll
-                for (int i = 0; i < W; ++i) ss += s_part[rc * W + i];
+                for (int i = 0; i < W; ++i) ss += s_part[turn][rc * W + i];
             }
-            const float rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+            const float rstd = 1.0f / sqrtf(fmaf(ss, inv_cols, a.eps));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = col0 + i * W * 256;
-                float w[8];
-                if (a.weight && c < a.cols) load8<TX>(static_cast<const TX*>(a.weight) + c, w);
-                else
+                float g[8];
+                w[i].get(g);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) w[k] = 1.f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * rstd * w[k];
+                for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * rstd * g[k];
             }
             if (a.y && live) {
                 TX* y = static_cast<TX*>(a.y) + row * a.y_ld;
@@ -162,53 +199,67 @@ row_blocks_kernel(RowArgs a) {
     ptx::pdl_trigger();
 }
 
-// Any width, stride and alignment: one CTA per row, element accesses, the row read a second time for the output (each
-// element is read and written by the same thread there, so the in-place forms hold).  A warp takes a block at a time,
-// each lane four columns 32 apart.
-constexpr int ROW_ANY_THREADS = 256;
-
-template <typename TX, typename TR, bool NORM>
-__global__ void __launch_bounds__(ROW_ANY_THREADS)
+// Any width, stride and alignment: one CTA per row, element accesses.  A warp holds whole blocks, each lane four columns 32
+// apart; up to MB blocks a warp stay in its registers.  MB = 0: wider rows, read a second time for the output (each element is
+// read and written by the same thread there, so the in-place forms hold).
+template <typename TX, typename TR, bool NORM, int THREADS, int MB>
+__global__ void __launch_bounds__(THREADS)
 row_blocks_any_kernel(RowArgs a) {
-    __shared__ float s_part[ROW_ANY_THREADS / 32];
+    constexpr int WARPS = THREADS / 32;
+    __shared__ float s_part[2][WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int blocks = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
     ptx::pdl_wait();
-    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    int turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const TX* x = static_cast<const TX*>(a.x) + row * a.x_ld;
         const TR* res = NORM && a.residual ? static_cast<const TR*>(a.residual) + row * a.res_ld : nullptr;
-        float rstd = 1.f;
-        if constexpr (NORM) {
-            float ss = 0.f;
-            for (int c = threadIdx.x; c < a.cols; c += ROW_ANY_THREADS) {
-                const float r = to_f<TX>(x[c]) + (res ? to_f<TR>(res[c]) : 0.f);
+        auto element = [&](int c) {
+            float r = to_f<TX>(x[c]);
+            if (res) r += to_f<TR>(res[c]);
+            return r;
+        };
+        float v[MB > 0 ? MB : 1][4];
+        float rstd = 1.f, ss = 0.f;
+        if constexpr (MB > 0) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = (i * WARPS + warp) * FP8_BLOCK + k * 32 + lane;
+                    v[i][k] = c < a.cols ? element(c) : 0.f;
+                }
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) ss = fmaf(v[i][k], v[i][k], ss);
+        } else if constexpr (NORM) {
+            for (int c = threadIdx.x; c < a.cols; c += THREADS) {
+                const float r = element(c);
                 ss = fmaf(r, r, ss);
             }
+        }
+        if constexpr (NORM) {
             ss = warp_sum(ss);
-            __syncthreads();
-            if (lane == 0) s_part[warp] = ss;
+            if (lane == 0) s_part[turn][warp] = ss;         // (two turns: a row's sums are read before the row after next is written)
             __syncthreads();
             ss = 0.f;
 #pragma unroll
-            for (int i = 0; i < ROW_ANY_THREADS / 32; ++i) ss += s_part[i];
+            for (int i = 0; i < WARPS; ++i) ss += s_part[turn][i];
             rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
         }
-        for (int b = warp; b < blocks; b += ROW_ANY_THREADS / 32) {
-            float v[4];
+        auto finish = [&](int b, float* u) {
             float amax = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int c = b * FP8_BLOCK + k * 32 + lane;
-                v[k] = 0.f;
                 if (c < a.cols) {
-                    v[k] = to_f<TX>(x[c]);
                     if constexpr (NORM) {
-                        if (res) v[k] += to_f<TR>(res[c]);
-                        if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(v[k]);
-                        v[k] = v[k] * rstd * (a.weight ? to_f<TX>(static_cast<const TX*>(a.weight)[c]) : 1.f);
-                        if (a.y) static_cast<TX*>(a.y)[row * a.y_ld + c] = from_f<TX>(v[k]);
+                        if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(u[k]);
+                        u[k] = u[k] * rstd * (a.weight ? to_f<TX>(static_cast<const TX*>(a.weight)[c]) : 1.f);
+                        if (a.y) static_cast<TX*>(a.y)[row * a.y_ld + c] = from_f<TX>(u[k]);
                     }
-                    amax = fmaxf(amax, fabsf(v[k]));
+                    amax = fmaxf(amax, fabsf(u[k]));
                 }
             }
             if (a.y8) {
@@ -217,19 +268,36 @@ row_blocks_any_kernel(RowArgs a) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int c = b * FP8_BLOCK + k * 32 + lane;
-                    if (c < a.cols) a.y8[row * a.y8_ld + c] = __nv_cvt_float_to_fp8(v[k] * inv, __NV_SATFINITE, __NV_E4M3);
+                    if (c < a.cols) a.y8[row * a.y8_ld + c] = __nv_cvt_float_to_fp8(u[k] * inv, __NV_SATFINITE, __NV_E4M3);
                 }
                 if (lane == 0) a.y8_scale[row * a.sc_ld + b] = amax / E4M3_MAX;
+            }
+        };
+        if constexpr (MB > 0) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+                if (i * WARPS + warp < blocks) finish(i * WARPS + warp, v[i]);
+        } else {
+            for (int b = warp; b < blocks; b += WARPS) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = b * FP8_BLOCK + k * 32 + lane;
+                    v[0][k] = c < a.cols ? element(c) : 0.f;
+                }
+                finish(b, v[0]);
             }
         }
     }
     ptx::pdl_trigger();
 }
 
+constexpr int ROW_CTAS = 8;                // CTAs per SM asked for: two rounds of what fits (6: 50.0 us, 12 and 16: 45.4 and 45.1, but 9.2
+                                           // and 10.6 against 8.7 us for 3997 x 1152)
+
 template <typename TX, typename TR, int W, int NV, bool NORM>
 cudaError_t launch_reg(const RowArgs& a, cudaStream_t st) {
     constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
-    const int grid = (int)min((a.rows + RPC - 1) / RPC, 1LL << 20);
+    const int grid = (int)min((a.rows + RPC - 1) / RPC, row_ahead<TX, TR, NORM> ? 148LL * ROW_CTAS : 1LL << 20);
     return ptx::launch_kernel(row_blocks_kernel<TX, TR, W, NV, NORM>, grid, THREADS, 0, st, true, a);
 }
 
@@ -255,12 +323,17 @@ cudaError_t launch_typed(const RowArgs& a, cudaStream_t st) {
                       ok(a.weight, 16, 1) && ok(a.y, a.y_ld, sizeof(TX)) &&
                       (!a.y8 || ((reinterpret_cast<uintptr_t>(a.y8) & 7) == 0 && a.y8_ld % 8 == 0));
     if (!fast) {
-        const int grid = (int)min(a.rows, 1LL << 20);
-        return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM>, grid, ROW_ANY_THREADS, 0, st, true, a);
+        const int grid = (int)min(a.rows, 1LL << 20), blocks = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
+        if (blocks <= 4) return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM, 128, 1>, grid, 128, 0, st, true, a);
+        if (blocks <= 8) return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM, 128, 2>, grid, 128, 0, st, true, a);
+        if (blocks <= 16) return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM, 128, 4>, grid, 128, 0, st, true, a);
+        if (blocks <= 32) return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM, 256, 4>, grid, 256, 0, st, true, a);
+        if (blocks <= 64) return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM, 256, 8>, grid, 256, 0, st, true, a);
+        return ptx::launch_kernel(row_blocks_any_kernel<TX, TR, NORM, 256, 0>, grid, 256, 0, st, true, a);
     }
-    // Warps per row: three vectors a lane where eight warps allow it (16380 x 1536, bf16 + fp32 residual to 8 bits: 47.1 us with two
-    // warps and three vectors, 56.7 with one and six, 48.0 with four and two, 62.9 with eight and one: more rows in flight
-    // against more lanes idle in the reductions); more warps when the rows alone would leave SMs idle.
+    // Warps per row: three vectors a lane where eight warps allow it (16380 x 1536, bf16 + fp32 residual to 8 bits, before CTAs
+    // stayed: 47.1 us with two warps and three vectors, 56.7 with one and six, 48.0 with four and two, 62.9 with eight and one: more
+    // rows in flight against more lanes idle in the reductions); more warps when the rows alone would leave SMs idle.
     int w = 1;
     while (w < ROW_MAX_W && (a.cols > 256 * w * 3 || (a.cols > 256 * w && a.rows * w < 148 * 4))) w *= 2;
     switch (w) {
