@@ -75,8 +75,8 @@ template <typename TX, typename TR, bool NORM> constexpr bool row_ahead = !NORM 
 
 // W warps hold one row, NV vectors of 8 columns per lane (cols <= 256 W NV, a multiple of 8).  CTAs stay and walk the rows: the
 // weights are fetched once, and the next row is requested before the present one is reduced.  (AHEAD; not with fp32 rows and
-// an fp32 residual, where its registers cost more warps than it gives: there a CTA takes one row, 4000 x 4608 in 45.9 us
-// against 51.5.)
+// an fp32 residual, where its registers cost more warps than it gives: there a CTA takes one row and fetches the weights late, 4000 x
+// 4608 in 47.1 us against 51.5.)
 template <typename TX, typename TR, int W, int NV, bool NORM>
 __global__ void __launch_bounds__(W < 4 ? 128 : 32 * W)
 row_blocks_kernel(RowArgs a) {
@@ -88,7 +88,7 @@ row_blocks_kernel(RowArgs a) {
     constexpr bool AHEAD = row_ahead<TX, TR, NORM>;
     const float inv_cols = 1.0f / (float)a.cols;
     ptx::pdl_wait();
-    Raw8<TX> x[NV], w[NORM ? NV : 1];
+    Raw8<TX> x[NV], w[NORM && AHEAD ? NV : 1];
     Raw8<TR> t[NORM ? NV : 1];
     auto request = [&](long long row) {
         const TX* px = static_cast<const TX*>(a.x) + row * a.x_ld + col0;
@@ -104,15 +104,13 @@ row_blocks_kernel(RowArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         x[i].set(0.f);
-        if constexpr (NORM) {
-            t[i].set(0.f);
-            w[i].set(1.f);
-        }
+        if constexpr (NORM) t[i].set(0.f);
+        if constexpr (NORM && AHEAD) w[i].set(1.f);
     }
     const long long step = (long long)gridDim.x * RPC;
     long long row0 = (long long)blockIdx.x * RPC;
     if (AHEAD && row0 + rc < a.rows) request(row0 + rc);
-    if constexpr (NORM)
+    if constexpr (NORM && AHEAD)
         if (a.weight)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
@@ -162,7 +160,12 @@ row_blocks_kernel(RowArgs a) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float g[8];
-                w[i].get(g);
+                if constexpr (AHEAD) w[i].get(g);
+                else {
+                    w[0].set(1.f);
+                    if (a.weight && col0 + i * W * 256 < a.cols) w[0].load(static_cast<const TX*>(a.weight) + col0 + i * W * 256);
+                    w[0].get(g);
+                }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * rstd * g[k];
             }
