@@ -874,7 +874,7 @@ fd_status fd_rope_axes(const fd_rope_spec* spec, const float* pos, int64_t token
         // rows of the output lie apart: heads inside a token's span, or tokens inside a head's
         const int64_t ts = r.out_token_stride, hs = r.out_head_stride, T = tokens, h = r.heads;
         const bool head_in = (h == 1 || hs >= head_dim) && (T <= 1 || ts >= (h - 1) * hs + head_dim);
-        const bool token_in = (T <= 1 || ts >= head_dim) && (h == 1 || hs >= (T - 1) * ts + head_dim);
+        const bool token_in = (T <= 1 || ts >= head_dim) && (h == 1 || (hs >= head_dim && (T <= 1 || (hs - head_dim) / ts >= T - 1)));
         if (!head_in && !token_in) return op_fail(FD_ERR_SHAPE, "%s: the output's rows overlap", who);
         if (r.in == r.out && ((T > 1 && r.in_token_stride != ts) || (h > 1 && r.in_head_stride != hs)))
             return op_fail(FD_ERR_SHAPE, "%s: in place needs equal strides", who);

@@ -159,3 +159,9 @@ def test_binding_refuses_cpu_tensors_and_wrong_types():
         with pytest.raises(fd.FlashDiffError) as e:
             call()
         assert e.value.status == fd.FD_ERR_INVALID_ARG
+
+
+def test_rope_axes_overlap_of_huge_strides():
+    big = 2 ** 40                                    # (tokens - 1) * stride is 2^64: the comparison must not wrap around
+    assert _rope(tokens=2 ** 24 + 1, sets=[dict(heads=65536, out_token_stride=big, out_head_stride=big)]) == fd.FD_ERR_SHAPE
+    assert "overlap" in _text()
