@@ -79,13 +79,15 @@ __device__ __forceinline__ void pass_regs(uint32_t* r) {
 }
 
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float rcp_approx(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // tanh-GELU as a sigmoid: 0.5 v (1 + tanh u) = v / (1 + exp(-2u)), accurate to a few fp32 roundings (the hardware tanh is
-// good to 2^-11 only, which the scale of an 8-bit output block would show).  Two values share one reciprocal; the exponent is
-// cut at 2^57 so that the product of the two denominators stays finite (the value is below 2^-53 of its argument there).  It
-// costs a tile about 3000 clk of instruction latency, not of the special-function unit: exponentials on the FMA pipe for
-// three of eight pairs made 16380 x 8960 x 1536 slower (300 us against 265), a reciprocal for every value made no difference.
+// good to 2^-11 only, which the scale of an 8-bit output block would show).  Two values share one reciprocal (one each: 274 us
+// against 258 for 16380 x 8960 x 1536), so the exponent is cut at 2^57 to keep the product of the two denominators finite, and the
+// factor v at -7.25, where the exponential reaches 2^55.9: the result is off by at most 1.1e-16 from there down.  A NaN stays
+// where it is: fminf keeps it out of the shared reciprocal.  The GELU costs a tile about 3000 clk of instruction latency, not of the
+// special-function unit: exponentials on the FMA pipe for three of eight pairs were slower.
 __device__ __forceinline__ void gelu_pair(float& v0, float& v1) {
     constexpr float C1 = -2.3022081985814995f, C2 = -0.10294323959957175f;      // -2 log2(e) sqrt(2 / pi) (1, 0.044715)
     const uint64_t v = attn::pair(v0, v1);
@@ -93,7 +95,7 @@ __device__ __forceinline__ void gelu_pair(float& v0, float& v1) {
     attn::unpair(mul2(v, attn::fma2(mul2(v, attn::pair(C2, C2)), v, attn::pair(C1, C1))), x0, x1);
     attn::unpair(attn::add2(attn::pair(attn::ex2(fminf(x0, 57.0f)), attn::ex2(fminf(x1, 57.0f))), attn::pair(1.0f, 1.0f)), d0, d1);
     const float r = rcp_approx(d0 * d1);
-    attn::unpair(mul2(v, mul2(attn::pair(r, r), attn::pair(d1, d0))), v0, v1);
+    attn::unpair(mul2(attn::pair(max_nan(v0, -7.25f), max_nan(v1, -7.25f)), mul2(attn::pair(r, r), attn::pair(d1, d0))), v0, v1);
 }
 
 // One warp's 32 rows x 128 columns of finished accumulators: bias, GELU, rounding, and the way out through the warp's two
@@ -187,6 +189,7 @@ __device__ __forceinline__ void gb_store(const GbArgs& g, const CUtensorMap* tm_
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
             uint8_t* tile = stage + (h & 1) * EPI_STAGE_BYTES_PER_WARP;
+            if (col0 + h * 32 >= g.n) break;                 // (the wait below counts stores: none may be left out before it)
             if (h >= 2) gb_stage_wait<1>(lane);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
@@ -250,14 +253,16 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
         attn::reg_dec<GB_REGS_LOAD>();
         if (warp == 0) {
             // (as for the products below: a converged warp with one elected lane; from a diverged lane a stage took 580 clk)
-            uint32_t it = 0, s = 0, ph = 0;
+            // Here and in the other roles a lane whose wait ran out does nothing more, but no lane leaves a loop before the others.
+            uint32_t issued = 0, s = 0, ph = 0;
             bool ok = true;
-            for (uint32_t tile = unit; tile < total && ok; tile += n_units) {
+            for (uint32_t tile = unit; tile < total; tile += n_units) {
                 const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
                 const int y_a = (m * CTAS + (int)rank) * GB_M, y_w = n * GB_N + (int)rank * Cfg::B_ROWS;
-                for (int kb = 0; kb < k_blocks; ++kb, ++it) {
-                    if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-                    if (elect_one()) {
+                for (int kb = 0; kb < k_blocks; ++kb) {
+                    ok = ok && mbar_wait(&empty[s], ph ^ 1, abort_flag);
+                    issued += ok;
+                    if (elect_one() && ok) {
                         if constexpr (PAIR) {
                             const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);  // the first CTA's barrier counts both halves
                             if (rank == 0) mbar_expect_tx(&full[s], 2 * Cfg::STAGE_BYTES);
@@ -274,9 +279,9 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
                 }
             }
             if (!ok) {
-                if (lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+                gb_report(g.status, FD_ERR_TIMEOUT);
                 int seen = 0;                // the copies still in flight land before the CTA leaves (a bounded wait each)
-                for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && rank == 0; ++j) mbar_wait(&full[j % STAGES], (j / STAGES) & 1, &seen);
+                for (uint32_t j = issued > STAGES ? issued - STAGES : 0; j < issued && rank == 0; ++j) mbar_wait(&full[j % STAGES], (j / STAGES) & 1, &seen);
             }
         } else if ((warp & 1) && rank == 0) {
             // Two issuing warps, one per TMEM buffer: the issue of a product waits for the tensor core to take it, so a single
@@ -288,14 +293,13 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             const uint32_t d = tmem_base + buf * GB_N;
             const uint32_t blocks = ((total - unit + n_units - 1) / n_units) * (uint32_t)k_blocks;     // of all this CTA's tiles
             bool ok = true;
-            for (uint32_t it = buf; it < blocks && ok; it += 2) {
+            for (uint32_t it = buf; it < blocks; it += 2) {
                 const int s = it % STAGES;
-                ok = mbar_wait(&full[s], (it / STAGES) & 1, abort_flag) && mbar_wait(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag);
-                if (!ok) break;
+                ok = ok && mbar_wait(&full[s], (it / STAGES) & 1, abort_flag) && mbar_wait(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag);
                 tc_fence_after();
                 const uint64_t da = smem_desc(smem_u32(sA + s * GB_A_BYTES), 16, 1024, SWZ_128B);
                 const uint64_t db = smem_desc(smem_u32(sB + s * Cfg::B_BYTES), 16, 1024, SWZ_128B);
-                if (elect_one()) {
+                if (elect_one() && ok) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         if constexpr (PAIR) mma_f8_ss_pair(d, da + 2 * k, db + 2 * k, idesc, k != 0);
@@ -307,7 +311,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
                 }
                 __syncwarp();
             }
-            if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+            if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
         } else if (warp == 2) {
             // Scales of this CTA's rows and of the tile's two weight blocks, GB_AHEAD blocks ahead of their use; rows behind m and
             // column blocks behind n take the last valid ones (their results are not stored).  The arrival on tfull for a block
@@ -344,15 +348,15 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             rows_of();
             for (int i = 0; i < GB_AHEAD; ++i) fetch();
             bool ok = true;
-            for (uint32_t it = 0; it < blocks && ok; ++it) {
-                if (it >= 2) ok = mbar_wait(&tfull[it & 1], ((it >> 1) & 1) ^ 1, abort_flag);
+            for (uint32_t it = 0; it < blocks; ++it) {
+                if (it >= 2) ok = ok && mbar_wait(&tfull[it & 1], ((it >> 1) & 1) ^ 1, abort_flag);
                 copy_async_wait<GB_AHEAD - 1>();             // this block's scales have landed
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&tfull[it & 1]);
                 fetch();
             }
             copy_async_wait<0>();
-            if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+            if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
         }
     } else {
         attn::reg_inc<GB_REGS_EPI>();
@@ -366,7 +370,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
         const uint32_t row_scale = smem_u32(s_scale + quad * 32 + lane), col_scale = smem_u32(s_scale + GB_M + half);
         uint32_t entry = 0, parity = 0;
         bool ok = true;
-        for (uint32_t tile = unit; tile < total && ok; tile += n_units) {
+        for (uint32_t tile = unit; tile < total; tile += n_units) {
             const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
             const int row_base = (m * CTAS + (int)rank) * GB_M + quad * 32, col0 = n * GB_N + half * 128;
             uint32_t b[4] = {0u, 0u, 0u, 0u};                // bias of columns lane, lane + 32, ...: raw bits, first looked at when the tile is done
@@ -386,7 +390,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             for (int i = 0; i < 128; ++i) acc[i] = 0.f;
 #pragma unroll 1
             for (int kb = 0; kb < k_blocks; ++kb) {
-                if (!mbar_try_wait_addr(full_bar, parity)) ok = mbar_wait_addr(full_bar, parity, abort_flag) && ok;
+                if (!mbar_try_wait_addr(full_bar, parity)) ok = ok && mbar_wait_addr(full_bar, parity, abort_flag);
                 const float s = load_shared(row_scale + entry) * load_shared(col_scale + entry);
                 tc_fence_after();
 #pragma unroll
@@ -412,10 +416,10 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
                 t_row ^= GB_N;
                 entry = entry + GB_ENTRY * 4 == GB_RING * GB_ENTRY * 4 ? 0 : entry + GB_ENTRY * 4;
             }
-            if (ok && row_base < g.m && col0 < g.n) gb_store<OUT, GELU>(g, &tm_o, acc, b, stage, lane, row_base, col0);
+            if (__all_sync(0xffffffffu, ok) && row_base < g.m && col0 < g.n) gb_store<OUT, GELU>(g, &tm_o, acc, b, stage, lane, row_base, col0);
         }
         if (lane == 0) bulk_wait_all();                          // this warp's stores have landed
-        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+        if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
     }
 
     tc_fence_before();
@@ -522,9 +526,9 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     const int k_blocks = (g.k + GB_K - 1) / GB_K;
     const int kb0 = (int)((long long)k_blocks * rank / splits), blocks = (int)((long long)k_blocks * (rank + 1) / splits) - kb0;
 
-    auto load_stage = [&](int it) {          // whole warp 0
+    auto load_stage = [&](int it, bool ok) { // whole warp 0
         const int s = it % GS_STAGES;
-        if (elect_one()) {
+        if (elect_one() && ok) {
             mbar_expect_tx(&full[s], a_rows * GB_K + GS_N * GB_K);
             tma_load_2d(sA + s * GB_A_BYTES, &tm_a, (kb0 + it) * GB_K, m0, &full[s]);
             tma_load_2d(sB + s * GS_N * GB_K, &tm_w, (kb0 + it) * GB_K, n0, &full[s]);
@@ -553,7 +557,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
         }
         __syncwarp();
         pdl_wait();
-        for (int it = 0; it < min(blocks, GS_STAGES); ++it) load_stage(it);
+        for (int it = 0; it < min(blocks, GS_STAGES); ++it) load_stage(it, true);
     } else if (warp == 1) {
         tmem_alloc(tmem_slot, GS_BUFS * GS_N);
         tmem_relinquish();
@@ -572,28 +576,28 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
 
     if (warp == 0) {
         bool ok = true;
-        int it = min(blocks, GS_STAGES);
-        for (; it < blocks; ++it) {
-            if (!mbar_wait(&empty[it % GS_STAGES], ((it / GS_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
-            load_stage(it);
+        int issued = min(blocks, GS_STAGES);
+        for (int it = issued; it < blocks; ++it) {
+            ok = ok && mbar_wait(&empty[it % GS_STAGES], ((it / GS_STAGES) & 1) ^ 1, abort_flag);
+            issued += ok;
+            load_stage(it, ok);
         }
         if (!ok) {
-            if (lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+            gb_report(g.status, FD_ERR_TIMEOUT);
             int seen = 0;                    // the copies still in flight land before the CTA leaves (a bounded wait each)
-            for (int j = max(0, it - GS_STAGES); j < it; ++j) mbar_wait(&full[j % GS_STAGES], (j / GS_STAGES) & 1, &seen);
+            for (int j = max(0, issued - GS_STAGES); j < issued; ++j) mbar_wait(&full[j % GS_STAGES], (j / GS_STAGES) & 1, &seen);
         }
     } else if (warp == 1 || warp == 3) {
         constexpr uint32_t idesc = idesc_e4m3(GB_M, GS_N);
         bool ok = true;
-        for (int it = warp >> 1; it < blocks && ok; it += 2) {
+        for (int it = warp >> 1; it < blocks; it += 2) {
             const int s = it % GS_STAGES, buf = it % GS_BUFS;
             const uint32_t d = tmem_base + buf * GS_N;
-            ok = mbar_wait(&full[s], (it / GS_STAGES) & 1, abort_flag) && mbar_wait(&tempty[buf], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
-            if (!ok) break;
+            ok = ok && mbar_wait(&full[s], (it / GS_STAGES) & 1, abort_flag) && mbar_wait(&tempty[buf], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
             tc_fence_after();
             const uint64_t da = smem_desc(smem_u32(sA + s * GB_A_BYTES), 16, 1024, SWZ_128B);
             const uint64_t db = smem_desc(smem_u32(sB + s * GS_N * GB_K), 16, 1024, SWZ_128B);
-            if (elect_one()) {
+            if (elect_one() && ok) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mma_f8_ss(d, da + 2 * k, db + 2 * k, idesc, k != 0);
                 mma_commit(&tfull[buf]);
@@ -601,18 +605,18 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
             }
             __syncwarp();
         }
-        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+        if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
     } else if (warp == 2) {
         bool ok = true;
-        for (int it = 0; it < blocks && ok; ++it) {
-            if (it >= GS_BUFS) ok = mbar_wait(&tfull[it % GS_BUFS], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
+        for (int it = 0; it < blocks; ++it) {
+            if (it >= GS_BUFS) ok = ok && mbar_wait(&tfull[it % GS_BUFS], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
             copy_async_wait<GB_AHEAD - 1>();
             __syncwarp();
             if (lane == 0) mbar_arrive(&tfull[it % GS_BUFS]);
             fetch(it + GB_AHEAD);
         }
         copy_async_wait<0>();
-        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+        if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
     } else {
         const int quad = warp & 3, half = (warp - 4) >> 2;      // TMEM lane quadrant, 64-column half
         const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + half * 64;
@@ -624,9 +628,9 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
 #pragma unroll
         for (int i = 0; i < 64; ++i) acc[i] = 0.f;
 #pragma unroll 1
-        for (int it = 0; it < blocks && ok; ++it) {
+        for (int it = 0; it < blocks; ++it) {
             const uint32_t buf = it % GS_BUFS, parity = (it / GS_BUFS) & 1;
-            if (!mbar_try_wait_addr(full_bar + 8 * buf, parity)) ok = mbar_wait_addr(full_bar + 8 * buf, parity, abort_flag);
+            if (!mbar_try_wait_addr(full_bar + 8 * buf, parity)) ok = ok && mbar_wait_addr(full_bar + 8 * buf, parity, abort_flag);
             const float s = load_shared(row_scale + entry) * load_shared(col_scale + entry);
             tc_fence_after();
             uint32_t r[64];
@@ -642,7 +646,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
             for (int i = 0; i < 64; ++i) acc[i] = fmaf(__uint_as_float(r[i]), s, acc[i]);
             entry = entry + GB_ENTRY * 4 == GB_RING * GB_ENTRY * 4 ? 0 : entry + GB_ENTRY * 4;
         }
-        if (!ok && lane == 0) gb_report(g.status, FD_ERR_TIMEOUT);
+        if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
         const int row = quad * 32 + lane;
         if (m0 + row < g.m) {
 #pragma unroll

@@ -187,3 +187,90 @@ def test_graph_replay(m):
     torch.cuda.synchronize()
     _check(out, sc, *ref.matmul(a8, a_s, w8, w_s), True)
     _check(y, None, *ref.matmul(out, sc, w2, w2_s), False)
+
+
+@pytest.mark.parametrize("n", [4, 36, 64, 1060, 1088, 1120])
+@pytest.mark.parametrize("m", [9400, 20000])
+def test_few_last_columns_in_fp32(m, n):
+    """Rows leave through two staging tiles in turn: columns of the last block that are not there must not let a tile be written
+    again while its store is under way.  Whole numbers, so every sum is exact."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    a, w = (torch.randint(-3, 4, (r, 128), generator=g, device="cuda").float() for r in (m, n))
+    a_s, w_s = torch.ones(m, 1, device="cuda"), torch.ones(ref.blocks(n), 1, device="cuda")
+    want = a @ w.t()                                           # below 2^11: exact in any order
+    a8, w8 = a.to(torch.float8_e4m3fn), w.to(torch.float8_e4m3fn)
+    for _ in range(4):
+        out = torch.full((m, n), float("nan"), device="cuda")
+        fd.fd_matmul_fp8_blocks(a8, a_s, w8, w_s, out)
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("m", [5, 200, 9400])
+@pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
+def test_gelu_far_out(m, out):
+    """Large arguments of either sign, an infinity and a NaN next to ordinary values: large ones pass, very negative ones vanish, the
+    others are as they would be alone.  One code per row carries the value; weights of one."""
+    n, k = 1024, 16
+    a8 = torch.zeros(m, k, dtype=torch.uint8, device="cuda")
+    a8[:, 0] = 0x38                                            # 1.0
+    w8 = torch.zeros(n, k, dtype=torch.uint8, device="cuda")
+    ones = torch.ones(m, 1, device="cuda"), torch.ones(n // 128, 1, device="cuda")
+    bias = torch.zeros(n, device="cuda")
+    bias[:128:2] = -torch.logspace(0, 37, 64, device="cuda")   # -1 ... -1e37 between zeros
+    bias[128:256:2] = torch.logspace(-3, 37, 64, device="cuda")
+    bias[256:384] = torch.linspace(-12, 12, 128, device="cuda")
+    bias[385], bias[387], bias[513] = float("nan"), float("inf"), float("-inf")
+    bias[384:640:2] = 0.75
+    got, sc, _ = _outputs(m, n, out)
+    fd.fd_matmul_fp8_blocks(a8, ones[0], w8, ones[1], got, bias=bias, gelu=True, out_scale=sc)
+    v = bias.double()
+    g, err = ref.gelu(v, torch.zeros_like(v))
+    g = torch.where(v < -12, torch.zeros_like(g), g)           # (the 64-bit form is 0 * inf for -1e37 too)
+    fine = torch.isfinite(v)                                   # (elsewhere the bound's own formula gives NaN, too)
+    err = torch.where(fine & (v >= -12), err, torch.zeros_like(g)) + 1.2e-16    # 7.25 * 2^-55.9: the cut of very negative arguments
+    g, err, fine = g.expand(m, n), err.expand(m, n), fine.expand(m, n)
+    if sc is not None:
+        assert bool(torch.isinf(sc[:, 3]).all())                # the block with the infinity
+        spoilt = torch.zeros_like(fine)
+        spoilt[:, 384:512] = True
+        assert bool((got.view(torch.uint8)[:, 385] & 0x7F == 0x7F).all() and (got.view(torch.uint8)[:, 387] & 0x7F == 0x7F).all())
+        clean = torch.where(fine & ~spoilt, g, torch.zeros_like(g))
+        codes = torch.where(spoilt, torch.zeros((), dtype=torch.uint8, device="cuda"), got.view(torch.uint8))
+        scale = torch.where(torch.isinf(sc), torch.full_like(sc, 2.0 ** -100 / 448), sc)
+        ref.check_codes(codes, scale, clean, absolute=err)
+        return
+    assert bool(got[:, 385].isnan().all()) and bool((got[:, 387] == float("inf")).all())
+    assert bool((got[:, 513].double().abs() <= 1.2e-16).all())
+    tol = err + ref.HALF_STEP[got.dtype] * (g.abs() + err)
+    bad = fine & ~((got.double() - g).abs() <= tol)
+    assert not bool(bad.any()), bad.nonzero()[:4]
+
+
+_FIRST_CAPTURED = """
+import torch, paper_2607_12121_b200 as fd
+m, n, k = {size}
+a8, w8 = torch.full((m, k), 0x38, dtype=torch.uint8, device="cuda"), torch.full((n, k), 0x38, dtype=torch.uint8, device="cuda")
+a_s, w_s = torch.ones(m, (k + 127) // 128, device="cuda"), torch.ones((n + 127) // 128, (k + 127) // 128, device="cuda")
+out, x, y8 = torch.zeros(m, n, device="cuda"), torch.ones(m, k, device="cuda"), torch.zeros(m, k, dtype=torch.uint8, device="cuda")
+pos, q = torch.zeros(m, 1, device="cuda"), torch.ones(m, 2, 64, device="cuda")
+spec, s = fd.make_rope_axes([64]), torch.zeros(m, (k + 127) // 128, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    fd.fd_matmul_fp8_blocks(a8, a_s, w8, w_s, out)
+    fd.fd_add_rmsnorm(x, None, 0.0, y8=y8, y8_scale=s)
+    fd.fd_rope_axes(spec, pos, q, q)
+g.replay()
+torch.cuda.synchronize()
+assert bool((out == k).all()) and bool((y8 == 0x7E).all()) and bool((q == 1).all())
+"""
+
+
+@pytest.mark.parametrize("size", [(4, 256, 128), (9400, 1024, 128)])
+def test_first_call_of_a_process_may_be_captured(size):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _FIRST_CAPTURED.format(size=size)], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
