@@ -94,3 +94,49 @@ def test_tables_feed_the_step():
         ys.append(host(buf.y))
         fd.fd_destroy(ctx)
     assert (ys[0] == ys[1]).all() and (ys[0] != ys[2]).any()
+
+
+def test_context_keys_and_values_feed_the_step():
+    """The context's states become the keys and values of every block's cross-attention (norm to 8 bits, then a product per block,
+    request and half, straight into the step's tensor), and the step behind them on the same stream reads them: bit for bit what
+    it gives with a copy made after everything has finished, and not what it gives with others."""
+    import numpy as np
+
+    import gen
+    from harness import StepBuffers, dev, gpu_step, host, make_ctx, tdtype
+    wl = gen.workload("audio_tc")
+    labels, n_ctx, H = gen.uniform_labels(wl), 37, wl.H
+    w, inp, dt = gen.block_weights(wl, 0), gen.step_inputs(wl, 0, labels), tdtype(wl)
+    cross = {k: dev(v, dt) for k, v in gen.cross_attention(wl, 3, n_ctx).items()}
+    g = torch.Generator(device="cuda").manual_seed(5)
+    states = torch.randn(wl.B * n_ctx, H, generator=g, device="cuda").bfloat16()
+    norm = (1 + 0.1 * torch.randn(H, generator=g, device="cuda")).bfloat16()
+    weights = [[ref.quantise(0.05 * torch.randn(H, H, generator=g, device="cuda"), True) for _ in range(2)] for _ in range(wl.L)]
+    c8, c_s = torch.empty(wl.B * n_ctx, H, dtype=torch.uint8, device="cuda"), torch.empty(wl.B * n_ctx, ref.blocks(H), device="cuda")
+    made_kv, other = cross["ctx_kv"], cross["ctx_kv"].clone()
+    x, cond, lab, ones = dev(inp["x_cur"], dt), dev(inp["cond"], dt), dev(labels), dev(np.ones((wl.B, wl.R), np.uint8))
+    torch.cuda.synchronize()
+    ys = []
+    for made in (True, False, None):
+        if made is False:
+            cross = dict(cross, ctx_kv=cross["ctx_kv"].clone())
+        if made is None:
+            cross = dict(cross, ctx_kv=other)
+        ctx, buf = make_ctx(wl, w, engine=fd.FD_ENGINE_TC), StepBuffers(wl, wl.L)
+        fd.fd_set_cross_attention(ctx, cross)
+        if made:
+            fd.fd_add_rmsnorm(states, norm, 1e-6, y8=c8, y8_scale=c_s)
+            for layer in range(wl.L):
+                for b in range(wl.B):
+                    at = slice(b * n_ctx, (b + 1) * n_ctx)
+                    for half in range(2):
+                        fd.fd_matmul_fp8_blocks(c8[at], c_s[at], *weights[layer][half], cross["ctx_kv"][layer, b, half])
+        gpu_step(ctx, wl, x, cond, lab, ones, buf)
+        ys.append(host(buf.y))
+        fd.fd_destroy(ctx)
+    for layer in range(wl.L):
+        for half in range(2):
+            v, err = ref.matmul(c8, c_s, *weights[layer][half])
+            got = made_kv[layer, :, half].reshape(wl.B * n_ctx, H)
+            assert bool(((got.double() - v).abs() <= err + ref.HALF_STEP[got.dtype] * (v.abs() + err)).all())
+    assert (ys[0] == ys[1]).all() and (ys[0] != ys[2]).any()
