@@ -7,6 +7,7 @@ in Python.  Importing this module fails loudly if the shared library has not bee
 from __future__ import annotations
 
 import ctypes
+import struct
 import os
 from typing import Dict, Optional
 
@@ -406,7 +407,24 @@ def fd_set_fp8_operands(ctx: Context, fp8: Optional[Dict[str, "object"]], text_s
 
 _TYPE_CODES = {torch.bfloat16: FD_BF16, torch.float32: FD_F32}
 _CODES_TYPES = (torch.uint8, torch.float8_e4m3fn)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # (a device tensor is at hand: CUDA is up)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+# The two argument structs as bytes in their C layout (a ctypes structure takes five times as long to fill).
+_pack_rmsnorm = struct.Struct("7P6q2if4x").pack
+_pack_matmul = struct.Struct("8P6q3i4x").pack
+assert struct.calcsize("7P6q2if4x") == ctypes.sizeof(FdRmsnormArgs) and struct.calcsize("8P6q3i4x") == ctypes.sizeof(FdMatmulFp8Args)
+
+
+def _packed(name: str, *argtypes):
+    fn = lib[name]                                   # a function object of its own: the prototype in lib takes the structure
+    fn.argtypes, fn.restype = [ctypes.c_char_p, *argtypes, ctypes.c_void_p], ctypes.c_int
+    return fn
+
+
+_call_rmsnorm = _packed("fd_add_rmsnorm", ctypes.c_int64, ctypes.c_int)
+_call_matmul = _packed("fd_matmul_fp8_blocks", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 
 
 def _op_fail(text: str):
@@ -420,36 +438,36 @@ def _type_code(t, name: str) -> int:
     return code
 
 
-def _rows(t, name: str, rows: int, cols: int, device: int) -> int:
-    """Row stride of the 2-D tensor ``t`` of the wanted shape on the device, columns contiguous."""
+def _rows(t, name: str, shape, device: int) -> int:
+    """Row stride of the 2-D tensor ``t`` of the wanted shape (rows, columns) on the device, columns contiguous."""
+    if t.shape != shape or t.get_device() != device:
+        _op_fail("%s must be %s on device %d, not %s on %s" % (name, list(shape), device, list(t.shape), t.device))
+    rows, cols = shape
+    if t.is_contiguous():
+        return cols
     stride = t.stride()
-    if len(stride) != 2 or t.get_device() != device:
-        _op_fail("%s must be [%d, %d] on device %d, not %s on %s" % (name, rows, cols, device, list(t.shape), t.device))
-    r, c = t.shape
-    if r != rows or c != cols:
-        _op_fail("%s must be [%d, %d], not %s" % (name, rows, cols, list(t.shape)))
     if stride[1] != 1 and cols > 1:
         _op_fail("%s must have contiguous columns" % name)
     return stride[0] if rows > 1 else max(stride[0], cols)
 
 
-def _codes(t, name: str, rows: int, cols: int, device: int) -> int:
+def _codes(t, name: str, shape, device: int) -> int:
     if t.dtype not in _CODES_TYPES:
         _op_fail("%s must hold E4M3 codes (uint8 or float8_e4m3fn), not %s" % (name, t.dtype))
-    return _rows(t, name, rows, cols, device)
+    return _rows(t, name, shape, device)
 
 
-def _scales(t, name: str, rows: int, cols: int, device: int) -> int:
+def _scales(t, name: str, shape, device: int) -> int:
     if t.dtype is not torch.float32:
         _op_fail("%s must be float32, not %s" % (name, t.dtype))
-    return _rows(t, name, rows, cols, device)
+    return _rows(t, name, shape, device)
 
 
 def _op_call(device: int, stream, fn, *args) -> None:
     """The call with the tensors' device current, on the given stream or that device's current one."""
     if device < 0:
         _op_fail("device tensors wanted")
-    if torch.cuda.current_device() == device:
+    if _current_device() == device:
         status = fn(*args, (_raw_stream(device) if stream is None else stream.cuda_stream) or None)
     else:
         with torch.cuda.device(device):
@@ -503,7 +521,7 @@ def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) ->
     """The rotary tables [tokens, head_dim / 2] float32 that fd_set_block_variants takes, from positions [tokens, n_axes]."""
     tokens, device, half = _rope_pos(spec, pos), pos.get_device(), cos_out.shape[-1]
     for t, name in ((cos_out, "cos_out"), (sin_out, "sin_out")):
-        if _scales(t, name, tokens, half, device) != half:
+        if _scales(t, name, (tokens, half), device) != half:
             _op_fail("%s must be contiguous" % name)
     if tokens:
         _op_call(device, stream, lib.fd_rope_axes_tables, spec, pos.data_ptr(), tokens, 2 * half, cos_out.data_ptr(), sin_out.data_ptr())
@@ -512,40 +530,45 @@ def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) ->
 def fd_add_rmsnorm(x, weight, eps: float, residual=None, residual_out=None, y=None, y8=None, y8_scale=None, stream=None) -> None:
     """r = x + residual (kept in residual_out if given), y = r / sqrt(mean(r^2) + eps) * weight; outputs y in x's type and / or
     y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)].  residual_out may be residual, y may be x."""
-    (rows, cols), device = x.shape, x.get_device()
-    x_stride = _rows(x, "x", rows, cols, device)
-    w = r = ro = py = p8 = ps = None
-    r_stride = ro_stride = y_stride = y8_stride = s_stride = r_type = 0
+    shape, device = x.shape, x.get_device()
+    x_stride = _rows(x, "x", shape, device)
+    rows, cols = shape
+    w = r = ro = py = p8 = ps = r_stride = ro_stride = y_stride = y8_stride = s_stride = r_type = 0
     if weight is not None:
-        if weight.dtype is not x.dtype or weight.get_device() != device or weight.shape != (cols,) or (cols > 1 and weight.stride(0) != 1):
+        if weight.dtype is not x.dtype or weight.get_device() != device or weight.shape != (cols,) or not weight.is_contiguous():
             _op_fail("weight must be a contiguous [%d] tensor of x's type and device" % cols)
         w = weight.data_ptr()
     if residual is not None:
-        r_type, r, r_stride = _type_code(residual, "residual"), residual.data_ptr(), _rows(residual, "residual", rows, cols, device)
+        r_type, r, r_stride = _type_code(residual, "residual"), residual.data_ptr(), _rows(residual, "residual", shape, device)
     if residual_out is not None:
-        if residual is not None and residual.dtype is not residual_out.dtype:
-            _op_fail("residual and residual_out must share one type")
-        r_type, ro = _type_code(residual_out, "residual_out"), residual_out.data_ptr()
-        ro_stride = r_stride if residual_out is residual else _rows(residual_out, "residual_out", rows, cols, device)
+        if residual_out is residual:
+            ro, ro_stride = r, r_stride
+        else:
+            if residual is not None and residual.dtype is not residual_out.dtype:
+                _op_fail("residual and residual_out must share one type")
+            r_type, ro, ro_stride = _type_code(residual_out, "residual_out"), residual_out.data_ptr(), _rows(residual_out, "residual_out", shape, device)
     if y is not None:
         if y.dtype is not x.dtype:
             _op_fail("y must have x's type")
-        py, y_stride = y.data_ptr(), _rows(y, "y", rows, cols, device)
+        py, y_stride = y.data_ptr(), _rows(y, "y", shape, device)
     if y8 is not None:
-        p8, y8_stride = y8.data_ptr(), _codes(y8, "y8", rows, cols, device)
+        p8, y8_stride = y8.data_ptr(), _codes(y8, "y8", shape, device)
     if y8_scale is not None:
-        ps, s_stride = y8_scale.data_ptr(), _scales(y8_scale, "y8_scale", rows, (cols + 127) // 128, device)
+        ps, s_stride = y8_scale.data_ptr(), _scales(y8_scale, "y8_scale", (rows, (cols + 127) // 128), device)
+    if not 0.0 <= eps < 3.0e38:
+        _op_fail("eps must be non-negative and finite")
     if rows:
-        _op_call(device, stream, lib.fd_add_rmsnorm,
-                 FdRmsnormArgs(x.data_ptr(), r, ro, w, py, p8, ps, x_stride, r_stride, ro_stride, y_stride, y8_stride, s_stride,
-                               _type_code(x, "x"), r_type, eps), rows, cols)
+        _op_call(device, stream, _call_rmsnorm, _pack_rmsnorm(x.data_ptr(), r, ro, w, py, p8, ps, x_stride, r_stride, ro_stride, y_stride, y8_stride,
+                                                              s_stride, _type_code(x, "x"), r_type, eps), rows, cols)
 
 
 def fd_quantize_fp8_blocks(x, y8, y8_scale, stream=None) -> None:
     """E4M3 codes y8 and scales y8_scale [rows, ceil(cols / 128)] of x [rows, cols] (float32 or bfloat16)."""
-    (rows, cols), device = x.shape, x.get_device()
-    args = (x.data_ptr(), _rows(x, "x", rows, cols, device), _type_code(x, "x"), rows, cols, y8.data_ptr(),
-            _codes(y8, "y8", rows, cols, device), y8_scale.data_ptr(), _scales(y8_scale, "y8_scale", rows, (cols + 127) // 128, device))
+    shape, device = x.shape, x.get_device()
+    x_stride = _rows(x, "x", shape, device)
+    rows, cols = shape
+    args = (x.data_ptr(), x_stride, _type_code(x, "x"), rows, cols, y8.data_ptr(), _codes(y8, "y8", shape, device), y8_scale.data_ptr(),
+            _scales(y8_scale, "y8_scale", (rows, (cols + 127) // 128), device))
     if rows:
         _op_call(device, stream, lib.fd_quantize_fp8_blocks, *args)
 
@@ -555,17 +578,18 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
     """out [m, n] = sum over the 128-blocks of k of a_scale * w_scale * (a8 w8^T) + bias, then tanh-GELU if asked.  a8 [m, k],
     w8 [n, k]: E4M3 codes; a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] float32; out float32, bfloat16,
     or codes with out_scale [m, ceil(n / 128)]; status_out: optional int32 device scalar."""
-    (m, k), n, device = a8.shape, w8.shape[0], a8.get_device()
+    a_shape, w_shape, device = a8.shape, w8.shape, a8.get_device()
+    a_stride = _codes(a8, "a8", a_shape, device)
+    (m, k), n = a_shape, w_shape[0]
+    w_stride = _codes(w8, "w8", (n, k), device)
     kb, nb = (k + 127) // 128, (n + 127) // 128
-    a_stride, w_stride = _codes(a8, "a8", m, k, device), _codes(w8, "w8", n, k, device)
     if m <= 1:                                          # the stride of a single row is free: round it up to what is asked for
         a_stride = (a_stride + 15) // 16 * 16
     if n <= 1:
         w_stride = (w_stride + 15) // 16 * 16
-    p_bias = p_scale = p_status = None
-    bias_type = s_stride = 0
+    p_bias = p_scale = p_status = bias_type = s_stride = 0
     if bias is not None:
-        if bias.get_device() != device or bias.shape != (n,) or (n > 1 and bias.stride(0) != 1):
+        if bias.get_device() != device or bias.shape != (n,) or not bias.is_contiguous():
             _op_fail("bias must be a contiguous [%d] tensor on the operands' device" % n)
         p_bias, bias_type = bias.data_ptr(), _type_code(bias, "bias")
     if out.dtype in _CODES_TYPES:
@@ -575,16 +599,16 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
     else:
         out_type = _type_code(out, "out")
     if out_scale is not None:
-        p_scale, s_stride = out_scale.data_ptr(), _scales(out_scale, "out_scale", m, nb, device)
+        p_scale, s_stride = out_scale.data_ptr(), _scales(out_scale, "out_scale", (m, nb), device)
     if status_out is not None:
         if status_out.dtype is not torch.int32 or status_out.get_device() != device or status_out.numel() < 1:
             _op_fail("status_out must be an int32 tensor on the operands' device")
         p_status = status_out.data_ptr()
-    args = FdMatmulFp8Args(a8.data_ptr(), a_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), p_bias, out.data_ptr(), p_scale, p_status,
-                           a_stride, _scales(a_scale, "a_scale", m, kb, device), w_stride, _scales(w_scale, "w_scale", nb, kb, device),
-                           _rows(out, "out", m, n, device), s_stride, bias_type, out_type, 1 if gelu else 0)
+    args = _pack_matmul(a8.data_ptr(), a_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), p_bias, out.data_ptr(), p_scale, p_status,
+                        a_stride, _scales(a_scale, "a_scale", (m, kb), device), w_stride, _scales(w_scale, "w_scale", (nb, kb), device),
+                        _rows(out, "out", (m, n), device), s_stride, bias_type, out_type, 1 if gelu else 0)
     if m:
-        _op_call(device, stream, lib.fd_matmul_fp8_blocks, args, m, n, k)
+        _op_call(device, stream, _call_matmul, args, m, n, k)
 
 
 def fd_sched_pack(load, cost, home):
