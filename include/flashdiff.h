@@ -423,7 +423,7 @@ fd_status fd_rope_axes_tables(const fd_rope_spec* spec, const float* pos, int64_
  *   residual, residual_out receives x);  weight [cols] of x_dtype or NULL (ones);  eps >= 0;
  *   y [rows, cols] of x_dtype or NULL;  y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)] f32, or both NULL; at
  *   least one of y, y8 is given.  residual_out may be residual, y may be x (same strides).
- * fd_quantize_fp8_blocks: the block form of a tensor as it is (an attention output, a weight's rows).
+ * fd_quantize_fp8_blocks: the block form of a tensor as it is (an attention output on its way into a projection).
  * Any width, any row stride of at least the width; 16-byte aligned rows of a multiple of 8 columns take the fast path.
  */
 typedef struct {
@@ -450,7 +450,8 @@ fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, i
  * once to out_dtype.  FD_E4M3 writes codes with a scale per 128 columns in out_scale [m, ceil(n / 128)], by the rule above:
  * the a8 / a_scale of the next product.
  *   a8 [m, k], w8 [n, k]: codes, k contiguous; base addresses 16-byte aligned, row strides multiples of 16 bytes
- *   a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] f32 (columns contiguous); the product of an a_scale
+ *   a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] f32 (columns contiguous): a scale for a row's 128
+ *   values of k on the left, for 128 x 128 weights on the right (quantised once by the caller); the product of an a_scale
  *   and a w_scale has to be finite
  *   bias [n] of bias_dtype (FD_F32 / FD_BF16) or NULL;  out [m, n], columns contiguous
  * Any m >= 0, n >= 1, k >= 1.

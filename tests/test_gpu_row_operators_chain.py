@@ -140,3 +140,47 @@ def test_context_keys_and_values_feed_the_step():
             got = made_kv[layer, :, half].reshape(wl.B * n_ctx, H)
             assert bool(((got.double() - v).abs() <= err + ref.HALF_STEP[got.dtype] * (v.abs() + err)).all())
     assert (ys[0] == ys[1]).all() and (ys[0] != ys[2]).any()
+
+
+def test_captured_behind_copies_fills_and_another_stream():
+    """Calls captured behind a copy, a fill and work of a second stream (two predecessors): replays read what those left."""
+    m, n, k = 300, 384, 512
+    g = torch.Generator(device="cuda").manual_seed(11)
+    srcs = [torch.randn(m, k, generator=g, device="cuda").bfloat16() for _ in range(2)]
+    fresh = torch.empty_like(srcs[0])
+    x, r = torch.empty_like(fresh), torch.empty(m, k, device="cuda")
+    w, w8, w_s = torch.empty(n, k, device="cuda"), torch.empty(n, k, dtype=torch.uint8, device="cuda"), torch.empty(n, 4, device="cuda")
+    w_src = torch.randn(n, k, generator=g, device="cuda")
+    a8, a_s, out = torch.empty(m, k, dtype=torch.uint8, device="cuda"), torch.empty(m, 4, device="cuda"), torch.empty(m, n, device="cuda")
+    rows = torch.empty(3, 4, device="cuda")                    # the weights' scales: one per 128 rows
+    side = torch.cuda.Stream()
+
+    def work():
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            w.copy_(w_src)
+            fd.fd_quantize_fp8_blocks(w, w8, w_s)
+            rows.copy_(w_s[::128])
+        x.copy_(fresh)
+        r.zero_()
+        fd.fd_add_rmsnorm(x, None, 1e-6, residual=r, residual_out=r, y8=a8, y8_scale=a_s)
+        here.wait_stream(side)
+        fd.fd_matmul_fp8_blocks(a8, a_s, w8, rows, out)
+
+    fresh.copy_(srcs[0])
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for i in (1, 0, 1):
+        fresh.copy_(srcs[i])
+        w_src.mul_(-2.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(r, srcs[i].float())
+        ref.check_codes(a8, a_s, ref.rmsnorm(srcs[i], None, 1e-6)[1], rel=ref.rmsnorm_rel(k))
+        ref.check_codes(w8, w_s, w_src.double())
+        v, err = ref.matmul(a8, a_s, w8, w_s[::128])
+        assert bool(((out.double() - v).abs() <= err + ref.HALF_STEP[out.dtype] * (v.abs() + err)).all())
