@@ -454,7 +454,8 @@ fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, i
  *   values of k on the left, for 128 x 128 weights on the right (quantised once by the caller); the product of an a_scale
  *   and a w_scale has to be finite
  *   bias [n] of bias_dtype (FD_F32 / FD_BF16) or NULL;  out [m, n], columns contiguous
- * Any m >= 0, n >= 1, k >= 1.
+ * Any m >= 0, n >= 1, k >= 1 up to 2^30 each whose product is at most 2^30 blocks, ceil(m / 128) * ceil(n / 256) *
+ * ceil(k / 128); FD_ERR_SHAPE otherwise.
  *   status_out: optional DEVICE int32 that receives, in stream order, 0 or FD_ERR_TIMEOUT if a bounded wait of the kernel
  *   ran out (the result is then incomplete); may be NULL.
  */

@@ -836,6 +836,7 @@ bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 size_t type_bytes(int dtype) { return dtype == FD_F32 ? 4 : 2; }
 constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
 constexpr int64_t MAX_ROWS = int64_t(1) << 31;
+constexpr int64_t MAX_BLOCKS = int64_t(1) << 30;    // of a block-scaled product
 
 fd_status rope_spec_ok(const char* who, const fd_rope_spec* s, const float* pos, int64_t tokens, int head_dim) {
     if (!s || !pos) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
@@ -957,6 +958,9 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k,
         return op_fail(FD_ERR_SHAPE, "%s: m in [0, 2^30], n and k in [1, 2^30]", who);
     if (!aligned16(f->a8) || !aligned16(f->w8)) return op_fail(FD_ERR_INVALID_ARG, "%s: a8 and w8 must be 16-byte aligned", who);
     const int64_t kb = (k + FP8_BLOCK - 1) / FP8_BLOCK, nb = (n + FP8_BLOCK - 1) / FP8_BLOCK;
+    // the kernels count tiles and blocks of K in 32 bits (a quotient on the right: the product can pass 64 bits)
+    const int64_t tiles = (((int64_t)m + 127) / 128) * (((int64_t)n + 255) / 256);
+    if (tiles > MAX_BLOCKS / kb) return op_fail(FD_ERR_SHAPE, "%s: more than 2^30 blocks of 128 x 256 x 128", who);
     // the tensor maps take the strides of single rows too
     if (f->a8_stride % 16 || f->w8_stride % 16 || f->a8_stride < k || f->w8_stride < k || f->a8_stride >= MAX_STRIDE || f->w8_stride >= MAX_STRIDE)
         return op_fail(FD_ERR_SHAPE, "%s: the strides of a8 and w8 must be multiples of 16, at least k and below 2^40", who);

@@ -246,7 +246,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     const uint32_t rank = PAIR ? cluster_ctarank() : 0;
     const uint32_t unit = blockIdx.x / CTAS, n_units = gridDim.x / CTAS;
     const uint32_t m_tiles = (uint32_t)(g.m + CTAS * GB_M - 1) / (CTAS * GB_M), n_tiles = (uint32_t)(g.n + GB_N - 1) / GB_N;
-    const uint32_t total = (uint32_t)m_tiles * (uint32_t)n_tiles;     // (the launcher has checked that it fits)
+    const uint32_t total = m_tiles * n_tiles;                         // (the entry point has checked that it fits)
     const int k_blocks = (g.k + GB_K - 1) / GB_K;
 
     if (warp < 4) {
@@ -781,10 +781,6 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
     const long long tiles_one = (m + GB_M - 1) / GB_M * n_tiles, tiles_pair = (m + 2 * GB_M - 1) / (2 * GB_M) * n_tiles;
     const double cost_one = (double)((tiles_one + dev->sms - 1) / dev->sms) * (k_blocks * 800.0 + 3000.0);
     const double cost_pair = (double)((tiles_pair + dev->pairs - 1) / dev->pairs) * (k_blocks * 715.0 + 3000.0);
-    if (tiles_one * k_blocks > 1LL << 30) {
-        if (why) *why = "more than 2^30 blocks of 128 x 256 x 128";
-        return cudaErrorInvalidValue;
-    }
     const bool split = tiles_split <= dev->clusters[0], pair = !split && cost_pair < cost_one;
     // With few rows the box ends with them: rows of a box that lie behind the tensor are filled with zeros at a cost (9 x 6144 x
     // 6144: 15.3 us with boxes of 128 rows, 9.9 so; eight rows x 9216 x 1536: 7.2 and 5.7).  What the products then read in the

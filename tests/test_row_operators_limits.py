@@ -1,0 +1,34 @@
+"""CPU: limits of the row operators' entry points and what their binding needs.  Refused calls are refused before any CUDA call (the
+pointers are invented numbers)."""
+import ctypes
+
+import pytest
+
+import paper_2607_12121_b200 as fd
+from paper_2607_12121_b200 import binding as b
+
+P = 1 << 20                                          # an address nothing reads
+
+
+def _text():
+    return fd.lib.fd_last_error(None).decode()
+
+
+def _product(m, n, k, **kw):
+    wide = (k + 15) // 16 * 16
+    f = b.FdMatmulFp8Args(a8=P, a_scale=P, w8=P, w_scale=P, out=2 * P, status_out=P, a8_stride=wide, a_scale_stride=(k + 127) // 128, w8_stride=wide,
+                          w_scale_stride=(k + 127) // 128, out_stride=n, out_dtype=fd.FD_BF16)
+    for key, v in kw.items():
+        setattr(f, key, v)
+    return fd.lib.fd_matmul_fp8_blocks(ctypes.byref(f), m, n, k, None)
+
+
+@pytest.mark.parametrize("m,n,k", [
+    (1 << 30, 1 << 30, 1 << 30),                      # 2^68 blocks: the count must not wrap around to none
+    (131072, 131072, 400000),                         # 1.6e9 blocks
+    (1 << 19, 1 << 18, (1 << 15) + 1),                # 2^12 * 2^10 * (2^8 + 1): one block of K too many
+    ((1 << 19) + 1, 1 << 18, 1 << 15), (1 << 19, (1 << 18) + 1, 1 << 15),
+])
+def test_products_of_too_many_blocks_are_a_shape_error(m, n, k):
+    assert _product(m, n, k) == fd.FD_ERR_SHAPE
+    assert "2^30 blocks" in _text()
