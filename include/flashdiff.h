@@ -457,7 +457,7 @@ fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, i
  * Any m >= 0, n >= 1, k >= 1 up to 2^30 each whose product is at most 2^30 blocks, ceil(m / 128) * ceil(n / 256) *
  * ceil(k / 128); FD_ERR_SHAPE otherwise.
  *   status_out: optional DEVICE int32 that receives, in stream order, 0 or FD_ERR_TIMEOUT if a bounded wait of the kernel
- *   ran out (the result is then incomplete); may be NULL.
+ *   ran out (the result is then incomplete); may be NULL.  With m = 0 it receives 0, and the tensors of m rows may be NULL.
  */
 typedef struct {
     const void* a8;

@@ -607,7 +607,7 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
     args = _pack_matmul(a8.data_ptr(), a_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), p_bias, out.data_ptr(), p_scale, p_status,
                         a_stride, _scales(a_scale, "a_scale", (m, kb), device), w_stride, _scales(w_scale, "w_scale", (nb, kb), device),
                         _rows(out, "out", (m, n), device), s_stride, bias_type, out_type, 1 if gelu else 0)
-    if m:
+    if m or p_status:                                   # (without rows the call still clears the status)
         _op_call(device, stream, _call_matmul, args, m, n, k)
 
 

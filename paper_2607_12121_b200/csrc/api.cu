@@ -950,10 +950,12 @@ fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, i
 fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k, void* cuda_stream) {
     const char* who = "fd_matmul_fp8_blocks";
     if (!f) return op_fail(FD_ERR_INVALID_ARG, "%s: args is null", who);
-    if (!f->a8 || !f->a_scale || !f->w8 || !f->w_scale || !f->out) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
+    // (tensors of no rows may have no memory)
+    if (!f->w8 || !f->w_scale || (m != 0 && (!f->a8 || !f->a_scale || !f->out))) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
     if (f->out_dtype != FD_F32 && f->out_dtype != FD_BF16 && f->out_dtype != FD_E4M3) return op_fail(FD_ERR_UNSUPPORTED, "%s: unknown out_dtype", who);
     if (f->bias && !storage_type(f->bias_dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: bias_dtype must be FD_F32 or FD_BF16", who);
-    if ((f->out_dtype == FD_E4M3) != (f->out_scale != nullptr)) return op_fail(FD_ERR_INVALID_ARG, "%s: out_scale goes with an E4M3 output", who);
+    if (f->out_scale ? f->out_dtype != FD_E4M3 : m != 0 && f->out_dtype == FD_E4M3)
+        return op_fail(FD_ERR_INVALID_ARG, "%s: out_scale goes with an E4M3 output", who);
     if (m < 0 || n < 1 || k < 1 || m > (1 << 30) || n > (1 << 30) || k > (1 << 30))
         return op_fail(FD_ERR_SHAPE, "%s: m in [0, 2^30], n and k in [1, 2^30]", who);
     if (!aligned16(f->a8) || !aligned16(f->w8)) return op_fail(FD_ERR_INVALID_ARG, "%s: a8 and w8 must be 16-byte aligned", who);
@@ -974,7 +976,8 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k,
     if ((s = op_rows(who, "out_scale", f->out_scale, f->out_scale_stride, 4, m, nb)) != FD_OK) return s;
     if (f->bias && !aligned_to(f->bias, type_bytes(f->bias_dtype))) return op_fail(FD_ERR_INVALID_ARG, "%s: bias is misaligned", who);
     if (f->status_out && !aligned4(f->status_out)) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is misaligned", who);
-    if (m == 0) return FD_OK;
+    if (m == 0)
+        return f->status_out ? op_launched(who, cudaMemsetAsync(f->status_out, 0, sizeof(int32_t), static_cast<cudaStream_t>(cuda_stream))) : FD_OK;
     try {
         std::string why;
         const cudaError_t e = launch_matmul_fp8_blocks(*f, m, n, k, static_cast<cudaStream_t>(cuda_stream), &why);

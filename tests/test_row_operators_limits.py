@@ -32,3 +32,10 @@ def _product(m, n, k, **kw):
 def test_products_of_too_many_blocks_are_a_shape_error(m, n, k):
     assert _product(m, n, k) == fd.FD_ERR_SHAPE
     assert "2^30 blocks" in _text()
+
+
+def test_a_product_without_rows_needs_no_memory_for_them():
+    for kw in (dict(), dict(out_dtype=fd.FD_E4M3), dict(out_dtype=fd.FD_F32)):
+        assert _product(0, 256, 256, a8=None, a_scale=None, out=None, status_out=None, **kw) == fd.FD_OK
+    assert _product(0, 256, 256, w8=None, status_out=None) == fd.FD_ERR_INVALID_ARG
+    assert _product(0, 256, 256, out_scale=P, status_out=None) == fd.FD_ERR_INVALID_ARG
