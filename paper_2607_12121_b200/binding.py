@@ -7,11 +7,9 @@ in Python.  Importing this module fails loudly if the shared library has not bee
 from __future__ import annotations
 
 import ctypes
-import struct
 import os
+import struct as _struct
 from typing import Dict, Optional
-
-import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libflashdiff.so")
@@ -404,17 +402,27 @@ def fd_set_fp8_operands(ctx: Context, fp8: Optional[Dict[str, "object"]], text_s
 
 # ---- row operators next to the step (no context; work on the tensors' device) ------------------------------------
 # A call's host time is what the smallest of these operators cost, so the checks below look at every tensor once.
+# torch's names are filled in by the first of these calls (the host-side scheduler calls need no torch).
+_TYPE_CODES, _CODES_TYPES = {}, ()
+_float32 = _int32 = _current_device = _raw_stream = _on_device = None
 
-_TYPE_CODES = {torch.bfloat16: FD_BF16, torch.float32: FD_F32}
-_CODES_TYPES = (torch.uint8, torch.float8_e4m3fn)
-_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # (a device tensor is at hand: CUDA is up)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+def _torch_names():
+    global _CODES_TYPES, _float32, _int32, _current_device, _raw_stream, _on_device
+    import torch
+    _CODES_TYPES = (torch.uint8, torch.float8_e4m3fn)
+    _int32, _on_device = torch.int32, torch.cuda.device
+    # (a device tensor is at hand by the time these two are called: CUDA is up)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _TYPE_CODES.update({torch.bfloat16: FD_BF16, torch.float32: FD_F32})
+    _float32 = torch.float32                         # last: what the calls look at
 
 
 # The two argument structs as bytes in their C layout (a ctypes structure takes five times as long to fill).
-_pack_rmsnorm = struct.Struct("7P6q2if4x").pack
-_pack_matmul = struct.Struct("8P6q3i4x").pack
-assert struct.calcsize("7P6q2if4x") == ctypes.sizeof(FdRmsnormArgs) and struct.calcsize("8P6q3i4x") == ctypes.sizeof(FdMatmulFp8Args)
+_pack_rmsnorm = _struct.Struct("7P6q2if4x").pack
+_pack_matmul = _struct.Struct("8P6q3i4x").pack
+assert _struct.calcsize("7P6q2if4x") == ctypes.sizeof(FdRmsnormArgs) and _struct.calcsize("8P6q3i4x") == ctypes.sizeof(FdMatmulFp8Args)
 
 
 def _packed(name: str, *argtypes):
@@ -458,7 +466,7 @@ def _codes(t, name: str, shape, device: int) -> int:
 
 
 def _scales(t, name: str, shape, device: int) -> int:
-    if t.dtype is not torch.float32:
+    if t.dtype is not _float32:
         _op_fail("%s must be float32, not %s" % (name, t.dtype))
     return _rows(t, name, shape, device)
 
@@ -470,7 +478,7 @@ def _op_call(device: int, stream, fn, *args) -> None:
     if _current_device() == device:
         status = fn(*args, (_raw_stream(device) if stream is None else stream.cuda_stream) or None)
     else:
-        with torch.cuda.device(device):
+        with _on_device(device):
             status = fn(*args, (_raw_stream(device) if stream is None else stream.cuda_stream) or None)
     if status != FD_OK:
         _check(None, status)
@@ -488,7 +496,7 @@ def make_rope_axes(axis_dims, theta=10000.0, pairing: str = "interleaved") -> Fd
 
 
 def _rope_pos(spec: FdRopeSpec, pos) -> int:
-    if pos.dtype is not torch.float32 or pos.dim() != 2 or pos.shape[1] != spec.n_axes or not pos.is_contiguous():
+    if pos.dtype is not _float32 or pos.dim() != 2 or pos.shape[1] != spec.n_axes or not pos.is_contiguous():
         _op_fail("pos must be a contiguous float32 tensor [tokens, %d]" % spec.n_axes)
     return pos.shape[0]
 
@@ -507,6 +515,8 @@ def _rope_set(a, b, tokens: int, dh: int, dtype, device: int):
 def fd_rope_axes(spec: FdRopeSpec, pos, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
     """Rotates q (and k) [tokens, heads, head_dim] by the tokens' positions pos [tokens, n_axes] into q_out (k_out);
     any token and head strides, the same tensor twice rotates in place.  ``inverse``: the inverse map, also the gradient."""
+    if _float32 is None:
+        _torch_names()
     tokens, device = _rope_pos(spec, pos), pos.get_device()
     if (k is None) != (k_out is None):
         _op_fail("k and k_out come together")
@@ -519,6 +529,8 @@ def fd_rope_axes(spec: FdRopeSpec, pos, q, q_out, k=None, k_out=None, inverse: b
 
 def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) -> None:
     """The rotary tables [tokens, head_dim / 2] float32 that fd_set_block_variants takes, from positions [tokens, n_axes]."""
+    if _float32 is None:
+        _torch_names()
     tokens, device, half = _rope_pos(spec, pos), pos.get_device(), cos_out.shape[-1]
     for t, name in ((cos_out, "cos_out"), (sin_out, "sin_out")):
         if _scales(t, name, (tokens, half), device) != half:
@@ -530,6 +542,8 @@ def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) ->
 def fd_add_rmsnorm(x, weight, eps: float, residual=None, residual_out=None, y=None, y8=None, y8_scale=None, stream=None) -> None:
     """r = x + residual (kept in residual_out if given), y = r / sqrt(mean(r^2) + eps) * weight; outputs y in x's type and / or
     y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)].  residual_out may be residual, y may be x."""
+    if _float32 is None:
+        _torch_names()
     shape, device = x.shape, x.get_device()
     x_stride = _rows(x, "x", shape, device)
     rows, cols = shape
@@ -564,6 +578,8 @@ def fd_add_rmsnorm(x, weight, eps: float, residual=None, residual_out=None, y=No
 
 def fd_quantize_fp8_blocks(x, y8, y8_scale, stream=None) -> None:
     """E4M3 codes y8 and scales y8_scale [rows, ceil(cols / 128)] of x [rows, cols] (float32 or bfloat16)."""
+    if _float32 is None:
+        _torch_names()
     shape, device = x.shape, x.get_device()
     x_stride = _rows(x, "x", shape, device)
     rows, cols = shape
@@ -578,6 +594,8 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
     """out [m, n] = sum over the 128-blocks of k of a_scale * w_scale * (a8 w8^T) + bias, then tanh-GELU if asked.  a8 [m, k],
     w8 [n, k]: E4M3 codes; a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] float32; out float32, bfloat16,
     or codes with out_scale [m, ceil(n / 128)]; status_out: optional int32 device scalar."""
+    if _float32 is None:
+        _torch_names()
     a_shape, w_shape, device = a8.shape, w8.shape, a8.get_device()
     a_stride = _codes(a8, "a8", a_shape, device)
     (m, k), n = a_shape, w_shape[0]
@@ -601,7 +619,7 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
     if out_scale is not None:
         p_scale, s_stride = out_scale.data_ptr(), _scales(out_scale, "out_scale", (m, nb), device)
     if status_out is not None:
-        if status_out.dtype is not torch.int32 or status_out.get_device() != device or status_out.numel() < 1:
+        if status_out.dtype is not _int32 or status_out.get_device() != device or status_out.numel() < 1:
             _op_fail("status_out must be an int32 tensor on the operands' device")
         p_status = status_out.data_ptr()
     args = _pack_matmul(a8.data_ptr(), a_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), p_bias, out.data_ptr(), p_scale, p_status,

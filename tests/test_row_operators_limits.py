@@ -39,3 +39,24 @@ def test_a_product_without_rows_needs_no_memory_for_them():
         assert _product(0, 256, 256, a8=None, a_scale=None, out=None, status_out=None, **kw) == fd.FD_OK
     assert _product(0, 256, 256, w8=None, status_out=None) == fd.FD_ERR_INVALID_ARG
     assert _product(0, 256, 256, out_scale=P, status_out=None) == fd.FD_ERR_INVALID_ARG
+
+
+_WITHOUT_TORCH = """
+import sys
+sys.modules["torch"] = None                           # an import of it raises
+import numpy as np
+import paper_2607_12121_b200 as fd
+assert fd.fd_sched_pack(np.zeros(2), np.array([3.0, 1.0, 1.0]), np.zeros(3, np.int32)).shape == (3,)
+st = fd.fd_rsearch_init(1, 32, 8)
+assert fd.fd_workspace_bytes(fd.FdConfig(1, 64, 1, 64, 128, 64, 1, 64, 4, fd.FD_F32, fd.FD_ENGINE_SIMT, 1e-6, 0.5, 2)) > 0
+assert not hasattr(fd, "torch") and not hasattr(fd, "struct")
+"""
+
+
+def test_host_side_calls_need_no_torch():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _WITHOUT_TORCH], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
