@@ -21,3 +21,56 @@ def test_status_of_a_product_without_rows(out):
                             torch.empty(0, 256, dtype=TYPES[out], device="cuda"), out_scale=torch.empty(0, 2, device="cuda") if out == "fp8" else None,
                             status_out=status)
     assert int(status) == 0
+
+
+_FRESH_THREADS = """
+import threading, torch, paper_2607_12121_b200 as fd
+m, n, k = {size}
+a8, w8 = torch.full((m, k), 0x38, dtype=torch.uint8, device="cuda"), torch.full((n, k), 0x38, dtype=torch.uint8, device="cuda")
+a_s, w_s = torch.ones(m, (k + 127) // 128, device="cuda"), torch.ones((n + 127) // 128, (k + 127) // 128, device="cuda")
+x, q, pos = torch.ones(m, k, device="cuda"), torch.ones(m, 2, 64, device="cuda"), torch.zeros(m, 1, device="cuda")
+out, y, y8, s = torch.zeros(m, n, device="cuda"), torch.zeros(m, k, device="cuda"), torch.zeros(m, k, dtype=torch.uint8, device="cuda"), torch.zeros_like(a_s)
+c, sn, spec = torch.zeros(m, 32, device="cuda"), torch.ones(m, 32, device="cuda"), fd.make_rope_axes([64])
+calls = [lambda st: fd.fd_matmul_fp8_blocks(a8, a_s, w8, w_s, out, stream=st), lambda st: fd.fd_add_rmsnorm(x, None, 0.0, y=y, stream=st),
+         lambda st: fd.fd_quantize_fp8_blocks(x, y8, s, stream=st), lambda st: fd.fd_rope_axes(spec, pos, q, q, stream=st),
+         lambda st: fd.fd_rope_axes_tables(spec, pos, c, sn, stream=st)]
+streams = [torch.cuda.Stream() for _ in calls]
+if {warm}:
+    for call, st in zip(calls, streams):
+        call(st)
+    for t in (out, y, y8, c):
+        t.zero_()
+torch.cuda.synchronize()
+failed = []
+
+def work(i):
+    try:
+        calls[i](streams[i])
+    except Exception as e:
+        failed.append(e)
+
+for i in range(len(calls)):
+    t = threading.Thread(target=work, args=(i,))
+    t.start()
+    t.join()
+assert not failed, failed
+torch.cuda.synchronize()
+assert bool((out == k).all()) and bool((y == 1).all()) and bool((y8 == 0x7E).all()) and bool((q == 1).all())
+assert bool((c == 1).all()) and bool((sn == 0).all())
+"""
+
+
+def _python(source):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", source], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("size", [(4, 256, 128), (9400, 1024, 128)])
+@pytest.mark.parametrize("warm", [True, False])
+def test_first_cuda_call_of_a_thread(size, warm):
+    """A host thread may start with any of the operators: nothing of CUDA has run in it before."""
+    _python(_FRESH_THREADS.format(size=size, warm=warm))
