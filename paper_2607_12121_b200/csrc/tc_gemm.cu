@@ -8,6 +8,7 @@
 //               gated residual / K-V scatter, 128-bit global stores
 // The number of active rows lives on the device; CTAs derive the tile count from it, so the host
 // never synchronises.  Rows of the last tile beyond the active count are computed and dropped.
+#include <atomic>
 #include <cstdlib>
 
 #include "epilogue.cuh"
@@ -368,8 +369,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 EncodeTiledFn encode_fn(std::string* err) {
-    static EncodeTiledFn fn = nullptr;
-    if (fn) return fn;
+    static std::atomic<EncodeTiledFn> known{nullptr};        // calls on several host threads may be the first at once
+    if (EncodeTiledFn fn = known.load(std::memory_order_relaxed)) return fn;
     void* p = nullptr;
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q);
@@ -377,8 +378,8 @@ EncodeTiledFn encode_fn(std::string* err) {
         if (err) *err = "cuTensorMapEncodeTiled is not available from the driver";
         return nullptr;
     }
-    fn = reinterpret_cast<EncodeTiledFn>(p);
-    return fn;
+    known.store(reinterpret_cast<EncodeTiledFn>(p), std::memory_order_relaxed);
+    return reinterpret_cast<EncodeTiledFn>(p);
 }
 
 int pick_bn(int n_out) { return (n_out % 256 == 0) ? 256 : 128; }

@@ -19,6 +19,7 @@
 // Large sizes then run at the card's power limit: 8192 x 8192 x 8192 at 486 us (2263 TFLOP/s) on a cool card, 560 us after
 // others.
 #include <atomic>
+#include <mutex>
 #include <string>
 
 #include "attn_common.cuh"
@@ -697,7 +698,8 @@ constexpr GsKernel GS_KERNELS[6] = {gemm_blocks_split_kernel<FD_F32, false>, gem
 
 // Per-device set-up, done once: shared-memory attributes, the number of SMs and of CTA pairs the device keeps resident.
 struct GbDevice {
-    std::atomic<int> ready{0};
+    std::mutex set_up;                          // held while the fields below are written
+    std::atomic<bool> ready{false};             // they do not change any more
     int sms = 0, pairs = 0, clusters[8] = {};   // clusters of 1 .. 8 CTAs of the split kernel resident at once
 };
 constexpr int GB_MAX_DEVICES = 64;
@@ -716,35 +718,44 @@ void cluster_config(cudaLaunchConfig_t& lc, cudaLaunchAttribute* at, int cluster
     lc.numAttrs = pdl ? 2 : 1;
 }
 
+cudaError_t gb_set_up(GbDevice& d, int dev) {
+    int n = 0;
+    cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    for (int i = 0; i < 6 && e == cudaSuccess; ++i) {
+        e = cudaFuncSetAttribute(GB_KERNELS<false>[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<false>::SMEM);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(GB_KERNELS<true>[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<true>::SMEM);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(GS_KERNELS[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GS_SMEM);
+    }
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t lc = {};
+    cudaLaunchAttribute at[2];
+    cluster_config(lc, at, 2, n & ~1, GbCfg<true>::SMEM, nullptr, false);
+    int clusters = 0;
+    e = cudaOccupancyMaxActiveClusters(&clusters, GB_KERNELS<true>[0], &lc);
+    if (e != cudaSuccess) return e;
+    d.pairs = max(1, min(n / 2, clusters));
+    for (int i = 0; i < 8; ++i) {
+        cluster_config(lc, at, i + 1, n / (i + 1) * (i + 1), GS_SMEM, nullptr, false);
+        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], GS_KERNELS[0], &lc);
+        if (e != cudaSuccess) return e;
+    }
+    d.sms = n;
+    return cudaSuccess;
+}
+
 cudaError_t gb_device(const GbDevice** out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= GB_MAX_DEVICES) return cudaErrorInvalidDevice;
     GbDevice& d = g_devices[dev];
-    if (!d.ready.load(std::memory_order_acquire)) {          // two threads may both do this: the same values
-        int n = 0;
-        e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-        for (int i = 0; i < 6 && e == cudaSuccess; ++i) {
-            e = cudaFuncSetAttribute(GB_KERNELS<false>[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<false>::SMEM);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(GB_KERNELS<true>[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GbCfg<true>::SMEM);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(GS_KERNELS[i], cudaFuncAttributeMaxDynamicSharedMemorySize, GS_SMEM);
-        }
-        if (e != cudaSuccess) return e;
-        cudaLaunchConfig_t lc = {};
-        cudaLaunchAttribute at[2];
-        cluster_config(lc, at, 2, n & ~1, GbCfg<true>::SMEM, nullptr, false);
-        int clusters = 0;
-        e = cudaOccupancyMaxActiveClusters(&clusters, GB_KERNELS<true>[0], &lc);
-        if (e != cudaSuccess) return e;
-        d.pairs = max(1, min(n / 2, clusters));
-        for (int i = 0; i < 8; ++i) {
-            cluster_config(lc, at, i + 1, n / (i + 1) * (i + 1), GS_SMEM, nullptr, false);
-            e = cudaOccupancyMaxActiveClusters(&d.clusters[i], GS_KERNELS[0], &lc);
+    if (!d.ready.load(std::memory_order_acquire)) {
+        std::lock_guard<std::mutex> lock(d.set_up);
+        if (!d.ready.load(std::memory_order_relaxed)) {
+            e = gb_set_up(d, dev);                           // (after an error the next call tries again)
             if (e != cudaSuccess) return e;
+            d.ready.store(true, std::memory_order_release);
         }
-        d.sms = n;
-        d.ready.store(1, std::memory_order_release);
     }
     *out = &d;
     return cudaSuccess;

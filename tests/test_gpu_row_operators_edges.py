@@ -74,3 +74,39 @@ def _python(source):
 def test_first_cuda_call_of_a_thread(size, warm):
     """A host thread may start with any of the operators: nothing of CUDA has run in it before."""
     _python(_FRESH_THREADS.format(size=size, warm=warm))
+
+
+_FIRST_CALLS = """
+import threading, torch, paper_2607_12121_b200 as fd
+sizes = [(4, 256, 128), (9400, 1024, 128), (5200, 4608, 128), (300, 1152, 1536)] * 2      # every form of the product, twice
+ops = []
+for m, n, k in sizes:
+    codes = [torch.full((r, k), 0x38, dtype=torch.uint8, device="cuda") for r in (m, n)]
+    ops.append((codes[0], torch.ones(m, (k + 127) // 128, device="cuda"), codes[1], torch.ones((n + 127) // 128, (k + 127) // 128, device="cuda"),
+                torch.zeros(m, n, device="cuda")))
+torch.cuda.synchronize()
+gate, failed = threading.Barrier(len(ops)), []
+
+def work(i):
+    stream = torch.cuda.Stream()
+    gate.wait()
+    try:
+        fd.fd_matmul_fp8_blocks(*ops[i], stream=stream)
+        stream.synchronize()
+    except Exception as e:
+        failed.append(e)
+
+threads = [threading.Thread(target=work, args=(i,)) for i in range(len(ops))]
+for t in threads:
+    t.start()
+for t in threads:
+    t.join()
+assert not failed, failed
+for (m, n, k), op in zip(sizes, ops):
+    assert bool((op[4] == k).all()), (m, n, k)
+"""
+
+
+def test_first_calls_of_several_threads_at_once():
+    """The product's per-device set-up belongs to whichever call comes first: eight threads make that call together in a new process."""
+    _python(_FIRST_CALLS)
