@@ -304,19 +304,21 @@ cudaError_t launch_reg(const RowArgs& a, cudaStream_t st) {
     return ptx::launch_kernel(row_blocks_kernel<TX, TR, W, NV, NORM>, grid, THREADS, 0, st, true, a);
 }
 
+constexpr int ROW_MAX_NV = 6, ROW_MAX_W = 8;
+
+// (fewer than ROW_MAX_W warps hold at most three vectors a lane: launch_typed)
 template <typename TX, typename TR, int W, bool NORM>
 cudaError_t launch_nv(const RowArgs& a, cudaStream_t st) {
-    switch ((a.cols + 256 * W - 1) / (256 * W)) {
-        case 1: return launch_reg<TX, TR, W, 1, NORM>(a, st);
-        case 2: return launch_reg<TX, TR, W, 2, NORM>(a, st);
-        case 3: return launch_reg<TX, TR, W, 3, NORM>(a, st);
-        case 4: return launch_reg<TX, TR, W, 4, NORM>(a, st);
-        case 5: return launch_reg<TX, TR, W, 5, NORM>(a, st);
-        default: return launch_reg<TX, TR, W, 6, NORM>(a, st);
+    const int nv = (a.cols + 256 * W - 1) / (256 * W);
+    if (nv == 1) return launch_reg<TX, TR, W, 1, NORM>(a, st);
+    if (nv == 2) return launch_reg<TX, TR, W, 2, NORM>(a, st);
+    if constexpr (W == ROW_MAX_W) {
+        if (nv == 4) return launch_reg<TX, TR, W, 4, NORM>(a, st);
+        if (nv == 5) return launch_reg<TX, TR, W, 5, NORM>(a, st);
+        if (nv == 6) return launch_reg<TX, TR, W, 6, NORM>(a, st);
     }
+    return launch_reg<TX, TR, W, 3, NORM>(a, st);
 }
-
-constexpr int ROW_MAX_NV = 6, ROW_MAX_W = 8;
 
 template <typename TX, typename TR, bool NORM>
 cudaError_t launch_typed(const RowArgs& a, cudaStream_t st) {

@@ -110,3 +110,51 @@ for (m, n, k), op in zip(sizes, ops):
 def test_first_calls_of_several_threads_at_once():
     """The product's per-device set-up belongs to whichever call comes first: eight threads make that call together in a new process."""
     _python(_FIRST_CALLS)
+
+
+def _row_forms():
+    """(rows, columns) for every number of warps a row and of vectors a lane of the aligned form, and the widths next to each."""
+    for rows, warps, vectors in [(700, 1, (1, 2, 3)), (9, 2, (1,)), (700, 2, (2, 3)), (9, 4, (1,)), (700, 4, (2, 3)), (9, 8, (1,)), (700, 8, (2, 3)),
+                                 (150, 8, (4, 5, 6))]:
+        for v in vectors:
+            for cols in (256 * warps * v - 8, 256 * warps * v):
+                yield rows, cols
+
+
+@pytest.mark.parametrize("rows,cols", sorted(set(_row_forms())))
+@pytest.mark.parametrize("xt,rt", [(torch.bfloat16, torch.float32), (torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16)])
+def test_every_aligned_form_of_the_norm_and_the_quantiser(rows, cols, xt, rt):
+    g = torch.Generator(device="cuda").manual_seed(rows * 7 + cols)
+    x, res = torch.randn(rows, cols, generator=g, device="cuda").to(xt), (3 * torch.randn(rows, cols, generator=g, device="cuda")).to(rt)
+    w = (1 + 0.2 * torch.randn(cols, generator=g, device="cuda")).to(xt)
+    out, y, y8, sc = torch.empty_like(res), torch.empty_like(x), torch.empty(rows, cols, dtype=torch.uint8, device="cuda"), torch.empty(rows, ref.blocks(cols), device="cuda")
+    fd.fd_add_rmsnorm(x, w, 1e-6, residual=res, residual_out=out, y=y, y8=y8, y8_scale=sc)
+    r, want = ref.rmsnorm(x, w, 1e-6, res)
+    rel = ref.rmsnorm_rel(cols)
+    assert bool(((out.double() - r).abs() <= (ref.U32 + ref.HALF_STEP[rt]) * r.abs() * (1 + 2.0 ** -8)).all())
+    assert bool(((y.double() - want).abs() <= (rel + ref.HALF_STEP[xt] * (1 + rel)) * want.abs()).all())
+    ref.check_codes(y8, sc, want, rel=rel)
+    fd.fd_quantize_fp8_blocks(x, y8, sc)
+    _equals_the_definition(x, y8, sc)
+
+
+def _equals_the_definition(x, y8, sc):
+    """Codes and scales bit for bit: max(amax, 2^-100) / 448 and v * (448 / max(amax, 2^-100)), each operation rounded once to fp32."""
+    rows, cols = x.shape
+    p = torch.nn.functional.pad(x.float(), (0, ref.blocks(cols) * 128 - cols)).view(rows, -1, 128)
+    amax = p.abs().amax(dim=2).clamp_min(2.0 ** -100)
+    most = torch.full_like(amax, 448.0)              # (a scalar numerator would be a reciprocal and a product)
+    codes = (p * (most / amax)[..., None]).to(torch.float8_e4m3fn).view(rows, -1)[:, :cols].contiguous()
+    assert torch.equal(sc, amax / most) and torch.equal(y8.view(torch.uint8), codes.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols", [(8192, 1536), (154, 1000), (3, 130), (1000, 1333), (2, 16384)])
+def test_quantiser_equals_the_headers_rule_bit_for_bit(rows, cols, dtype):
+    """Rounding ties are frequent in bf16 data: the header's two roundings decide them, in every form of the kernel."""
+    x = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(cols), device="cuda") * 2
+    x[:, ::190] *= 20.0
+    x = x.to(dtype)
+    y8, sc = torch.empty(rows, cols, dtype=torch.uint8, device="cuda"), torch.empty(rows, ref.blocks(cols), device="cuda")
+    fd.fd_quantize_fp8_blocks(x, y8, sc)
+    _equals_the_definition(x, y8, sc)
