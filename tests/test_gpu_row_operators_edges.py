@@ -158,3 +158,78 @@ def test_quantiser_equals_the_headers_rule_bit_for_bit(rows, cols, dtype):
     y8, sc = torch.empty(rows, cols, dtype=torch.uint8, device="cuda"), torch.empty(rows, ref.blocks(cols), device="cuda")
     fd.fd_quantize_fp8_blocks(x, y8, sc)
     _equals_the_definition(x, y8, sc)
+
+
+def _operands(m, n, k, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed + m * 3 + n * 5 + k)
+    a = torch.randn(m, k, generator=g, device="cuda") * torch.exp(torch.randn(m, 1, generator=g, device="cuda"))
+    a[:, ::29] *= 8
+    return (*ref.quantise(a, False), *ref.quantise(0.05 * torch.randn(n, k, generator=g, device="cuda"), True))
+
+
+def _product(a8, a_s, w8, w_s, out, bias=None, gelu=False, **kw):
+    """One product in the default form (no status word), held to the 64-bit definition."""
+    m, n = a8.shape[0], w8.shape[0]
+    o = torch.full((m, n), 5.0, device="cuda").to(TYPES[out])
+    sc = torch.full((m, ref.blocks(n)), 9.0, device="cuda") if out == "fp8" else None
+    fd.fd_matmul_fp8_blocks(a8, a_s, w8, w_s, o, bias=bias, gelu=gelu, out_scale=sc, **kw)
+    v, err = ref.matmul(a8, a_s, w8, w_s, bias)
+    if gelu:
+        v, err = ref.gelu(v, err)
+    if sc is not None:
+        ref.check_codes(o, sc, v, absolute=err)
+    else:
+        assert bool(((o.double() - v).abs() <= err + ref.HALF_STEP[o.dtype] * (v.abs() + err)).all())
+    return o
+
+
+@pytest.mark.parametrize("out,bias,gelu", [("bf16", None, False), ("f32", torch.float32, True), ("fp8", torch.bfloat16, True)])
+@pytest.mark.parametrize("m,n", [(1, 300), (40, 128), (121, 300), (128, 128), (130, 300)])
+@pytest.mark.parametrize("k", [3840, 4224, 5376, 6144, 8960])
+def test_blocks_of_k_shared_out_to_five_to_eight_ctas(m, n, k, out, bias, gelu):
+    """At least six blocks of 128 go to a CTA: 30 and 33 blocks to five, 42 to seven, 48 and 70 to eight.  With seven the rows of a tile
+    are finished in slices of 24, the last CTA having none."""
+    b = None if bias is None else (torch.randn(n, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda") * 0.3).to(bias)
+    _product(*_operands(m, n, k), out, b, gelu)
+
+
+@pytest.mark.parametrize("k", [3840, 5376, 6144, 8960])
+@pytest.mark.parametrize("m", [1, 20, 121, 128, 200])
+def test_whole_numbers_over_many_blocks_are_exact_and_repeat(m, k):
+    """Codes of at most 2 and scales from 1/2 to 2: every term is a whole number of quarters of at most 16, so a sum of 8960 of them is
+    below 2^20 quarters: exact in fp32 in any order."""
+    n = 300
+    g = torch.Generator(device="cuda").manual_seed(m + k)
+    a8, w8 = (torch.randint(-2, 3, (r, k), generator=g, device="cuda").float().to(torch.float8_e4m3fn) for r in (m, n))
+    a_s = torch.exp2(torch.randint(-1, 2, (m, ref.blocks(k)), generator=g, device="cuda").float())
+    w_s = torch.exp2(torch.randint(-1, 2, (ref.blocks(n), ref.blocks(k)), generator=g, device="cuda").float())
+    outs = [torch.empty(m, n, device="cuda") for _ in range(3)]
+    for o in outs:
+        fd.fd_matmul_fp8_blocks(a8, a_s, w8, w_s, o)
+    v, _ = ref.matmul(a8, a_s, w8, w_s)
+    assert all(torch.equal(o.double(), v) for o in outs)
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp8"])
+@pytest.mark.parametrize("m,n,k", [(1, 1536, 8960), (121, 300, 5376), (700, 1536, 1536), (5200, 4608, 256), (9400, 1024, 256)])
+def test_repeated_products_with_gelu_are_bit_equal(m, n, k, out):
+    a8, a_s, w8, w_s = _operands(m, n, k)
+    outs = [_product(a8, a_s, w8, w_s, out, gelu=True) for _ in range(2)]
+    assert torch.equal(outs[0].view(torch.uint8), outs[1].view(torch.uint8))
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("m,n,k", [(1, 130, 100), (8, 9216, 256), (154, 1536, 1536), (257, 513, 1000), (5200, 4600, 300), (9400, 1000, 300)])
+def test_default_form_behind_the_kernel_that_makes_its_operand(m, n, k, out):
+    """Without a status word the launch may start while its predecessor still runs: the quantiser that writes the activations, twice
+    over the same memory."""
+    _, _, w8, w_s = _operands(1, n, k)
+    wide = (k + 15) // 16 * 16
+    w = torch.empty(n, wide, dtype=torch.uint8, device="cuda")[:, :k]
+    w.copy_(w8.view(torch.uint8))
+    a8, a_s = torch.empty(m, wide, dtype=torch.uint8, device="cuda")[:, :k], torch.empty(m, ref.blocks(k), device="cuda")
+    for seed in (1, 2):
+        x = torch.randn(m, k, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").bfloat16()
+        torch.cuda.synchronize()
+        fd.fd_quantize_fp8_blocks(x, a8, a_s)
+        _product(a8, a_s, w, w_s, out, gelu=True)
