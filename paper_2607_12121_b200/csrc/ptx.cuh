@@ -85,8 +85,9 @@ __device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// Bounded wait.  `abort_flag` (shared memory) lets one role's time-out release the others.
-constexpr uint32_t WAIT_LIMIT = 1u << 22;
+// Bounded wait.  `abort_flag` (shared memory) lets one role's time-out release the others.  A poll that finds nothing takes 4.1 us
+// (the blocking try_wait keeps the thread for most of it): 1.1 s in all.  With 2^22 polls a wait took 17.2 s to give up.
+constexpr uint32_t WAIT_LIMIT = 1u << 18;
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     // the non-blocking test first: it returns sooner than try_wait when the phase has already completed
     if (mbar_test_wait(bar, parity)) return true;
