@@ -486,6 +486,13 @@ fd_status fd_poll_status(fd_ctx* ctx, void* cuda_stream);
  */
 fd_status fd_selftest_bounded_wait(fd_ctx* ctx, void* cuda_stream);
 
+/*
+ * The same for the waits inside fd_matmul_fp8_blocks: the product's own kernel for these arguments, but one that fetches no
+ * operands, so that every wait for them runs out.  The kernel returns normally after a second or so; status_out (required
+ * here) receives FD_ERR_TIMEOUT and `out` holds nothing of use.
+ */
+fd_status fd_selftest_matmul_wait(const fd_matmul_fp8_args* args, int m, int n, int k, void* cuda_stream);
+
 /* Number of kernels the library has launched through this context so far (host counter). */
 int64_t fd_launch_count(const fd_ctx* ctx);
 

@@ -27,7 +27,8 @@ EXPORTS = ["fd_workspace_bytes", "fd_create", "fd_partition_regions", "fd_region
            "fd_embed_latent", "fd_update_latent", "fd_regional_step_mass", "fd_region_activity_attn",
            "fd_sched_pack", "fd_sched_form_batch", "fd_rsearch_init", "fd_rsearch_update", "fd_set_block_variants",
            "fd_set_text_stream", "fd_set_cross_attention", "fd_set_fp8_operands", "fd_debug_buffer", "fd_set_fp8_text_stream",
-           "fd_rope_axes", "fd_rope_axes_tables", "fd_add_rmsnorm", "fd_quantize_fp8_blocks", "fd_matmul_fp8_blocks"]
+           "fd_rope_axes", "fd_rope_axes_tables", "fd_add_rmsnorm", "fd_quantize_fp8_blocks", "fd_matmul_fp8_blocks",
+           "fd_selftest_matmul_wait"]
 FD_NOALLOC_MAX_REGION_SLOTS = 16384
 PROF_GROUPS = ["activity", "compact", "adaln", "ln_modulate", "gemm_qkv", "attention", "gemm_out", "gemm_fc1",
                "gemm_fc2", "partition", "sampler", "qk_variants", "cross_attention"]
@@ -166,6 +167,8 @@ def _load() -> ctypes.CDLL:
     lib.fd_quantize_fp8_blocks.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, i64, vp]
     lib.fd_matmul_fp8_blocks.restype = i32
     lib.fd_matmul_fp8_blocks.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
+    lib.fd_selftest_matmul_wait.restype = i32
+    lib.fd_selftest_matmul_wait.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
     lib.fd_launch_count.restype = ctypes.c_int64
     lib.fd_launch_count.argtypes = [vp]
     lib.fd_destroy.restype = i32
@@ -433,6 +436,7 @@ def _packed(name: str, *argtypes):
 
 _call_rmsnorm = _packed("fd_add_rmsnorm", ctypes.c_int64, ctypes.c_int)
 _call_matmul = _packed("fd_matmul_fp8_blocks", ctypes.c_int, ctypes.c_int, ctypes.c_int)
+_call_matmul_selftest = _packed("fd_selftest_matmul_wait", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 
 
 def _op_fail(text: str):
@@ -590,10 +594,12 @@ def fd_quantize_fp8_blocks(x, y8, y8_scale, stream=None) -> None:
 
 
 def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = False, out_scale=None, status_out=None,
-                         stream=None) -> None:
+                         stream=None, _call=_call_matmul) -> None:
     """out [m, n] = sum over the 128-blocks of k of a_scale * w_scale * (a8 w8^T) + bias, then tanh-GELU if asked.  a8 [m, k],
     w8 [n, k]: E4M3 codes; a_scale [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)] float32; out float32, bfloat16,
-    or codes with out_scale [m, ceil(n / 128)]; status_out: optional int32 device scalar."""
+    or codes with out_scale [m, ceil(n / 128)].  status_out: optional int32 device scalar that receives 0, or FD_ERR_TIMEOUT if a
+    bounded wait of the kernel ran out; without it an incomplete result goes unreported, with it the launch waits for the one
+    before it to end."""
     if _float32 is None:
         _torch_names()
     a_shape, w_shape, device = a8.shape, w8.shape, a8.get_device()
@@ -626,7 +632,12 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
                         a_stride, _scales(a_scale, "a_scale", (m, kb), device), w_stride, _scales(w_scale, "w_scale", (nb, kb), device),
                         _rows(out, "out", (m, n), device), s_stride, bias_type, out_type, 1 if gelu else 0)
     if m or p_status:                                   # (without rows the call still clears the status)
-        _op_call(device, stream, _call_matmul, args, m, n, k)
+        _op_call(device, stream, _call, args, m, n, k)
+
+
+def fd_selftest_matmul_wait(a8, a_scale, w8, w_scale, out, status_out, out_scale=None, stream=None) -> None:
+    """fd_matmul_fp8_blocks without its operands' copies: every wait runs out, status_out receives FD_ERR_TIMEOUT."""
+    fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, None, False, out_scale, status_out, stream, _call_matmul_selftest)
 
 
 def fd_sched_pack(load, cost, home):

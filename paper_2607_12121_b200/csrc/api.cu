@@ -947,8 +947,8 @@ fd_status fd_quantize_fp8_blocks(const void* x, int64_t x_stride, int x_dtype, i
     return row_blocks_call("fd_quantize_fp8_blocks", a, rows, cols, false, cuda_stream);
 }
 
-fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k, void* cuda_stream) {
-    const char* who = "fd_matmul_fp8_blocks";
+namespace {
+fd_status matmul_fp8_call(const char* who, const fd_matmul_fp8_args* f, int m, int n, int k, bool starve, void* cuda_stream) {
     if (!f) return op_fail(FD_ERR_INVALID_ARG, "%s: args is null", who);
     // (tensors of no rows may have no memory)
     if (!f->w8 || !f->w_scale || (m != 0 && (!f->a8 || !f->a_scale || !f->out))) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
@@ -980,11 +980,22 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* f, int m, int n, int k,
         return f->status_out ? op_launched(who, cudaMemsetAsync(f->status_out, 0, sizeof(int32_t), static_cast<cudaStream_t>(cuda_stream))) : FD_OK;
     try {
         std::string why;
-        const cudaError_t e = launch_matmul_fp8_blocks(*f, m, n, k, static_cast<cudaStream_t>(cuda_stream), &why);
+        const cudaError_t e = launch_matmul_fp8_blocks(*f, m, n, k, starve, static_cast<cudaStream_t>(cuda_stream), &why);
         return op_launched(who, e, why);
     } catch (...) {
         return op_fail(FD_ERR_CUDA, "%s: out of host memory", who);
     }
+}
+}  // namespace
+
+fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* args, int m, int n, int k, void* cuda_stream) {
+    return matmul_fp8_call("fd_matmul_fp8_blocks", args, m, n, k, false, cuda_stream);
+}
+
+fd_status fd_selftest_matmul_wait(const fd_matmul_fp8_args* args, int m, int n, int k, void* cuda_stream) {
+    const char* who = "fd_selftest_matmul_wait";
+    if (args && !args->status_out) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is null", who);
+    return matmul_fp8_call(who, args, m, n, k, true, cuda_stream);
 }
 
 fd_status fd_poll_status(fd_ctx* c, void* cuda_stream) {

@@ -215,8 +215,8 @@ cudaError_t launch_rope_tables(const fd_rope_spec& spec, const float* pos, int64
 // row_blocks.cu: residual addition + RMS norm (norm = false: none of both), 8-bit output with block scales
 cudaError_t launch_row_blocks(const fd_rmsnorm_args& a, int64_t rows, int cols, bool norm, cudaStream_t st);
 
-// tc_gemm_blocks.cu
-cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& a, int m, int n, int k, cudaStream_t st, std::string* why);
+// tc_gemm_blocks.cu (starve: the self-test's form, which issues no copies)
+cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& a, int m, int n, int k, bool starve, cudaStream_t st, std::string* why);
 
 // partition.cu
 size_t partition_scratch_bytes(int max_batch, int max_tokens, int max_regions);

@@ -64,6 +64,7 @@ struct GbArgs {
     int bias_bf16;
     int tma_out;                               // `out` is stored through its tensor map (whole 16-byte units)
     int vec_out;                               // `out` takes stores of four columns
+    int starve;                                // self-test: no copy is issued, so that every wait for one runs out
 };
 
 __device__ __forceinline__ void gb_report(int32_t* status, int code) {
@@ -257,7 +258,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             // Here and in the other roles a lane whose wait ran out does nothing more, but no lane leaves a loop before the others.
             uint32_t issued = 0, s = 0, ph = 0;
             bool ok = true;
-            for (uint32_t tile = unit; tile < total; tile += n_units) {
+            const uint32_t end = g.starve ? 0 : total;
+            for (uint32_t tile = unit; tile < end; tile += n_units) {
                 const int m = (int)(tile / n_tiles), n = (int)(tile % n_tiles);
                 const int y_a = (m * CTAS + (int)rank) * GB_M, y_w = n * GB_N + (int)rank * Cfg::B_ROWS;
                 for (int kb = 0; kb < k_blocks; ++kb) {
@@ -527,6 +529,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     const int k_blocks = (g.k + GB_K - 1) / GB_K;
     const int kb0 = (int)((long long)k_blocks * rank / splits), blocks = (int)((long long)k_blocks * (rank + 1) / splits) - kb0;
 
+    const int loads = g.starve ? 0 : blocks;
     auto load_stage = [&](int it, bool ok) { // whole warp 0
         const int s = it % GS_STAGES;
         if (elect_one() && ok) {
@@ -558,7 +561,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
         }
         __syncwarp();
         pdl_wait();
-        for (int it = 0; it < min(blocks, GS_STAGES); ++it) load_stage(it, true);
+        for (int it = 0; it < min(loads, GS_STAGES); ++it) load_stage(it, true);
     } else if (warp == 1) {
         tmem_alloc(tmem_slot, GS_BUFS * GS_N);
         tmem_relinquish();
@@ -577,8 +580,8 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
 
     if (warp == 0) {
         bool ok = true;
-        int issued = min(blocks, GS_STAGES);
-        for (int it = issued; it < blocks; ++it) {
+        int issued = min(loads, GS_STAGES);
+        for (int it = issued; it < loads; ++it) {
             ok = ok && mbar_wait(&empty[it % GS_STAGES], ((it / GS_STAGES) & 1) ^ 1, abort_flag);
             issued += ok;
             load_stage(it, ok);
@@ -763,7 +766,7 @@ cudaError_t gb_device(const GbDevice** out) {
 
 }  // namespace
 
-cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, int k, cudaStream_t st, std::string* why) {
+cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, int k, bool starve, cudaStream_t st, std::string* why) {
     const GbDevice* dev = nullptr;
     cudaError_t e = gb_device(&dev);
     if (e != cudaSuccess) return e;
@@ -772,7 +775,7 @@ cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& f, int m, int n, 
              f.out_scale_stride, m, n, k, f.bias_dtype == FD_BF16,
              // (a bulk store clips columns to whole 16 bytes)
              (reinterpret_cast<uintptr_t>(f.out) & 15) == 0 && f.out_stride * es % 16 == 0 && f.out_stride * es < 1LL << 40 && (long long)n * es % 16 == 0,
-             reinterpret_cast<uintptr_t>(f.out) % (4 * es) == 0 && f.out_stride % 4 == 0};
+             reinterpret_cast<uintptr_t>(f.out) % (4 * es) == 0 && f.out_stride % 4 == 0, starve};
     if (f.status_out) {
         e = cudaMemsetAsync(f.status_out, 0, sizeof(int32_t), st);
         if (e != cudaSuccess) return e;

@@ -60,3 +60,13 @@ def test_host_side_calls_need_no_torch():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", _WITHOUT_TORCH], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_the_wait_selftest_checks_its_arguments():
+    call = fd.lib.fd_selftest_matmul_wait
+    f = b.FdMatmulFp8Args(a8=P, a_scale=P, w8=P, w_scale=P, out=2 * P, a8_stride=256, a_scale_stride=2, w8_stride=256, w_scale_stride=2, out_stride=256,
+                          out_dtype=fd.FD_BF16)
+    assert call(None, 4, 256, 256, None) == fd.FD_ERR_INVALID_ARG
+    assert call(ctypes.byref(f), 4, 256, 256, None) == fd.FD_ERR_INVALID_ARG and "status_out" in _text()
+    f.status_out, f.w8_stride = P, 240
+    assert call(ctypes.byref(f), 4, 256, 256, None) == fd.FD_ERR_SHAPE and "fd_selftest_matmul_wait" in _text()
