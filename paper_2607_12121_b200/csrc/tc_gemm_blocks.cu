@@ -67,6 +67,12 @@ struct GbArgs {
     int starve;                                // self-test: no copy is issued, so that every wait for one runs out
 };
 
+// After a time-out, before the CTA leaves: copies that it or its peer still has in flight land (a few microseconds are enough), whichever
+// CTA's barrier they are counted on.
+__device__ __forceinline__ void gb_settle() {
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+}
+
 __device__ __forceinline__ void gb_report(int32_t* status, int code) {
     if (status) atomicCAS(status, 0, code);
 }
@@ -355,7 +361,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
                 if (it >= 2) ok = ok && mbar_wait(&tfull[it & 1], ((it >> 1) & 1) ^ 1, abort_flag);
                 copy_async_wait<GB_AHEAD - 1>();             // this block's scales have landed
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&tfull[it & 1]);
+                if (lane == 0 && ok) mbar_arrive(&tfull[it & 1]);          // (after a time-out the phases are not in step any more)
                 fetch();
             }
             copy_async_wait<0>();
@@ -427,6 +433,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 
     tc_fence_before();
     __syncthreads();
+    if (warp == 1 && *abort_flag) gb_settle();
+    __syncwarp();
     if constexpr (PAIR) cluster_sync_all();  // neither CTA leaves while its peer may still signal it
     if (warp == 1) {
         tc_fence_after();
@@ -616,7 +624,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
             if (it >= GS_BUFS) ok = ok && mbar_wait(&tfull[it % GS_BUFS], ((it / GS_BUFS) & 1) ^ 1, abort_flag);
             copy_async_wait<GB_AHEAD - 1>();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&tfull[it % GS_BUFS]);
+            if (lane == 0 && ok) mbar_arrive(&tfull[it % GS_BUFS]);
             fetch(it + GB_AHEAD);
         }
         copy_async_wait<0>();
@@ -673,6 +681,7 @@ gemm_blocks_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem_base, GS_BUFS * GS_N);
+        if (*abort_flag) gb_settle();
     }
     if (warp >= 4) {
         const uint32_t part = smem_u32(s_part);
