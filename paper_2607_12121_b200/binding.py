@@ -452,6 +452,8 @@ def _type_code(t, name: str) -> int:
 
 def _rows(t, name: str, shape, device: int) -> int:
     """Row stride of the 2-D tensor ``t`` of the wanted shape (rows, columns) on the device, columns contiguous."""
+    if len(shape) != 2:
+        _op_fail("%s must have two dimensions, not %s" % (name, list(shape)))
     if t.shape != shape or t.get_device() != device:
         _op_fail("%s must be %s on device %d, not %s on %s" % (name, list(shape), device, list(t.shape), t.device))
     rows, cols = shape
@@ -524,7 +526,7 @@ def fd_rope_axes(spec: FdRopeSpec, pos, q, q_out, k=None, k_out=None, inverse: b
     tokens, device = _rope_pos(spec, pos), pos.get_device()
     if (k is None) != (k_out is None):
         _op_fail("k and k_out come together")
-    code, dh = _type_code(q, "q"), q.shape[-1]
+    code, dh = _type_code(q, "q"), q.shape[-1] if q.shape else 0
     first = _rope_set(q, q_out, tokens, dh, q.dtype, device)
     rows = (FdRopeRows * 2)(first) if k is None else (FdRopeRows * 2)(first, _rope_set(k, k_out, tokens, dh, q.dtype, device))
     if tokens:
@@ -535,7 +537,7 @@ def fd_rope_axes_tables(spec: FdRopeSpec, pos, cos_out, sin_out, stream=None) ->
     """The rotary tables [tokens, head_dim / 2] float32 that fd_set_block_variants takes, from positions [tokens, n_axes]."""
     if _float32 is None:
         _torch_names()
-    tokens, device, half = _rope_pos(spec, pos), pos.get_device(), cos_out.shape[-1]
+    tokens, device, half = _rope_pos(spec, pos), pos.get_device(), cos_out.shape[-1] if cos_out.shape else 0
     for t, name in ((cos_out, "cos_out"), (sin_out, "sin_out")):
         if _scales(t, name, (tokens, half), device) != half:
             _op_fail("%s must be contiguous" % name)
@@ -604,7 +606,7 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
         _torch_names()
     a_shape, w_shape, device = a8.shape, w8.shape, a8.get_device()
     a_stride = _codes(a8, "a8", a_shape, device)
-    (m, k), n = a_shape, w_shape[0]
+    (m, k), n = a_shape, w_shape[0] if w_shape else 0
     w_stride = _codes(w8, "w8", (n, k), device)
     kb, nb = (k + 127) // 128, (n + 127) // 128
     if m <= 1:                                          # the stride of a single row is free: round it up to what is asked for

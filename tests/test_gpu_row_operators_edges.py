@@ -233,3 +233,23 @@ def test_default_form_behind_the_kernel_that_makes_its_operand(m, n, k, out):
         torch.cuda.synchronize()
         fd.fd_quantize_fp8_blocks(x, a8, a_s)
         _product(a8, a_s, w, w_s, out, gelu=True)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("stride", [0, 1 << 39])
+@pytest.mark.parametrize("n", [640, 20000])
+def test_the_stride_of_a_single_output_row_is_free(n, stride, out):
+    """With one row no row follows: any stride is accepted, in every form (20000 columns are too many tiles for the small one)."""
+    a8, a_s, w8, w_s = _operands(1, n, 256)
+    o = torch.full((1, n), 5.0, device="cuda").to(TYPES[out])
+    sc = torch.full((1, ref.blocks(n)), 9.0, device="cuda")
+    f = b.FdMatmulFp8Args(a8=a8.data_ptr(), a_scale=a_s.data_ptr(), w8=w8.data_ptr(), w_scale=w_s.data_ptr(), out=o.data_ptr(),
+                          out_scale=sc.data_ptr() if out == "fp8" else None, a8_stride=256, a_scale_stride=0, w8_stride=256, w_scale_stride=2,
+                          out_stride=stride, out_scale_stride=0, out_dtype={"bf16": fd.FD_BF16, "f32": fd.FD_F32, "fp8": fd.FD_E4M3}[out])
+    st = fd.lib.fd_matmul_fp8_blocks(ctypes.byref(f), 1, n, 256, torch.cuda.current_stream().cuda_stream or None)
+    assert st == fd.FD_OK, fd.lib.fd_last_error(None)
+    v, err = ref.matmul(a8, a_s, w8, w_s)
+    if out == "fp8":
+        ref.check_codes(o, sc, v, absolute=err)
+    else:
+        assert bool(((o.double() - v).abs() <= err + ref.HALF_STEP[o.dtype] * (v.abs() + err)).all())

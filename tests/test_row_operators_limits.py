@@ -70,3 +70,20 @@ def test_the_wait_selftest_checks_its_arguments():
     assert call(ctypes.byref(f), 4, 256, 256, None) == fd.FD_ERR_INVALID_ARG and "status_out" in _text()
     f.status_out, f.w8_stride = P, 240
     assert call(ctypes.byref(f), 4, 256, 256, None) == fd.FD_ERR_SHAPE and "fd_selftest_matmul_wait" in _text()
+
+
+def test_binding_refuses_other_numbers_of_dimensions():
+    import torch
+    x, x3, none = torch.zeros(2, 256), torch.zeros(1, 2, 256), torch.zeros(())
+    codes, scale, w = torch.zeros(2, 256, dtype=torch.uint8), torch.zeros(2, 2), torch.zeros(256, 256, dtype=torch.uint8)
+    spec, pos = fd.make_rope_axes([32, 32]), torch.zeros(2, 2)
+    for call in (lambda: fd.fd_quantize_fp8_blocks(x3, codes, scale), lambda: fd.fd_quantize_fp8_blocks(x, codes[0], scale),
+                 lambda: fd.fd_quantize_fp8_blocks(none, codes, scale), lambda: fd.fd_add_rmsnorm(x3, None, 1e-6, y=x3),
+                 lambda: fd.fd_add_rmsnorm(x, none, 1e-6, y=x), lambda: fd.fd_add_rmsnorm(x, None, 1e-6, y=x3),
+                 lambda: fd.fd_matmul_fp8_blocks(codes[None], scale, w, scale, x), lambda: fd.fd_matmul_fp8_blocks(codes, scale, w.view(-1)[0], scale, x),
+                 lambda: fd.fd_matmul_fp8_blocks(codes, scale, w, scale, x3), lambda: fd.fd_matmul_fp8_blocks(codes, scale[0], w, scale, x),
+                 lambda: fd.fd_rope_axes(spec, pos, x, x), lambda: fd.fd_rope_axes(spec, pos, none, none), lambda: fd.fd_rope_axes(spec, pos[0], x, x),
+                 lambda: fd.fd_rope_axes_tables(spec, pos, none, none), lambda: fd.fd_rope_axes_tables(spec, pos, x3, x3)):
+        with pytest.raises(fd.FlashDiffError) as e:
+            call()
+        assert e.value.status == fd.FD_ERR_INVALID_ARG
