@@ -238,10 +238,10 @@ def run(s):
     case = s["case"]
     op = case["op"]
     if op == "rope":
-        spec = fd.make_rope_axes(s["axes"], s["theta"], case["pairing"])
-        if case["form"] == "tables":
-            fd.fd_rope_axes_tables(spec, s["pos"], s["cos"], s["sin"])
+        if case["form"] == "tables":                           # (the same for either pairing; the step's tables are those of neighbours)
+            fd.fd_rope_axes_tables(fd.make_rope_axes(s["axes"], s["theta"]), s["pos"], s["cos"], s["sin"])
             return s["cos"], s["sin"]
+        spec = fd.make_rope_axes(s["axes"], s["theta"], case["pairing"])
         fd.fd_rope_axes(spec, s["pos"], s["q"], s["q_out"], s["k"], s["k_out"])
         return s["q_out"], s["k_out"]
     if op == "quantize":
