@@ -374,7 +374,8 @@ fd_status fd_region_activity_noalloc(const float* z_cur, const float* z_prev, co
  *   axis a owns axis_dim[a] channels of every head, i.e. axis_dim[a] / 2 channel pairs; the axes' pairs follow one
  *   another in the order of the axes, and pair i of axis a turns by  pos[t, a] * theta[a]^(-2 i / axis_dim[a]);
  *   FD_ROPE_INTERLEAVED: pair p is the channels (2p, 2p + 1);  FD_ROPE_HALVES: pair p is (p, p + rot / 2), where
- *   rot = the sum of axis_dim;  (a, b) -> (a cos - b sin, a sin + b cos);  channels from rot on are copied.
+ *   rot = the sum of axis_dim;  (a, b) -> (a cos - b sin, a sin + b cos);  channels from rot on are copied (a bf16 NaN as
+ *   the standard one).
  * Angles are formed and reduced in 64 bits, so positions far from the origin keep their accuracy; the rotation is fp32
  * with one rounding to the storage type.
  *   spec (HOST)  n_axes in 1..4, axis_dim positive and even with a sum of at most head_dim, theta positive and finite
@@ -418,7 +419,9 @@ fd_status fd_rope_axes_tables(const fd_rope_spec* spec, const float* pos, int64_
  *
  * fd_add_rmsnorm: residual addition and root-mean-square norm in one pass over the rows,
  *   r = x + residual,   y = r / sqrt(mean(r^2) + eps) * weight,
- * sums and norm in fp32; r is rounded only where it is stored (the norm reads the unrounded sum).
+ * sums and norm in fp32; r is rounded only where it is stored (the norm reads the unrounded sum).  The squares are fp32 too: a row
+ * whose sum of squares passes fp32's range (values around 2^64) comes out as zeros, and with eps = 0 one whose values are all
+ * below 2^-75 as infinities or NaN.
  *   x [rows, cols] of x_dtype;  residual, residual_out of residual_dtype, or NULL (no addition / sum not kept; without a
  *   residual, residual_out receives x);  weight [cols] of x_dtype or NULL (ones);  eps >= 0;
  *   y [rows, cols] of x_dtype or NULL;  y8 (E4M3 codes) with y8_scale [rows, ceil(cols / 128)] f32, or both NULL; at

@@ -253,3 +253,33 @@ def test_the_stride_of_a_single_output_row_is_free(n, stride, out):
         ref.check_codes(o, sc, v, absolute=err)
     else:
         assert bool(((o.double() - v).abs() <= err + ref.HALF_STEP[o.dtype] * (v.abs() + err)).all())
+
+
+@pytest.mark.parametrize("cols", [1536, 100])
+def test_rows_outside_the_range_of_fp32_squares(cols):
+    """What the header says of rows whose squares leave fp32's range; rows next to them are as ever."""
+    x = torch.randn(4, cols, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    x[1, 3] = 2.0 ** 65
+    x[2] = 2.0 ** -80
+    x[2, 5] = 0.0
+    y = torch.empty_like(x)
+    fd.fd_add_rmsnorm(x, None, 0.0, y=y)
+    assert bool((y[1] == 0).all()) and bool(y[2, 5].isnan()) and bool(y[2, 6:].isinf().all())
+    want, rel = ref.rmsnorm(x[[0, 3]], None, 0.0)[1], ref.rmsnorm_rel(cols)
+    assert bool(((y[[0, 3]].double() - want).abs() <= (rel + ref.U32 * (1 + rel)) * want.abs()).all())
+
+
+@pytest.mark.parametrize("pairing", ["interleaved", "halves"])
+@pytest.mark.parametrize("axes,dh", [([34], 64), ([8, 12], 64), ([36], 72)])
+def test_bf16_channels_behind_the_axes(pairing, axes, dh):
+    """Copied bit for bit, a NaN as the standard one."""
+    x = torch.randn(20, 3, dh, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
+    rot = sum(axes)
+    x[:, :, rot + 1], x[:, :, dh - 1] = float("inf"), -0.0
+    x.view(torch.int16)[:, :, rot + 3] = -63                    # a negative NaN with a payload
+    out = torch.empty_like(x)
+    fd.fd_rope_axes(fd.make_rope_axes(axes, pairing=pairing), torch.zeros(20, len(axes), device="cuda"), x, out)
+    a, b_ = x.view(torch.int16).clone(), out.view(torch.int16)
+    assert bool(out[:, :, rot + 3].isnan().all())
+    a[:, :, rot + 3] = b_[:, :, rot + 3]
+    assert torch.equal(a, b_)                                   # at position 0 the rotated channels are the same, too
