@@ -385,7 +385,8 @@ fd_status fd_region_activity_noalloc(const float* z_cur, const float* z_prev, co
  * fd_rope_axes rotates one or two sets of rows (HOST array; queries and keys), element type dtype (FD_F32 / FD_BF16):
  * row (t, h) of a set is at in + t * in_token_stride + h * in_head_stride, so slices of a fused projection's output need
  * no copy.  out may be in with the same strides (in place).  inverse != 0 turns by the negative angles: the inverse
- * map, which is also the gradient of the forward one.  An output's rows must not overlap one another: FD_ERR_SHAPE.
+ * map, which is also the gradient of the forward one.  An output's rows must not overlap one another, nor one set's output be
+ * the other's rows: FD_ERR_SHAPE.
  *
  * fd_rope_axes_tables writes the tables fd_set_block_variants takes: cos_out, sin_out [tokens, head_dim / 2] f32, pair p
  * of the interleaved pairing in column p (FD_ROPE_HALVES is refused: the step pairs neighbours), 1 and 0 behind rot / 2.

@@ -881,6 +881,9 @@ fd_status fd_rope_axes(const fd_rope_spec* spec, const float* pos, int64_t token
             return op_fail(FD_ERR_SHAPE, "%s: in place needs equal strides", who);
     }
     if (tokens == 0) return FD_OK;
+    // (what one pointer tells: the same rows given for both sets, or one set's output for the other's input)
+    if (n_sets == 2 && (sets[0].out == sets[1].out || sets[0].out == sets[1].in || sets[1].out == sets[0].in))
+        return op_fail(FD_ERR_SHAPE, "%s: the two sets share rows", who);
     return op_launched(who, launch_rope_axes(*spec, pos, tokens, head_dim, dtype, sets, n_sets, inverse != 0, static_cast<cudaStream_t>(cuda_stream)));
 }
 
@@ -978,6 +981,7 @@ fd_status matmul_fp8_call(const char* who, const fd_matmul_fp8_args* f, int m, i
     if (f->status_out && !aligned4(f->status_out)) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is misaligned", who);
     if (m == 0)
         return f->status_out ? op_launched(who, cudaMemsetAsync(f->status_out, 0, sizeof(int32_t), static_cast<cudaStream_t>(cuda_stream))) : FD_OK;
+    if (f->out == f->a8 || f->out == f->w8) return op_fail(FD_ERR_INVALID_ARG, "%s: out is an operand", who);
     try {
         std::string why;
         const cudaError_t e = launch_matmul_fp8_blocks(*f, m, n, k, starve, static_cast<cudaStream_t>(cuda_stream), &why);

@@ -87,3 +87,17 @@ def test_binding_refuses_other_numbers_of_dimensions():
         with pytest.raises(fd.FlashDiffError) as e:
             call()
         assert e.value.status == fd.FD_ERR_INVALID_ARG
+
+
+def _rope(*sets):
+    s = b.make_rope_axes([32, 32])
+    rows = (b.FdRopeRows * 2)(*[b.FdRopeRows(i, o, 256, 64, 256, 64, 4) for i, o in sets])
+    return fd.lib.fd_rope_axes(ctypes.byref(s), P, 4, 64, fd.FD_BF16, rows, 2, 0, None)
+
+
+def test_the_same_rows_in_both_roles():
+    """In place twice over the same rows, or one set's output as the other's input: which comes first is not defined."""
+    for sets in (((P, P), (P, P)), ((P, 2 * P), (3 * P, 2 * P)), ((P, 2 * P), (2 * P, 3 * P)), ((P, 2 * P), (3 * P, P))):
+        assert _rope(*sets) == fd.FD_ERR_SHAPE and "share rows" in _text()
+    assert _product(4, 256, 256, a8=2 * P, status_out=None) == fd.FD_ERR_INVALID_ARG and "operand" in _text()
+    assert _product(4, 256, 256, w8=2 * P, status_out=None) == fd.FD_ERR_INVALID_ARG and "operand" in _text()
