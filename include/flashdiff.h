@@ -45,8 +45,9 @@ typedef enum {
     FD_ERR_TIMEOUT = 7      /* a bounded device-side wait expired                           */
 } fd_status;
 
-/* FD_E4M3 is an output type of fd_matmul_fp8_blocks only; a context's storage type is one of the first two. */
-typedef enum { FD_F32 = 0, FD_BF16 = 1, FD_E4M3 = 2 } fd_dtype;
+/* FD_E4M3 is an output type of fd_matmul_fp8_blocks and fd_gated_norm, FD_I8 of fd_gated_norm; a context's storage type is
+   one of the first two. */
+typedef enum { FD_F32 = 0, FD_BF16 = 1, FD_E4M3 = 2, FD_I8 = 3 } fd_dtype;
 
 /* Which kernels run the dense contractions. */
 typedef enum {
@@ -476,6 +477,118 @@ typedef struct {
     int32_t bias_dtype, out_dtype, gelu;
 } fd_matmul_fp8_args;
 fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* args, int m, int n, int k, void* cuda_stream);
+
+/*
+ * Operators on the active rows of a step, with 8-bit integers (no counterpart in the paper: the block structure is that of the published
+ * models, the 8-bit conventions are this library's).  They are row operators like the ones above (no context, no workspace, nothing kept
+ * between calls; strides in elements; errors to fd_last_error(NULL)), and take a row count that only the device knows:
+ *   rows_used   optional DEVICE int32, read in stream order: the call works on the first min(rows, max(0, *rows_used)) rows; `rows`
+ *               (m of the product) is then their capacity.  Rows behind them are not read, and outputs there are left as they were.
+ *               fd_regional_step leaves this number at cu_active_out + B.
+ *   status_out  optional DEVICE int32 that receives, in stream order, 0, FD_ERR_STATE if an index was refused (its row is skipped:
+ *               outputs as they were), or FD_ERR_TIMEOUT if a bounded wait of the product ran out (the result is then incomplete).
+ *
+ * 8-bit integers stand for v by a scale over a set of values (a row; a token's head):
+ *   a = max(largest |v|, 2^-100),   scale = a / 127,   code = v * (127 / a) rounded to the nearest whole number, ties to even,
+ * in fp32; codes are -127 .. 127.  A set that holds a NaN or an infinity has the scale NaN and codes 0, so that it stands for NaN.
+ *
+ * fd_gated_norm: the norms behind one branch of a block and in front of the next, with the gate and the residual addition between them:
+ *   n = post(x) * post_weight,   r = residual_scale * residual + gate[g] * n,   y = pre(r) * pre_weight * (1 + scale[g]) + shift[g]
+ * post, pre: FD_NORM_NONE v, FD_NORM_RMS v / sqrt(mean(v^2) + eps), FD_NORM_LAYER (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps).
+ * FD_NORM_NONE behind and FD_NORM_LAYER in front is the step's own block, FD_NORM_RMS on both sides the sandwich form.  A row's g is
+ * (row_index ? row_index[row] : row) / rows_per_group: with the step's active_idx_out and N tokens per group, the request of the token.
+ *   x [rows, cols] of x_dtype;  residual, residual_out of residual_dtype, or NULL (no addition / r not kept);  post_weight,
+ *   pre_weight [cols] of x_dtype or NULL (ones);  gate, scale, shift [groups, cols] of mod_dtype or NULL (1, 0, 0; rows_per_group,
+ *   groups and row_index are then not looked at, if all three are NULL);  residual_scale finite;  eps >= 0
+ *   y [rows, cols] of x_dtype or NULL;  y8 of y8_dtype with y8_scale, or both NULL:  FD_I8 [rows], one scale a row;  FD_E4M3 [rows,
+ *   ceil(cols / 128)], the block form of fd_add_rmsnorm.  At least one of residual_out, y, y8 is given.
+ *   residual_out may be residual, y may be x (same strides).  A row_index outside [0, groups * rows_per_group) is refused.
+ * Sums, norms and r are fp32; r is rounded only where it is stored (the norm in front reads it unrounded).  Squares are fp32 too, with
+ * the consequences that fd_add_rmsnorm has.
+ * fd_quantize_int8_rows: the codes and scales (y8_scale [rows], contiguous) of a tensor as it is.
+ */
+typedef enum { FD_NORM_NONE = 0, FD_NORM_RMS = 1, FD_NORM_LAYER = 2 } fd_norm_kind;
+typedef struct {
+    const void* x;
+    const void* residual;
+    void* residual_out;
+    const void* post_weight;
+    const void* pre_weight;
+    const void* gate;
+    const void* scale;
+    const void* shift;
+    void* y;
+    void* y8;
+    float* y8_scale;
+    const int32_t* row_index;
+    const int32_t* rows_used;
+    int32_t* status_out;
+    int64_t x_stride, residual_stride, residual_out_stride, gate_stride, scale_stride, shift_stride, y_stride, y8_stride, y8_scale_stride;
+    int32_t x_dtype, residual_dtype, mod_dtype, y8_dtype;
+    int32_t post_norm, pre_norm; /* fd_norm_kind */
+    int32_t groups, rows_per_group;
+    float residual_scale, eps;
+} fd_gated_norm_args;
+fd_status fd_gated_norm(const fd_gated_norm_args* args, int64_t rows, int cols, void* cuda_stream);
+fd_status fd_quantize_int8_rows(const void* x, int64_t x_stride, int x_dtype, int64_t rows, int cols, void* y8, int64_t y8_stride,
+                                float* y8_scale, const int32_t* rows_used, void* cuda_stream);
+
+/*
+ * Matrix product of 8-bit integers with a scale for each token (row of a8) and each channel (row of w8):
+ *   v[i, j] = (sum over k of a8[i, k] * w8[j, k]) * a_scale[i] * w_scale[j] + bias[j],   out[i, j] = v, or tanh-GELU(v) with gelu != 0
+ * The sum is exact (32-bit integers); the rest is fp32, rounded once to out_dtype (FD_F32 / FD_BF16).
+ *   a8 [m, k], w8 [n, k]: any values of 8 bits, k contiguous; base addresses 16-byte aligned, row strides multiples of 16 bytes
+ *   a_scale [m], w_scale [n] f32;  bias [n] of bias_dtype (FD_F32 / FD_BF16) or NULL;  out [m, n], columns contiguous
+ * 0 <= m, 1 <= n, both up to 2^30 with at most 2^30 tiles, ceil(m / 128) * ceil(n / 128);  1 <= k < 2^17;  FD_ERR_SHAPE otherwise.
+ * out must not overlap the operands.
+ */
+typedef struct {
+    const void* a8;
+    const float* a_scale;
+    const void* w8;
+    const float* w_scale;
+    const void* bias;
+    void* out;
+    const int32_t* rows_used;
+    int32_t* status_out;
+    int64_t a8_stride, w8_stride, out_stride;
+    int32_t bias_dtype, out_dtype, gelu;
+} fd_matmul_int8_args;
+fd_status fd_matmul_int8(const fd_matmul_int8_args* args, int m, int n, int k, void* cuda_stream);
+
+/*
+ * Keys and values in 8-bit integers, a scale for every token and head: half the bytes of the step's bf16 cache, for requests whose state is
+ * kept while others run.  A cache has groups * tokens_per_group slots; slot s is token s % tokens_per_group of request s / tokens_per_group, the
+ * numbering of active_idx_out.  Element c of head h of slot (g, t) is
+ *   codes[g * codes_group_stride + t * codes_token_stride + h * codes_head_stride + c],   its scale
+ *   scale[g * scale_group_stride + t * scale_token_stride + h * scale_head_stride],
+ * so that [B, 2, N, heads * head_dim] as the step has it, keys and values apart, or heads outside tokens are all expressible.
+ * fd_kv_store_int8 quantises rows of storage type (dtype) into slots, fd_kv_load_int8 writes slots' values, code * scale, rounded to dtype,
+ * into rows.  Row i belongs to slot index[i], or to slot i without an index.  rows_by_slot = 0: row i lies at i * rows_token_stride
+ * (a slice of a fused projection's output); rows_by_slot = 1: at its slot's g * rows_group_stride + t * rows_token_stride (the step's
+ * kv_cache itself); head h at h * rows_head_stride from there, channels contiguous.
+ *   index [rows] int32 or NULL (rows is then at most the number of slots).  A row whose index is no slot is refused; fd_kv_store_int8 also refuses
+ *   one whose index is not above the index before it (no slot is written twice).
+ *   sets: one or two (keys and values; HOST array inside the struct) with the same shape;  head_dim 1 .. 256
+ * Slots and rows that are written must not overlap one another: FD_ERR_SHAPE unless every stride, from the smallest up, spans what is inside.
+ */
+typedef struct {
+    void* rows;                                                 /* read by the store, written by the load */
+    void* codes;
+    float* scale;
+    int64_t rows_group_stride, rows_token_stride, rows_head_stride;
+    int64_t codes_group_stride, codes_token_stride, codes_head_stride;
+    int64_t scale_group_stride, scale_token_stride, scale_head_stride;
+} fd_kv_int8_set;
+typedef struct {
+    fd_kv_int8_set sets[2];
+    const int32_t* index;
+    const int32_t* rows_used;
+    int32_t* status_out;
+    int32_t n_sets, heads, head_dim, dtype, groups, tokens_per_group, rows_by_slot;
+} fd_kv_int8_args;
+fd_status fd_kv_store_int8(const fd_kv_int8_args* args, int64_t rows, void* cuda_stream);
+fd_status fd_kv_load_int8(const fd_kv_int8_args* args, int64_t rows, void* cuda_stream);
 
 /*
  * Reads the device-side status word (synchronises `cuda_stream`).  Returns FD_OK, or the first

@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(_HERE, "libflashdiff.so")
 FD_OK = 0
 FD_ERR_INVALID_ARG, FD_ERR_SHAPE, FD_ERR_STATE, FD_ERR_WORKSPACE = 1, 2, 3, 4
 FD_ERR_UNSUPPORTED, FD_ERR_CUDA, FD_ERR_TIMEOUT = 5, 6, 7
-FD_F32, FD_BF16, FD_E4M3 = 0, 1, 2
+FD_F32, FD_BF16, FD_E4M3, FD_I8 = 0, 1, 2, 3
+FD_NORM_NONE, FD_NORM_RMS, FD_NORM_LAYER = 0, 1, 2
 FD_ROPE_INTERLEAVED, FD_ROPE_HALVES = 0, 1
 FD_ENGINE_AUTO, FD_ENGINE_SIMT, FD_ENGINE_TC = 0, 1, 2
 
@@ -28,7 +29,7 @@ EXPORTS = ["fd_workspace_bytes", "fd_create", "fd_partition_regions", "fd_region
            "fd_sched_pack", "fd_sched_form_batch", "fd_rsearch_init", "fd_rsearch_update", "fd_set_block_variants",
            "fd_set_text_stream", "fd_set_cross_attention", "fd_set_fp8_operands", "fd_debug_buffer", "fd_set_fp8_text_stream",
            "fd_rope_axes", "fd_rope_axes_tables", "fd_add_rmsnorm", "fd_quantize_fp8_blocks", "fd_matmul_fp8_blocks",
-           "fd_selftest_matmul_wait"]
+           "fd_selftest_matmul_wait", "fd_gated_norm", "fd_quantize_int8_rows", "fd_matmul_int8", "fd_kv_store_int8", "fd_kv_load_int8"]
 FD_NOALLOC_MAX_REGION_SLOTS = 16384
 PROF_GROUPS = ["activity", "compact", "adaln", "ln_modulate", "gemm_qkv", "attention", "gemm_out", "gemm_fc1",
                "gemm_fc2", "partition", "sampler", "qk_variants", "cross_attention"]
@@ -93,6 +94,33 @@ class FdMatmulFp8Args(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("a8_stride", "a_scale_stride", "w8_stride", "w_scale_stride", "out_stride",
                                               "out_scale_stride")] + \
                [(n, ctypes.c_int32) for n in ("bias_dtype", "out_dtype", "gelu")]
+
+
+class FdGatedNormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "residual_out", "post_weight", "pre_weight", "gate", "scale", "shift", "y", "y8",
+                                               "y8_scale", "row_index", "rows_used", "status_out")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "gate_stride", "scale_stride", "shift_stride",
+                                              "y_stride", "y8_stride", "y8_scale_stride")] + \
+               [(n, ctypes.c_int32) for n in ("x_dtype", "residual_dtype", "mod_dtype", "y8_dtype", "post_norm", "pre_norm", "groups",
+                                              "rows_per_group")] + [("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class FdMatmulInt8Args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("a8", "a_scale", "w8", "w_scale", "bias", "out", "rows_used", "status_out")] + \
+               [(n, ctypes.c_int64) for n in ("a8_stride", "w8_stride", "out_stride")] + \
+               [(n, ctypes.c_int32) for n in ("bias_dtype", "out_dtype", "gelu")]
+
+
+class FdKvInt8Set(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("rows", "codes", "scale")] + \
+               [(n, ctypes.c_int64) for n in ("rows_group_stride", "rows_token_stride", "rows_head_stride", "codes_group_stride",
+                                              "codes_token_stride", "codes_head_stride", "scale_group_stride", "scale_token_stride",
+                                              "scale_head_stride")]
+
+
+class FdKvInt8Args(ctypes.Structure):
+    _fields_ = [("sets", FdKvInt8Set * 2)] + [(n, ctypes.c_void_p) for n in ("index", "rows_used", "status_out")] + \
+               [(n, ctypes.c_int32) for n in ("n_sets", "heads", "head_dim", "dtype", "groups", "tokens_per_group", "rows_by_slot")]
 
 
 class FlashDiffError(RuntimeError):
@@ -169,6 +197,15 @@ def _load() -> ctypes.CDLL:
     lib.fd_matmul_fp8_blocks.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
     lib.fd_selftest_matmul_wait.restype = i32
     lib.fd_selftest_matmul_wait.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
+    lib.fd_gated_norm.restype = i32
+    lib.fd_gated_norm.argtypes = [ctypes.POINTER(FdGatedNormArgs), i64, i32, vp]
+    lib.fd_quantize_int8_rows.restype = i32
+    lib.fd_quantize_int8_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, vp, vp]
+    lib.fd_matmul_int8.restype = i32
+    lib.fd_matmul_int8.argtypes = [ctypes.POINTER(FdMatmulInt8Args), i32, i32, i32, vp]
+    for name in ("fd_kv_store_int8", "fd_kv_load_int8"):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [ctypes.POINTER(FdKvInt8Args), i64, vp]
     lib.fd_launch_count.restype = ctypes.c_int64
     lib.fd_launch_count.argtypes = [vp]
     lib.fd_destroy.restype = i32
@@ -407,14 +444,14 @@ def fd_set_fp8_operands(ctx: Context, fp8: Optional[Dict[str, "object"]], text_s
 # A call's host time is what the smallest of these operators cost, so the checks below look at every tensor once.
 # torch's names are filled in by the first of these calls (the host-side scheduler calls need no torch).
 _TYPE_CODES, _CODES_TYPES = {}, ()
-_float32 = _int32 = _current_device = _raw_stream = _on_device = None
+_float32 = _int32 = _int8 = _current_device = _raw_stream = _on_device = None
 
 
 def _torch_names():
-    global _CODES_TYPES, _float32, _int32, _current_device, _raw_stream, _on_device
+    global _CODES_TYPES, _float32, _int32, _int8, _current_device, _raw_stream, _on_device
     import torch
     _CODES_TYPES = (torch.uint8, torch.float8_e4m3fn)
-    _int32, _on_device = torch.int32, torch.cuda.device
+    _int32, _int8, _on_device = torch.int32, torch.int8, torch.cuda.device
     # (a device tensor is at hand by the time these two are called: CUDA is up)
     _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -422,10 +459,15 @@ def _torch_names():
     _float32 = torch.float32                         # last: what the calls look at
 
 
-# The two argument structs as bytes in their C layout (a ctypes structure takes five times as long to fill).
+# The argument structs as bytes in their C layout (a ctypes structure takes five times as long to fill).
 _pack_rmsnorm = _struct.Struct("7P6q2if4x").pack
 _pack_matmul = _struct.Struct("8P6q3i4x").pack
+_pack_gated_norm = _struct.Struct("14P9q8i2f").pack
+_pack_matmul_int8 = _struct.Struct("8P3q3i4x").pack
+_pack_kv = _struct.Struct("3P9q3P9q3P7i4x").pack
 assert _struct.calcsize("7P6q2if4x") == ctypes.sizeof(FdRmsnormArgs) and _struct.calcsize("8P6q3i4x") == ctypes.sizeof(FdMatmulFp8Args)
+assert _struct.calcsize("14P9q8i2f") == ctypes.sizeof(FdGatedNormArgs) and _struct.calcsize("8P3q3i4x") == ctypes.sizeof(FdMatmulInt8Args)
+assert _struct.calcsize("3P9q3P9q3P7i4x") == ctypes.sizeof(FdKvInt8Args)
 
 
 def _packed(name: str, *argtypes):
@@ -436,6 +478,10 @@ def _packed(name: str, *argtypes):
 
 _call_rmsnorm = _packed("fd_add_rmsnorm", ctypes.c_int64, ctypes.c_int)
 _call_matmul = _packed("fd_matmul_fp8_blocks", ctypes.c_int, ctypes.c_int, ctypes.c_int)
+_call_gated_norm = _packed("fd_gated_norm", ctypes.c_int64, ctypes.c_int)
+_call_matmul_int8 = _packed("fd_matmul_int8", ctypes.c_int, ctypes.c_int, ctypes.c_int)
+_call_kv_store = _packed("fd_kv_store_int8", ctypes.c_int64)
+_call_kv_load = _packed("fd_kv_load_int8", ctypes.c_int64)
 _call_matmul_selftest = _packed("fd_selftest_matmul_wait", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 
 
@@ -640,6 +686,210 @@ def fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = 
 def fd_selftest_matmul_wait(a8, a_scale, w8, w_scale, out, status_out, out_scale=None, stream=None) -> None:
     """fd_matmul_fp8_blocks without its operands' copies: every wait runs out, status_out receives FD_ERR_TIMEOUT."""
     fd_matmul_fp8_blocks(a8, a_scale, w8, w_scale, out, None, False, out_scale, status_out, stream, _call_matmul_selftest)
+
+
+# ---- operators on the active rows, with 8-bit integers ---------------------------------------------------------------
+_NORMS = {None: FD_NORM_NONE, "none": FD_NORM_NONE, "rms": FD_NORM_RMS, "layer": FD_NORM_LAYER}
+
+
+def _word(t, name: str, device: int) -> int:
+    """Address of an int32 device scalar."""
+    if t.dtype is not _int32 or t.get_device() != device or t.numel() < 1:
+        _op_fail("%s must be an int32 tensor on the operands' device" % name)
+    return t.data_ptr()
+
+
+def _index(t, name: str, rows: int, device: int) -> int:
+    if t.dtype is not _int32 or t.get_device() != device or t.dim() != 1 or t.shape[0] < rows or not (t.is_contiguous() or rows <= 1):
+        _op_fail("%s must be a contiguous int32 tensor of at least %d numbers on the operands' device" % (name, rows))
+    return t.data_ptr()
+
+
+def _vector(t, name: str, size: int, device: int, dtype) -> int:
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (size,) or not t.is_contiguous():
+        _op_fail("%s must be a contiguous [%d] tensor of %s on the operands' device" % (name, size, dtype))
+    return t.data_ptr()
+
+
+def _int8_rows(t, name: str, shape, device: int) -> int:
+    if t.dtype is not _int8:
+        _op_fail("%s must be int8, not %s" % (name, t.dtype))
+    return _rows(t, name, shape, device)
+
+
+def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1.0, post_norm="rms", post_weight=None, gate=None, pre_norm="rms",
+                  pre_weight=None, scale=None, shift=None, eps: float = 1e-6, rows_per_group=None, row_index=None, rows_used=None, y=None, y8=None,
+                  y8_scale=None, status_out=None, stream=None) -> None:
+    """n = post(x) * post_weight, r = residual_scale * residual + gate[g] * n (kept in residual_out), y = pre(r) * pre_weight * (1 + scale[g]) +
+    shift[g], on rows [rows, cols].  Norms: "rms", "layer" or None.  gate, scale, shift [groups, cols]: one type, any row stride; the row's g is
+    (row_index or the row's own number) // rows_per_group (default: rows over groups, rounded up).  Outputs y in x's type and / or y8: int8 with
+    y8_scale [rows], or E4M3 codes with y8_scale [rows, ceil(cols / 128)].  rows_used, status_out: int32 device scalars, the number of
+    rows in use and what receives 0 or FD_ERR_STATE (a row_index that is no row of any group)."""
+    if _float32 is None:
+        _torch_names()
+    shape, device, dtype = x.shape, x.get_device(), x.dtype
+    x_stride = _rows(x, "x", shape, device)
+    rows, cols = shape
+    if post_norm not in _NORMS or pre_norm not in _NORMS:
+        _op_fail("norms are \"rms\", \"layer\" or None")
+    r = ro = r_stride = ro_stride = r_type = w1 = w2 = pg = psc = psh = g_stride = sc_stride = sh_stride = mod_type = groups = per_group = 0
+    py = p8 = ps = y_stride = y8_stride = s_stride = idx = used = status = 0
+    y8_type = FD_I8
+    if residual is not None:
+        r_type, r, r_stride = _type_code(residual, "residual"), residual.data_ptr(), _rows(residual, "residual", shape, device)
+    if residual_out is not None:
+        if residual_out is residual:
+            ro, ro_stride = r, r_stride
+        else:
+            if residual is not None and residual.dtype is not residual_out.dtype:
+                _op_fail("residual and residual_out must share one type")
+            r_type, ro, ro_stride = _type_code(residual_out, "residual_out"), residual_out.data_ptr(), _rows(residual_out, "residual_out", shape, device)
+    if post_weight is not None:
+        w1 = _vector(post_weight, "post_weight", cols, device, dtype)
+    if pre_weight is not None:
+        w2 = _vector(pre_weight, "pre_weight", cols, device, dtype)
+    mod = gate if gate is not None else scale if scale is not None else shift
+    if mod is not None:
+        mod_type, mod_shape = _type_code(mod, "gate, scale and shift"), mod.shape
+        for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
+            if t is not None and t.dtype is not mod.dtype:
+                _op_fail("gate, scale and shift must share one type")
+        if len(mod_shape) != 2 or mod_shape[0] < 1 or mod_shape[1] != cols:
+            _op_fail("gate, scale and shift must be [groups, %d]" % cols)
+        groups = mod_shape[0]
+        if gate is not None:
+            pg, g_stride = gate.data_ptr(), _rows(gate, "gate", mod_shape, device)
+        if scale is not None:
+            psc, sc_stride = scale.data_ptr(), _rows(scale, "scale", mod_shape, device)
+        if shift is not None:
+            psh, sh_stride = shift.data_ptr(), _rows(shift, "shift", mod_shape, device)
+        per_group = max(1, -(-rows // groups)) if rows_per_group is None else rows_per_group
+        if not 0 < per_group < 2 ** 31:
+            _op_fail("rows_per_group must be positive")
+        if row_index is not None:
+            idx = _index(row_index, "row_index", rows, device)
+    if y is not None:
+        if y.dtype is not dtype:
+            _op_fail("y must have x's type")
+        py, y_stride = y.data_ptr(), _rows(y, "y", shape, device)
+    if (y8 is None) != (y8_scale is None):
+        _op_fail("y8 and y8_scale come together")
+    if y8 is not None:
+        p8, ps = y8.data_ptr(), y8_scale.data_ptr()
+        if y8.dtype is _int8:
+            y8_stride, s_stride = _rows(y8, "y8", shape, device), 1
+            _vector(y8_scale, "y8_scale", rows, device, _float32)
+        else:
+            y8_type, y8_stride, s_stride = FD_E4M3, _codes(y8, "y8", shape, device), _scales(y8_scale, "y8_scale", (rows, (cols + 127) // 128), device)
+    if rows_used is not None:
+        used = _word(rows_used, "rows_used", device)
+    if status_out is not None:
+        status = _word(status_out, "status_out", device)
+    if not 0.0 <= eps < 3.0e38 or not abs(residual_scale) < 3.0e38:
+        _op_fail("eps must be non-negative and finite, residual_scale finite")
+    if rows or status:
+        _op_call(device, stream, _call_gated_norm, _pack_gated_norm(
+            x.data_ptr(), r, ro, w1, w2, pg, psc, psh, py, p8, ps, idx, used, status, x_stride, r_stride, ro_stride, g_stride, sc_stride, sh_stride,
+            y_stride, y8_stride, s_stride, _type_code(x, "x"), r_type, mod_type, y8_type, _NORMS[post_norm], _NORMS[pre_norm], groups, per_group,
+            residual_scale, eps), rows, cols)
+
+
+def fd_quantize_int8_rows(x, y8, y8_scale, rows_used=None, stream=None) -> None:
+    """int8 codes y8 and scales y8_scale [rows] of x [rows, cols] (float32 or bfloat16), the first rows_used rows of them if given."""
+    if _float32 is None:
+        _torch_names()
+    shape, device = x.shape, x.get_device()
+    x_stride = _rows(x, "x", shape, device)
+    rows, cols = shape
+    args = (x.data_ptr(), x_stride, _type_code(x, "x"), rows, cols, y8.data_ptr(), _int8_rows(y8, "y8", shape, device),
+            _vector(y8_scale, "y8_scale", rows, device, _float32), 0 if rows_used is None else _word(rows_used, "rows_used", device))
+    if rows:
+        _op_call(device, stream, lib.fd_quantize_int8_rows, *args)
+
+
+def fd_matmul_int8(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = False, rows_used=None, status_out=None, stream=None,
+                   _call=_call_matmul_int8) -> None:
+    """out [m, n] = (a8 w8^T) * a_scale[:, None] * w_scale + bias, then tanh-GELU if asked.  a8 [m, k], w8 [n, k] int8 in rows of whole 16-byte
+    units; a_scale [m], w_scale [n] float32; out float32 or bfloat16.  rows_used, status_out: int32 device scalars, the number of rows in use
+    and what receives 0, or FD_ERR_TIMEOUT if a bounded wait of the kernel ran out (without it an incomplete result goes unreported)."""
+    if _float32 is None:
+        _torch_names()
+    a_shape, w_shape, device = a8.shape, w8.shape, a8.get_device()
+    a_stride = _int8_rows(a8, "a8", a_shape, device)
+    (m, k), n = a_shape, w_shape[0] if w_shape else 0
+    w_stride = _int8_rows(w8, "w8", (n, k), device)
+    if m <= 1:                                          # the stride of a single row is free: round it up to what is asked for
+        a_stride = (a_stride + 15) // 16 * 16
+    if n <= 1:
+        w_stride = (w_stride + 15) // 16 * 16
+    p_bias = bias_type = used = status = 0
+    if bias is not None:
+        bias_type = _type_code(bias, "bias")
+        p_bias = _vector(bias, "bias", n, device, bias.dtype)
+    if rows_used is not None:
+        used = _word(rows_used, "rows_used", device)
+    if status_out is not None:
+        status = _word(status_out, "status_out", device)
+    args = _pack_matmul_int8(a8.data_ptr(), _vector(a_scale, "a_scale", m, device, _float32), w8.data_ptr(),
+                             _vector(w_scale, "w_scale", n, device, _float32), p_bias, out.data_ptr(), used, status, a_stride, w_stride,
+                             _rows(out, "out", (m, n), device), bias_type, _type_code(out, "out"), 1 if gelu else 0)
+    if m or status:                                     # (without rows the call still clears the status)
+        _op_call(device, stream, _call, args, m, n, k)
+
+
+def _kv_set(rows, codes, scale, shape, dtype, count: int, device: int):
+    """A set's addresses and strides: rows [rows, heads, head_dim] or [groups, tokens, heads, head_dim]."""
+    groups, tokens, heads, dh = shape
+    if codes.dtype is not _int8 or codes.shape != shape or codes.get_device() != device:
+        _op_fail("codes must be int8 %s on device %d" % (list(shape), device))
+    if scale.dtype is not _float32 or scale.shape != shape[:3] or scale.get_device() != device:
+        _op_fail("scales must be float32 %s on device %d" % (list(shape[:3]), device))
+    if rows.dtype is not dtype or rows.get_device() != device or rows.shape[-2:] != shape[2:] or (rows.shape != shape if rows.dim() == 4 else rows.shape[0] != count):
+        _op_fail("rows must be [rows, %d, %d] or %s, of one type and the codes' device" % (heads, dh, list(shape)))
+    rs, cs, ss = rows.stride(), codes.stride(), scale.stride()
+    if dh > 1 and (rs[-1] != 1 or cs[3] != 1):
+        _op_fail("channels must be contiguous")
+    return rows.data_ptr(), codes.data_ptr(), scale.data_ptr(), rs[0] if len(rs) == 4 else 0, rs[-3], rs[-2], cs[0], cs[1], cs[2], ss[0], ss[1], ss[2]
+
+
+def _kv(call, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stream) -> None:
+    if _float32 is None:
+        _torch_names()
+    device, shape, dims = k8.get_device(), k8.shape, k.dim()
+    if len(shape) != 4 or dims not in (3, 4):
+        _op_fail("codes must be [groups, tokens, heads, head_dim], rows [rows, heads, head_dim] or the codes' shape")
+    idx = used = status = 0
+    if dims == 3:
+        rows = k.shape[0]
+    else:
+        rows = shape[0] * shape[1] if index is None else index.shape[0] if index.dim() == 1 else -1
+    if index is not None:
+        idx = _index(index, "index", rows, device)
+    if (v is None) != (v8 is None) or (v is None) != (v_scale is None) or (v is not None and v.dim() != dims):
+        _op_fail("v, v8 and v_scale come together, with k's number of dimensions")
+    first = _kv_set(k, k8, k_scale, shape, k.dtype, rows, device)
+    second = first if v is None else _kv_set(v, v8, v_scale, shape, k.dtype, rows, device)
+    if rows_used is not None:
+        used = _word(rows_used, "rows_used", device)
+    if status_out is not None:
+        status = _word(status_out, "status_out", device)
+    if shape.numel() and (rows or status):
+        _op_call(device, stream, call, _pack_kv(*first, *second, idx, used, status, 1 if v is None else 2, shape[2], shape[3], _type_code(k, "rows"),
+                                                shape[0], shape[1], 1 if dims == 4 else 0), rows)
+
+
+def fd_kv_store_int8(k, k8, k_scale, v=None, v8=None, v_scale=None, index=None, rows_used=None, status_out=None, stream=None) -> None:
+    """Quantises keys (and values) into a cache k8 [groups, tokens, heads, head_dim] int8 with k_scale [groups, tokens, heads] float32.  k: rows
+    [rows, heads, head_dim], row i for slot index[i] (slot i without an index), or [groups, tokens, heads, head_dim], of which the index's slots
+    are taken.  index: strictly ascending int32, group * tokens + token.  rows_used, status_out: int32 device scalars, the number of
+    rows in use and what receives 0 or FD_ERR_STATE (a refused index)."""
+    _kv(_call_kv_store, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stream)
+
+
+def fd_kv_load_int8(k8, k_scale, k, v8=None, v_scale=None, v=None, index=None, rows_used=None, status_out=None, stream=None) -> None:
+    """Writes the values of a cache's slots into k (and v): all of them, or the index's, into rows [rows, heads, head_dim] or at their place
+    in [groups, tokens, heads, head_dim]; arguments as in fd_kv_store_int8, the index in any order."""
+    _kv(_call_kv_load, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stream)
 
 
 def fd_sched_pack(load, cost, home):

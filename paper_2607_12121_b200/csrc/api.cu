@@ -2,6 +2,7 @@
 // queues one region-selective step (compaction, adaLN vectors, then per block: gather + LN +
 // modulation, QKV with K/V scatter, attention over all keys, out-projection, MLP, residual
 // scatter) on the caller's stream without ever reading the active count back to the host.
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -1000,6 +1001,180 @@ fd_status fd_selftest_matmul_wait(const fd_matmul_fp8_args* args, int m, int n, 
     const char* who = "fd_selftest_matmul_wait";
     if (args && !args->status_out) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is null", who);
     return matmul_fp8_call(who, args, m, n, k, true, cuda_stream);
+}
+
+// ---- operators on the active rows, with 8-bit integers ----------------------------------------------------------------
+namespace {
+fd_status op_words(const char* who, const int32_t* rows_used, const int32_t* status_out, const int32_t* index) {
+    if (!aligned4(rows_used)) return op_fail(FD_ERR_INVALID_ARG, "%s: rows_used is misaligned", who);
+    if (!aligned4(status_out)) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is misaligned", who);
+    if (!aligned4(index)) return op_fail(FD_ERR_INVALID_ARG, "%s: the index is misaligned", who);
+    if (status_out && (status_out == rows_used || status_out == index))
+        return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is an input", who);
+    return FD_OK;
+}
+// a call without rows still clears the status
+fd_status op_no_rows(const char* who, int32_t* status_out, void* cuda_stream) {
+    if (!status_out) return FD_OK;
+    return op_launched(who, cudaMemsetAsync(status_out, 0, sizeof(int32_t), static_cast<cudaStream_t>(cuda_stream)));
+}
+bool norm_kind(int k) { return k == FD_NORM_NONE || k == FD_NORM_RMS || k == FD_NORM_LAYER; }
+
+fd_status gated_norm_call(const char* who, const fd_gated_norm_args& a, int64_t rows, int cols, void* cuda_stream) {
+    if (rows < 0 || rows >= MAX_ROWS || cols < 1 || cols > (1 << 30)) return op_fail(FD_ERR_SHAPE, "%s: rows in [0, 2^31), cols in [1, 2^30]", who);
+    const bool any = rows > 0;                               // (tensors of no rows may have no memory)
+    if (any && !a.x) return op_fail(FD_ERR_INVALID_ARG, "%s: x is null", who);
+    if (any && !a.residual_out && !a.y && !a.y8) return op_fail(FD_ERR_INVALID_ARG, "%s: no output", who);
+    if (any && (a.y8 == nullptr) != (a.y8_scale == nullptr)) return op_fail(FD_ERR_INVALID_ARG, "%s: the codes and their scales come together", who);
+    if (!norm_kind(a.post_norm) || !norm_kind(a.pre_norm)) return op_fail(FD_ERR_INVALID_ARG, "%s: unknown norm", who);
+    const bool mod = a.gate || a.scale || a.shift;
+    if (!storage_type(a.x_dtype) || ((a.residual || a.residual_out) && !storage_type(a.residual_dtype)) || (mod && !storage_type(a.mod_dtype)))
+        return op_fail(FD_ERR_UNSUPPORTED, "%s: dtypes must be FD_F32 or FD_BF16", who);
+    if (a.y8 && a.y8_dtype != FD_I8 && a.y8_dtype != FD_E4M3) return op_fail(FD_ERR_UNSUPPORTED, "%s: y8_dtype must be FD_I8 or FD_E4M3", who);
+    if (!(a.eps >= 0.f) || !(a.eps < 3.0e38f)) return op_fail(FD_ERR_INVALID_ARG, "%s: eps must be non-negative and finite", who);
+    if (a.residual && !(a.residual_scale > -3.0e38f && a.residual_scale < 3.0e38f)) return op_fail(FD_ERR_INVALID_ARG, "%s: residual_scale must be finite", who);
+    if (mod) {
+        if (a.groups < 1 || a.rows_per_group < 1) return op_fail(FD_ERR_SHAPE, "%s: groups and rows_per_group must be positive", who);
+        if (!a.row_index && rows > (int64_t)a.groups * a.rows_per_group) return op_fail(FD_ERR_SHAPE, "%s: more rows than groups * rows_per_group", who);
+    }
+    const size_t xs = type_bytes(a.x_dtype), rs = type_bytes(a.residual_dtype), ms = type_bytes(a.mod_dtype);
+    if (!aligned_to(a.post_weight, xs) || !aligned_to(a.pre_weight, xs)) return op_fail(FD_ERR_INVALID_ARG, "%s: a weight is misaligned", who);
+    fd_status s = FD_OK;
+    if ((s = op_words(who, a.rows_used, a.status_out, mod ? a.row_index : nullptr)) != FD_OK) return s;
+    if ((s = op_rows(who, "x", a.x, a.x_stride, xs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "residual", a.residual, a.residual_stride, rs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "residual_out", a.residual_out, a.residual_out_stride, rs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "gate", a.gate, a.gate_stride, ms, a.groups, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "scale", a.scale, a.scale_stride, ms, a.groups, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "shift", a.shift, a.shift_stride, ms, a.groups, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "y", a.y, a.y_stride, xs, rows, cols)) != FD_OK) return s;
+    if ((s = op_rows(who, "y8", a.y8, a.y8_stride, 1, rows, cols)) != FD_OK) return s;
+    const int64_t scales = a.y8_dtype == FD_I8 ? 1 : (cols + FP8_BLOCK - 1) / FP8_BLOCK;
+    if ((s = op_rows(who, "y8_scale", a.y8_scale, a.y8_scale_stride, 4, rows, scales)) != FD_OK) return s;
+    // (what one pointer tells) in place: the residual and x, with equal strides; no output in the role of another tensor
+    if (rows > 1 && ((a.residual_out && a.residual_out == a.residual && a.residual_out_stride != a.residual_stride) ||
+                     (a.y && a.y == a.x && a.y_stride != a.x_stride)))
+        return op_fail(FD_ERR_SHAPE, "%s: in place needs equal strides", who);
+    if ((a.residual_out && (a.residual_out == a.x || a.residual_out == a.y || a.residual_out == a.y8)) || (a.y && (a.y == a.residual || a.y == a.y8)) ||
+        (a.y8 && (a.y8 == a.x || a.y8 == a.residual)))
+        return op_fail(FD_ERR_SHAPE, "%s: an output shares rows with another tensor", who);
+    if (rows == 0) return op_no_rows(who, a.status_out, cuda_stream);
+    return op_launched(who, launch_gated_norm(a, rows, cols, static_cast<cudaStream_t>(cuda_stream)));
+}
+}  // namespace
+
+fd_status fd_gated_norm(const fd_gated_norm_args* args, int64_t rows, int cols, void* cuda_stream) {
+    if (!args) return op_fail(FD_ERR_INVALID_ARG, "fd_gated_norm: args is null");
+    return gated_norm_call("fd_gated_norm", *args, rows, cols, cuda_stream);
+}
+
+fd_status fd_quantize_int8_rows(const void* x, int64_t x_stride, int x_dtype, int64_t rows, int cols, void* y8, int64_t y8_stride,
+                                float* y8_scale, const int32_t* rows_used, void* cuda_stream) {
+    fd_gated_norm_args a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.x_dtype = x_dtype;
+    a.y8 = y8;
+    a.y8_dtype = FD_I8;
+    a.y8_stride = y8_stride;
+    a.y8_scale = y8_scale;
+    a.y8_scale_stride = 1;
+    a.rows_used = rows_used;
+    return gated_norm_call("fd_quantize_int8_rows", a, rows, cols, cuda_stream);
+}
+
+namespace {
+fd_status matmul_int8_call(const char* who, const fd_matmul_int8_args* f, int m, int n, int k, void* cuda_stream) {
+    if (!f) return op_fail(FD_ERR_INVALID_ARG, "%s: args is null", who);
+    if (!f->w8 || !f->w_scale || (m != 0 && (!f->a8 || !f->a_scale || !f->out))) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
+    if (!storage_type(f->out_dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: out_dtype must be FD_F32 or FD_BF16", who);
+    if (f->bias && !storage_type(f->bias_dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: bias_dtype must be FD_F32 or FD_BF16", who);
+    if (m < 0 || n < 1 || m > (1 << 30) || n > (1 << 30)) return op_fail(FD_ERR_SHAPE, "%s: m in [0, 2^30], n in [1, 2^30]", who);
+    if (k < 1 || k >= (1 << 17)) return op_fail(FD_ERR_SHAPE, "%s: k in [1, 2^17): the sums are 32-bit integers", who);
+    if (((int64_t)m + 127) / 128 * (((int64_t)n + 127) / 128) > MAX_BLOCKS) return op_fail(FD_ERR_SHAPE, "%s: more than 2^30 tiles of 128 x 128", who);
+    if (!aligned16(f->a8) || !aligned16(f->w8)) return op_fail(FD_ERR_INVALID_ARG, "%s: a8 and w8 must be 16-byte aligned", who);
+    if (f->a8_stride % 16 || f->w8_stride % 16 || f->a8_stride < k || f->w8_stride < k || f->a8_stride >= MAX_STRIDE || f->w8_stride >= MAX_STRIDE)
+        return op_fail(FD_ERR_SHAPE, "%s: the strides of a8 and w8 must be multiples of 16, at least k and below 2^40", who);
+    if (!aligned4(f->a_scale) || !aligned4(f->w_scale)) return op_fail(FD_ERR_INVALID_ARG, "%s: the scales are misaligned", who);
+    if (f->bias && !aligned_to(f->bias, type_bytes(f->bias_dtype))) return op_fail(FD_ERR_INVALID_ARG, "%s: bias is misaligned", who);
+    fd_status s = FD_OK;
+    if ((s = op_rows(who, "out", f->out, f->out_stride, type_bytes(f->out_dtype), m, n)) != FD_OK) return s;
+    if ((s = op_words(who, f->rows_used, f->status_out, nullptr)) != FD_OK) return s;
+    if (m == 0) return op_no_rows(who, f->status_out, cuda_stream);
+    if (f->out == f->a8 || f->out == f->w8) return op_fail(FD_ERR_INVALID_ARG, "%s: out is an operand", who);
+    try {
+        std::string why;
+        const cudaError_t e = launch_matmul_int8(*f, m, n, k, static_cast<cudaStream_t>(cuda_stream), &why);
+        return op_launched(who, e, why);
+    } catch (...) {
+        return op_fail(FD_ERR_CUDA, "%s: out of host memory", who);
+    }
+}
+}  // namespace
+
+fd_status fd_matmul_int8(const fd_matmul_int8_args* args, int m, int n, int k, void* cuda_stream) {
+    return matmul_int8_call("fd_matmul_int8", args, m, n, k, cuda_stream);
+}
+
+namespace {
+struct Axis { int64_t size, stride; };
+// Elements lie apart: every stride, from the smallest up, spans what is inside it.
+bool lie_apart(Axis* ax, int n, int64_t width) {
+    std::sort(ax, ax + n, [](const Axis& p, const Axis& q) { return p.stride < q.stride; });
+    __int128 span = width;
+    for (int i = 0; i < n; ++i) {
+        if (ax[i].size <= 1) continue;
+        if (ax[i].stride < span) return false;
+        span += (__int128)ax[i].stride * (ax[i].size - 1);
+    }
+    return true;
+}
+fd_status kv_call(const char* who, const fd_kv_int8_args* a, int64_t rows, bool store, void* cuda_stream) {
+    if (!a) return op_fail(FD_ERR_INVALID_ARG, "%s: args is null", who);
+    if (a->n_sets < 1 || a->n_sets > 2) return op_fail(FD_ERR_INVALID_ARG, "%s: one or two sets", who);
+    if (!storage_type(a->dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: dtype must be FD_F32 or FD_BF16", who);
+    if (rows < 0 || rows >= MAX_ROWS) return op_fail(FD_ERR_SHAPE, "%s: rows in [0, 2^31)", who);
+    if (a->heads < 1 || a->heads > 65536 || a->head_dim < 1 || a->head_dim > 256) return op_fail(FD_ERR_SHAPE, "%s: heads in 1 .. 65536, head_dim in 1 .. 256", who);
+    if (a->groups < 1 || a->tokens_per_group < 1 || (int64_t)a->groups * a->tokens_per_group >= MAX_ROWS)
+        return op_fail(FD_ERR_SHAPE, "%s: groups and tokens_per_group positive, fewer than 2^31 slots", who);
+    if (!a->index && rows > (int64_t)a->groups * a->tokens_per_group) return op_fail(FD_ERR_SHAPE, "%s: more rows than slots", who);
+    fd_status s = FD_OK;
+    if ((s = op_words(who, a->rows_used, a->status_out, a->index)) != FD_OK) return s;
+    for (int i = 0; i < a->n_sets; ++i) {
+        const fd_kv_int8_set& k = a->sets[i];
+        if (!k.codes || !k.scale || (rows > 0 && !k.rows)) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
+        if (!aligned_to(k.rows, type_bytes(a->dtype)) || !aligned4(k.scale)) return op_fail(FD_ERR_INVALID_ARG, "%s: rows or scales are misaligned", who);
+        const int64_t st[9] = {k.rows_group_stride, k.rows_token_stride, k.rows_head_stride, k.codes_group_stride, k.codes_token_stride,
+                               k.codes_head_stride, k.scale_group_stride, k.scale_token_stride, k.scale_head_stride};
+        for (int64_t v : st)
+            if (v < 0 || v > MAX_STRIDE) return op_fail(FD_ERR_SHAPE, "%s: strides must be in [0, 2^40]", who);
+        const int64_t g = a->groups, t = a->tokens_per_group, h = a->heads;
+        Axis codes[3] = {{g, k.codes_group_stride}, {t, k.codes_token_stride}, {h, k.codes_head_stride}};
+        Axis scale[3] = {{g, k.scale_group_stride}, {t, k.scale_token_stride}, {h, k.scale_head_stride}};
+        Axis by_slot[3] = {{g, k.rows_group_stride}, {t, k.rows_token_stride}, {h, k.rows_head_stride}};
+        Axis compact[2] = {{rows, k.rows_token_stride}, {h, k.rows_head_stride}};
+        if (store ? !lie_apart(codes, 3, a->head_dim) || !lie_apart(scale, 3, 1)
+                  : !(a->rows_by_slot ? lie_apart(by_slot, 3, a->head_dim) : lie_apart(compact, 2, a->head_dim)))
+            return op_fail(FD_ERR_SHAPE, "%s: what is written overlaps", who);
+        if (k.rows == k.codes || k.rows == (const void*)k.scale || k.codes == (const void*)k.scale) return op_fail(FD_ERR_SHAPE, "%s: a set's tensors share memory", who);
+    }
+    if (a->n_sets == 2) {                                        // (what one pointer tells)
+        const fd_kv_int8_set &p = a->sets[0], &q = a->sets[1];
+        if (store ? p.codes == q.codes || p.scale == q.scale || p.codes == q.rows || q.codes == p.rows
+                  : rows > 0 && (p.rows == q.rows || p.rows == q.codes || q.rows == p.codes))
+            return op_fail(FD_ERR_SHAPE, "%s: the two sets share rows", who);
+    }
+    if (rows == 0) return op_no_rows(who, a->status_out, cuda_stream);
+    return op_launched(who, launch_kv_int8(*a, rows, store, static_cast<cudaStream_t>(cuda_stream)));
+}
+}  // namespace
+
+fd_status fd_kv_store_int8(const fd_kv_int8_args* args, int64_t rows, void* cuda_stream) {
+    return kv_call("fd_kv_store_int8", args, rows, true, cuda_stream);
+}
+
+fd_status fd_kv_load_int8(const fd_kv_int8_args* args, int64_t rows, void* cuda_stream) {
+    return kv_call("fd_kv_load_int8", args, rows, false, cuda_stream);
 }
 
 fd_status fd_poll_status(fd_ctx* c, void* cuda_stream) {

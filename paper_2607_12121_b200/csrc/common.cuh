@@ -62,6 +62,30 @@ constexpr int FP8_BLOCK = 128;
 constexpr float E4M3_MAX = 448.0f;
 constexpr float FP8_AMAX_FLOOR = 0x1p-100f;
 
+// 8-bit integers with a scale over a set of values, from the bit pattern of the largest magnitude: patterns of magnitudes are ordered like
+// the magnitudes, NaN above infinity above all numbers, so a maximum over them also says whether every value is a number.
+constexpr float I8_MAX = 127.0f, I8_AMAX_FLOOR = 0x1p-100f;
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+struct I8Scale {
+    float scale, inv;
+    // nearest whole number, ties to even: |v * inv| is at most 127 and a rounding, and inv = 0 stands for a set that has no codes
+    __device__ __forceinline__ uint8_t code(float v) const { return (uint8_t)(inv == 0.f ? 0 : __float2int_rn(v * inv)); }
+};
+__device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
+    if (amax_bits >= 0x7f800000u) return {__uint_as_float(0x7fffffffu), 0.f};
+    const float a = fmaxf(__uint_as_float(amax_bits), I8_AMAX_FLOOR);
+    return {a / I8_MAX, I8_MAX / a};
+}
+
+// Rows a call works on: a capacity, and optionally a count that only the device knows.
+__device__ __forceinline__ long long used_rows(long long rows, const int32_t* used) {
+    return used ? min(rows, (long long)max(0, *used)) : rows;
+}
+// First device-side problem of a call without a context.
+__device__ __forceinline__ void report_status(int32_t* status, int code) {
+    if (status) atomicCAS(status, 0, code);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -217,6 +241,15 @@ cudaError_t launch_row_blocks(const fd_rmsnorm_args& a, int64_t rows, int cols, 
 
 // tc_gemm_blocks.cu (starve: the self-test's form, which issues no copies)
 cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& a, int m, int n, int k, bool starve, cudaStream_t st, std::string* why);
+
+// gated_norm.cu: norm, gate, residual addition, norm, modulation; 8-bit integers of rows (quantize_int8: no norm, no addition)
+cudaError_t launch_gated_norm(const fd_gated_norm_args& a, int64_t rows, int cols, cudaStream_t st);
+
+// kv_int8.cu
+cudaError_t launch_kv_int8(const fd_kv_int8_args& a, int64_t rows, bool store, cudaStream_t st);
+
+// gemm_int8.cu
+cudaError_t launch_matmul_int8(const fd_matmul_int8_args& a, int m, int n, int k, cudaStream_t st, std::string* why);
 
 // partition.cu
 size_t partition_scratch_bytes(int max_batch, int max_tokens, int max_regions);
