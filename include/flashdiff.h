@@ -610,6 +610,9 @@ fd_status fd_selftest_bounded_wait(fd_ctx* ctx, void* cuda_stream);
  */
 fd_status fd_selftest_matmul_wait(const fd_matmul_fp8_args* args, int m, int n, int k, void* cuda_stream);
 
+/* The same for fd_matmul_int8. */
+fd_status fd_selftest_matmul_int8_wait(const fd_matmul_int8_args* args, int m, int n, int k, void* cuda_stream);
+
 /* Number of kernels the library has launched through this context so far (host counter). */
 int64_t fd_launch_count(const fd_ctx* ctx);
 

@@ -29,7 +29,8 @@ EXPORTS = ["fd_workspace_bytes", "fd_create", "fd_partition_regions", "fd_region
            "fd_sched_pack", "fd_sched_form_batch", "fd_rsearch_init", "fd_rsearch_update", "fd_set_block_variants",
            "fd_set_text_stream", "fd_set_cross_attention", "fd_set_fp8_operands", "fd_debug_buffer", "fd_set_fp8_text_stream",
            "fd_rope_axes", "fd_rope_axes_tables", "fd_add_rmsnorm", "fd_quantize_fp8_blocks", "fd_matmul_fp8_blocks",
-           "fd_selftest_matmul_wait", "fd_gated_norm", "fd_quantize_int8_rows", "fd_matmul_int8", "fd_kv_store_int8", "fd_kv_load_int8"]
+           "fd_selftest_matmul_wait", "fd_gated_norm", "fd_quantize_int8_rows", "fd_matmul_int8", "fd_kv_store_int8", "fd_kv_load_int8",
+           "fd_selftest_matmul_int8_wait"]
 FD_NOALLOC_MAX_REGION_SLOTS = 16384
 PROF_GROUPS = ["activity", "compact", "adaln", "ln_modulate", "gemm_qkv", "attention", "gemm_out", "gemm_fc1",
                "gemm_fc2", "partition", "sampler", "qk_variants", "cross_attention"]
@@ -203,6 +204,8 @@ def _load() -> ctypes.CDLL:
     lib.fd_quantize_int8_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, vp, vp]
     lib.fd_matmul_int8.restype = i32
     lib.fd_matmul_int8.argtypes = [ctypes.POINTER(FdMatmulInt8Args), i32, i32, i32, vp]
+    lib.fd_selftest_matmul_int8_wait.restype = i32
+    lib.fd_selftest_matmul_int8_wait.argtypes = [ctypes.POINTER(FdMatmulInt8Args), i32, i32, i32, vp]
     for name in ("fd_kv_store_int8", "fd_kv_load_int8"):
         getattr(lib, name).restype = i32
         getattr(lib, name).argtypes = [ctypes.POINTER(FdKvInt8Args), i64, vp]
@@ -480,6 +483,7 @@ _call_rmsnorm = _packed("fd_add_rmsnorm", ctypes.c_int64, ctypes.c_int)
 _call_matmul = _packed("fd_matmul_fp8_blocks", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 _call_gated_norm = _packed("fd_gated_norm", ctypes.c_int64, ctypes.c_int)
 _call_matmul_int8 = _packed("fd_matmul_int8", ctypes.c_int, ctypes.c_int, ctypes.c_int)
+_call_matmul_int8_selftest = _packed("fd_selftest_matmul_int8_wait", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 _call_kv_store = _packed("fd_kv_store_int8", ctypes.c_int64)
 _call_kv_load = _packed("fd_kv_load_int8", ctypes.c_int64)
 _call_matmul_selftest = _packed("fd_selftest_matmul_wait", ctypes.c_int, ctypes.c_int, ctypes.c_int)
@@ -835,6 +839,11 @@ def fd_matmul_int8(a8, a_scale, w8, w_scale, out, bias=None, gelu: bool = False,
                              _rows(out, "out", (m, n), device), bias_type, _type_code(out, "out"), 1 if gelu else 0)
     if m or status:                                     # (without rows the call still clears the status)
         _op_call(device, stream, _call, args, m, n, k)
+
+
+def fd_selftest_matmul_int8_wait(a8, a_scale, w8, w_scale, out, status_out, stream=None) -> None:
+    """fd_matmul_int8 without its operands' copies: every wait runs out, status_out receives FD_ERR_TIMEOUT."""
+    fd_matmul_int8(a8, a_scale, w8, w_scale, out, None, False, None, status_out, stream, _call_matmul_int8_selftest)
 
 
 def _kv_set(rows, codes, scale, shape, dtype, count: int, device: int):

@@ -1084,7 +1084,7 @@ fd_status fd_quantize_int8_rows(const void* x, int64_t x_stride, int x_dtype, in
 }
 
 namespace {
-fd_status matmul_int8_call(const char* who, const fd_matmul_int8_args* f, int m, int n, int k, void* cuda_stream) {
+fd_status matmul_int8_call(const char* who, const fd_matmul_int8_args* f, int m, int n, int k, bool starve, void* cuda_stream) {
     if (!f) return op_fail(FD_ERR_INVALID_ARG, "%s: args is null", who);
     if (!f->w8 || !f->w_scale || (m != 0 && (!f->a8 || !f->a_scale || !f->out))) return op_fail(FD_ERR_INVALID_ARG, "%s: null pointer argument", who);
     if (!storage_type(f->out_dtype)) return op_fail(FD_ERR_UNSUPPORTED, "%s: out_dtype must be FD_F32 or FD_BF16", who);
@@ -1104,7 +1104,7 @@ fd_status matmul_int8_call(const char* who, const fd_matmul_int8_args* f, int m,
     if (f->out == f->a8 || f->out == f->w8) return op_fail(FD_ERR_INVALID_ARG, "%s: out is an operand", who);
     try {
         std::string why;
-        const cudaError_t e = launch_matmul_int8(*f, m, n, k, static_cast<cudaStream_t>(cuda_stream), &why);
+        const cudaError_t e = launch_matmul_int8(*f, m, n, k, starve, static_cast<cudaStream_t>(cuda_stream), &why);
         return op_launched(who, e, why);
     } catch (...) {
         return op_fail(FD_ERR_CUDA, "%s: out of host memory", who);
@@ -1113,7 +1113,13 @@ fd_status matmul_int8_call(const char* who, const fd_matmul_int8_args* f, int m,
 }  // namespace
 
 fd_status fd_matmul_int8(const fd_matmul_int8_args* args, int m, int n, int k, void* cuda_stream) {
-    return matmul_int8_call("fd_matmul_int8", args, m, n, k, cuda_stream);
+    return matmul_int8_call("fd_matmul_int8", args, m, n, k, false, cuda_stream);
+}
+
+fd_status fd_selftest_matmul_int8_wait(const fd_matmul_int8_args* args, int m, int n, int k, void* cuda_stream) {
+    const char* who = "fd_selftest_matmul_int8_wait";
+    if (args && !args->status_out) return op_fail(FD_ERR_INVALID_ARG, "%s: status_out is null", who);
+    return matmul_int8_call(who, args, m, n, k, true, cuda_stream);
 }
 
 namespace {

@@ -70,11 +70,24 @@ struct I8Scale {
     float scale, inv;
     // nearest whole number, ties to even: |v * inv| is at most 127 and a rounding, and inv = 0 stands for a set that has no codes
     __device__ __forceinline__ uint8_t code(float v) const { return (uint8_t)(inv == 0.f ? 0 : __float2int_rn(v * inv)); }
+    // four codes, the first in the low byte: 1.5 * 2^23 added to a number this small leaves it, rounded, in the low bits
+    __device__ __forceinline__ uint32_t code4(const float* v) const {
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.0f));
+        const uint32_t q = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+        return inv == 0.f ? 0u : q;
+    }
 };
 __device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
     if (amax_bits >= 0x7f800000u) return {__uint_as_float(0x7fffffffu), 0.f};
     const float a = fmaxf(__uint_as_float(amax_bits), I8_AMAX_FLOOR);
     return {a / I8_MAX, I8_MAX / a};
+}
+
+// the value of code i (0 .. 3) of four: with its sign bit flipped a code lies 128 above itself, in the low bits of 2^23
+__device__ __forceinline__ float i8_value(uint32_t q, int i) {
+    return __uint_as_float(__byte_perm(q ^ 0x80808080u, 0x4B000000u, 0x7540 + i)) - 8388736.0f;
 }
 
 // Rows a call works on: a capacity, and optionally a count that only the device knows.
@@ -248,8 +261,8 @@ cudaError_t launch_gated_norm(const fd_gated_norm_args& a, int64_t rows, int col
 // kv_int8.cu
 cudaError_t launch_kv_int8(const fd_kv_int8_args& a, int64_t rows, bool store, cudaStream_t st);
 
-// gemm_int8.cu
-cudaError_t launch_matmul_int8(const fd_matmul_int8_args& a, int m, int n, int k, cudaStream_t st, std::string* why);
+// tc_gemm_int8.cu (starve: the self-test's form, which issues no copies)
+cudaError_t launch_matmul_int8(const fd_matmul_int8_args& a, int m, int n, int k, bool starve, cudaStream_t st, std::string* why);
 
 // partition.cu
 size_t partition_scratch_bytes(int max_batch, int max_tokens, int max_regions);

@@ -2,10 +2,22 @@
 // Bound by memory: 3 bytes a bf16 value either way, and 4 bytes a head for its scale.
 #include "common.cuh"
 #include "ptx.cuh"
+#include "row_vec.cuh"
 
 namespace fd {
 
 namespace {
+
+// Quotient by a number below 2^31 of one below 2^31: with 2^(31 + s) < d * m <= 2^(31 + s) + 2^s, s the bits of d - 1, the product's
+// excess over the quotient is below 1 / d for every such n.
+struct Divisor {
+    uint32_t d, mul, shift;
+    __host__ explicit Divisor(uint32_t by) : d(by), mul(0), shift(0) {
+        while ((1ull << shift) < by) ++shift;
+        mul = (uint32_t)(((1ull << (31 + shift)) + by - 1) / by);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return d == 1 ? n : (uint32_t)(((unsigned long long)n * mul) >> (31 + shift)); }
+};
 
 struct KvArgs {
     fd_kv_int8_set sets[2];
@@ -14,6 +26,7 @@ struct KvArgs {
     int32_t* status;
     long long rows, slots;
     int heads, dh, tokens, by_slot;
+    Divisor by_heads, by_tokens;
 };
 
 // The slot of row i, or -1 where its index is refused.
@@ -22,6 +35,89 @@ __device__ __forceinline__ long long kv_slot(const KvArgs& a, long long i, bool 
     const long long s = a.index[i];
     if (s < 0 || s >= a.slots || (ascending && i > 0 && a.index[i - 1] >= s)) return -1;
     return s;
+}
+
+// Head dims of whole 16-byte units: LANES lanes hold one head, NU units of 8 channels each; keys and values of a head are in flight together.
+template <typename T, bool STORE, int LANES, int NU>
+__global__ void __launch_bounds__(256) kv_kernel(KvArgs a, int n_sets) {
+    const int l = threadIdx.x % LANES, units = a.dh / 8;
+    const unsigned group_mask = LANES == 32 ? 0xffffffffu : ((1u << LANES) - 1) << ((threadIdx.x & 31) / LANES * LANES);
+    ptx::pdl_wait();
+    const uint32_t items = (uint32_t)(used_rows(a.rows, a.rows_used) * a.heads);       // (below 2^31: the launcher has checked)
+    constexpr int HPC = 256 / LANES;                        // heads of a CTA
+    for (uint32_t w = blockIdx.x * HPC + threadIdx.x / LANES; w < items; w += gridDim.x * HPC) {
+        const uint32_t i = a.by_heads.of(w);
+        const int h = (int)(w - i * a.heads);
+        const long long slot = kv_slot(a, i, STORE);
+        if (slot < 0) {
+            if (l == 0 && h == 0) report_status(a.status, FD_ERR_STATE);
+            continue;
+        }
+        const uint32_t g = a.by_tokens.of((uint32_t)slot), t = (uint32_t)slot - g * a.tokens;
+        T* row[2];
+        int8_t* codes[2];
+        float* scale[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const fd_kv_int8_set& k = a.sets[s];
+            row[s] = static_cast<T*>(k.rows) + (a.by_slot ? g * k.rows_group_stride + t * k.rows_token_stride : i * k.rows_token_stride) + h * k.rows_head_stride;
+            codes[s] = static_cast<int8_t*>(k.codes) + g * k.codes_group_stride + t * k.codes_token_stride + h * k.codes_head_stride;
+            scale[s] = k.scale + g * k.scale_group_stride + t * k.scale_token_stride + h * k.scale_head_stride;
+        }
+        if constexpr (STORE) {
+            Raw8<T> x[2][NU];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s < n_sets)
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+                        if (l + u * LANES < units) x[s][u].load_stream(row[s] + (l + u * LANES) * 8);
+                        else x[s][u].set(0.f);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s >= n_sets) break;
+                float v[NU][8];
+                uint32_t m = 0;
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    x[s][u].get(v[u]);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) m = max(m, abs_bits(v[u][c]));
+                }
+#pragma unroll
+                for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(group_mask, m, o));
+                const I8Scale i8 = i8_scale(m);
+                if (l == 0) *scale[s] = i8.scale;
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+                    if (l + u * LANES < units) *reinterpret_cast<uint2*>(codes[s] + (l + u * LANES) * 8) = make_uint2(i8.code4(v[u]), i8.code4(v[u] + 4));
+            }
+        } else {
+            uint2 q[2][NU];
+            float f[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s < n_sets) {
+                    f[s] = *scale[s];
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+                        if (l + u * LANES < units) q[s][u] = *reinterpret_cast<const uint2*>(codes[s] + (l + u * LANES) * 8);
+                }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s >= n_sets) break;
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    if (l + u * LANES >= units) continue;
+                    float v[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[c] = i8_value((c < 4 ? q[s][u].x : q[s][u].y), c & 3) * f[s];
+                    store8<T>(row[s] + (l + u * LANES) * 8, v);
+                }
+            }
+        }
+    }
+    ptx::pdl_trigger();
 }
 
 // Any head dim, stride and alignment: a warp a head, four channels a lane and turn.
@@ -64,20 +160,47 @@ __global__ void __launch_bounds__(256) kv_any_kernel(KvArgs a) {
     ptx::pdl_trigger();
 }
 
+template <typename T, bool STORE, int LANES, int NU>
+cudaError_t launch_lanes(const KvArgs& a, int n_sets, cudaStream_t st) {
+    const long long ctas = (a.rows * a.heads + 256 / LANES - 1) / (256 / LANES);
+    return ptx::launch_kernel(kv_kernel<T, STORE, LANES, NU>, (int)min(ctas, 148LL * 16), 256, 0, st, a.status == nullptr, a, n_sets);
+}
+
+template <typename T, bool STORE>
+cudaError_t launch_typed(const KvArgs& a, int n_sets, cudaStream_t st) {
+    bool fast = a.dh % 8 == 0 && a.rows * a.heads < 1LL << 31;
+    for (int i = 0; i < n_sets; ++i) {
+        const fd_kv_int8_set& k = a.sets[i];
+        const long long rows = k.rows_head_stride | k.rows_token_stride | (a.by_slot ? k.rows_group_stride : 0);
+        const long long codes = k.codes_head_stride | k.codes_token_stride | k.codes_group_stride;
+        fast = fast && (reinterpret_cast<uintptr_t>(k.rows) & 15) == 0 && rows * (long long)sizeof(T) % 16 == 0 &&
+               (reinterpret_cast<uintptr_t>(k.codes) & 7) == 0 && codes % 8 == 0;
+    }
+    if (!fast) {
+        const dim3 grid((unsigned)min((a.rows * a.heads + 7) / 8, 148LL * 16), n_sets);
+        return ptx::launch_kernel(kv_any_kernel<T, STORE>, grid, 256, 0, st, a.status == nullptr, a);
+    }
+    // 128-byte lines of bf16 for head dims of 64 and its multiples; four lanes and enough units for the others (72: 9 of 12)
+    if (a.dh == 64) return launch_lanes<T, STORE, 8, 1>(a, n_sets, st);
+    if (a.dh == 128) return launch_lanes<T, STORE, 8, 2>(a, n_sets, st);
+    if (a.dh <= 32) return launch_lanes<T, STORE, 4, 1>(a, n_sets, st);
+    if (a.dh <= 96) return launch_lanes<T, STORE, 4, 3>(a, n_sets, st);
+    if (a.dh <= 192) return launch_lanes<T, STORE, 8, 3>(a, n_sets, st);
+    return launch_lanes<T, STORE, 8, 4>(a, n_sets, st);
+}
+
 }  // namespace
 
 cudaError_t launch_kv_int8(const fd_kv_int8_args& f, int64_t rows, bool store, cudaStream_t st) {
-    KvArgs a{{f.sets[0], f.n_sets > 1 ? f.sets[1] : f.sets[0]}, f.index, f.rows_used, f.status_out, rows, (long long)f.groups * f.tokens_per_group,
-             f.heads, f.head_dim, f.tokens_per_group, f.rows_by_slot};
+    const KvArgs a{{f.sets[0], f.n_sets > 1 ? f.sets[1] : f.sets[0]}, f.index, f.rows_used, f.status_out, rows, (long long)f.groups * f.tokens_per_group,
+                   f.heads, f.head_dim, f.tokens_per_group, f.rows_by_slot, Divisor(f.heads), Divisor(f.tokens_per_group)};
     if (f.status_out) {
         const cudaError_t e = cudaMemsetAsync(f.status_out, 0, sizeof(int32_t), st);
         if (e != cudaSuccess) return e;
     }
-    const dim3 grid((unsigned)min((long long)(rows * f.heads + 7) / 8, 148LL * 16), f.n_sets);
-    const bool pdl = f.status_out == nullptr;
     using bf = __nv_bfloat16;
-    if (f.dtype == FD_BF16) return ptx::launch_kernel(store ? kv_any_kernel<bf, true> : kv_any_kernel<bf, false>, grid, 256, 0, st, pdl, a);
-    return ptx::launch_kernel(store ? kv_any_kernel<float, true> : kv_any_kernel<float, false>, grid, 256, 0, st, pdl, a);
+    if (f.dtype == FD_BF16) return store ? launch_typed<bf, true>(a, f.n_sets, st) : launch_typed<bf, false>(a, f.n_sets, st);
+    return store ? launch_typed<float, true>(a, f.n_sets, st) : launch_typed<float, false>(a, f.n_sets, st);
 }
 
 }  // namespace fd

@@ -222,3 +222,15 @@ def test_first_call_of_a_process_may_be_captured(size):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", _FIRST_CAPTURED.format(size=size)], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("m,n", [(8, 512), (300, 384), (9400, 1024), (16380, 2048)])
+def test_waits_are_bounded(m, n):
+    """The product's kernels with a loader that fetches nothing: every wait runs out, the status says so, and the next call is whole."""
+    (a8, a_s), (w8, w_s) = _operand(m, 1536, 1), _operand(n, 1536, 2)
+    out, status = torch.empty(m, n, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    fd.fd_selftest_matmul_int8_wait(a8, a_s, w8, w_s, out, status)
+    assert int(status) == fd.FD_ERR_TIMEOUT
+    fd.fd_matmul_int8(a8, a_s, w8, w_s, out, status_out=status)
+    assert int(status) == 0
+    _check(out, *ref.matmul(a8, a_s, w8, w_s))
