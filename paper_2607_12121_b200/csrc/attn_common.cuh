@@ -22,7 +22,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// ---- two fp32 values per instruction (add/sub/fma .f32x2) --------------------------------------------
+// ---- two fp32 values per instruction (add/sub/mul/fma .f32x2) --------------------------------------------
 __device__ __forceinline__ uint64_t pair(float a, float b) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
@@ -32,6 +32,11 @@ __device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mo
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {

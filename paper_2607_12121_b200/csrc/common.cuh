@@ -10,6 +10,7 @@
 #include <string>
 
 #include "../../include/flashdiff.h"
+#include "attn_common.cuh"
 
 namespace fd {
 
@@ -72,10 +73,22 @@ struct I8Scale {
     __device__ __forceinline__ uint8_t code(float v) const { return (uint8_t)(inv == 0.f ? 0 : __float2int_rn(v * inv)); }
     // four codes, the first in the low byte: 1.5 * 2^23 added to a number this small leaves it, rounded, in the low bits
     __device__ __forceinline__ uint32_t code4(const float* v) const {
-        uint32_t b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.0f));
-        const uint32_t q = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+        return pack(__fadd_rn(__fmul_rn(v[0], inv), 12582912.0f), __fadd_rn(__fmul_rn(v[1], inv), 12582912.0f),
+                    __fadd_rn(__fmul_rn(v[2], inv), 12582912.0f), __fadd_rn(__fmul_rn(v[3], inv), 12582912.0f));
+    }
+    // the same of two packed pairs (products one by one: a packed product and the addition behind it would become one operation with one
+    // rounding, and v = a / 2, common in bf16, then 63.4999 instead of 63.5)
+    __device__ __forceinline__ uint32_t code4(const uint64_t* v) const {
+        const uint64_t magic = attn::pair(12582912.0f, 12582912.0f);
+        float b[4];
+        attn::unpair(v[0], b[0], b[1]);
+        attn::unpair(v[1], b[2], b[3]);
+        attn::unpair(attn::add2(attn::pair(__fmul_rn(b[0], inv), __fmul_rn(b[1], inv)), magic), b[0], b[1]);
+        attn::unpair(attn::add2(attn::pair(__fmul_rn(b[2], inv), __fmul_rn(b[3], inv)), magic), b[2], b[3]);
+        return pack(b[0], b[1], b[2], b[3]);
+    }
+    __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) const {
+        const uint32_t q = __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
         return inv == 0.f ? 0u : q;
     }
 };

@@ -2,7 +2,10 @@
 // the rows:  n = post(x) * post_weight,  r = residual_scale * residual + gate[g] * n,  y = pre(r) * pre_weight * (1 + scale[g]) + shift[g],
 // y in the storage type and / or as 8-bit integers with a scale per row or E4M3 codes with a scale per 128 columns.
 // Bound by memory: every element of x and the residual is read once, r and y are written once.
+#include <atomic>
+
 #include "common.cuh"
+#include "gemm_8bit.cuh"
 #include "ptx.cuh"
 #include "row_vec.cuh"
 
@@ -46,35 +49,66 @@ template <int RPC, int THREADS> __device__ __forceinline__ void row_barrier(int 
     else asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
-// eight values of a conditioning vector (of a few rows that every CTA reads again and again: they come out of the first-level cache)
-__device__ __forceinline__ void load8_mod(const void* p, bool bf16, long long at, float* f) {
-    if (bf16) {
-        Raw8<__nv_bfloat16> r;
-        r.load(static_cast<const __nv_bfloat16*>(p) + at);
-        r.get(f);
-    } else {
-        Raw8<float> r;
-        r.load(static_cast<const float*>(p) + at);
-        r.get(f);
+// Four values of a conditioning vector of either type
+struct RawMod {
+    uint4 q;                                                // bf16: the first half
+    __device__ __forceinline__ void load(const void* p, bool bf16, long long at) {
+        if (bf16) {
+            const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + at);
+            q.x = h.x;
+            q.y = h.y;
+        } else {
+            q = *reinterpret_cast<const uint4*>(static_cast<const float*>(p) + at);
+        }
     }
+    __device__ __forceinline__ void get(bool bf16, uint64_t* v) const {
+        if (bf16) Raw4<__nv_bfloat16>{make_uint2(q.x, q.y)}.get(v);
+        else Raw4<float>{q}.get(v);
+    }
+};
+
+// magnitudes: the larger of three, NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+    return d;
 }
 
-// W warps hold one row, NV vectors of 8 columns per lane (cols <= 256 W NV, a multiple of 8); 16 lanes hold one block of 128 columns.  CTAs
-// stay and walk the rows; the next row's values are requested as soon as the registers of the present one's are free.
-template <typename TX, typename TR, int W, int NV, bool NORM>
+// W warps hold one row, NG groups of 4 columns per lane: a warp's group is 128 columns, one block of the E4M3 form, and every access is whole
+// lines (128 W (NG - 1) < cols <= 128 W NG).  CTAs stay and walk the rows.  Rows of x and the residual come by bulk copies into a ring of
+// NORM_RING rows in shared memory, so that what is under way does not cost registers.  The weights and conditioning vectors are fetched ahead
+// of the sums that stand before their use, out of the first-level cache: rows pass it by.
+constexpr int NORM_RING = 2;
+template <typename TX, typename TR, int W, int NG, bool NORM>
 __global__ void __launch_bounds__(W < 4 ? 128 : 32 * W)
 gated_norm_kernel(NormArgs a) {
-    constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
+    using attn::add2; using attn::fma2; using attn::mul2; using attn::pair; using attn::unpair;
+    constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W), SPAN = 128 * W;
+    extern __shared__ __align__(16) uint8_t s_ring[];
+    __shared__ uint64_t s_full[RPC][NORM_RING];
+    __shared__ int s_abort;
     __shared__ uint32_t s_part[2][THREADS / 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wr = warp % W, rc = warp / W;                 // warp within its row, row within the CTA
-    const int col0 = (wr * 2 + (lane >> 4)) * FP8_BLOCK + (lane & 15) * 8;
+    const int col0 = wr * 128 + lane * 4;
+    const bool last = col0 + SPAN * (NG - 1) < a.cols;      // this lane's last group is there
+    auto in = [&](int i) { return i < NG - 1 || last; };
+    const uint32_t x_bytes = a.cols * (uint32_t)sizeof(TX), t_bytes = NORM && a.residual ? a.cols * (uint32_t)sizeof(TR) : 0u;
+    if (threadIdx.x == 0) {
+        for (int r = 0; r < RPC; ++r)
+            for (int b = 0; b < NORM_RING; ++b) ptx::mbar_init(&s_full[r][b], 1);
+        s_abort = 0;
+        ptx::fence_barrier_init();
+    }
+    __syncthreads();
     const float inv_cols = 1.0f / (float)a.cols;
     ptx::pdl_wait();
     const long long rows = used_rows(a.rows, a.rows_used), step = (long long)gridDim.x * RPC;
     int turn = 0;                                           // (two turns: a sum has been read before the one after next is written)
-    auto row_sum = [&](float v) {
-        v = warp_sum(v);
+    auto row_sum = [&](uint64_t p) {
+        float v, w;
+        unpair(p, v, w);
+        v = warp_sum(v + w);
         if constexpr (W > 1) {
             if (lane == 0) s_part[turn][warp] = __float_as_uint(v);
             row_barrier<RPC, 32 * W>(rc);
@@ -96,165 +130,218 @@ gated_norm_kernel(NormArgs a) {
         }
         return v;
     };
-    Raw8<TX> x[NV];
-    Raw8<TR> t[NORM ? NV : 1];
     int index = 0;
-    const bool mod = NORM && (a.gate || a.scale || a.shift);
-    auto request_x = [&](long long row) {
-        const TX* p = static_cast<const TX*>(a.x) + row * a.x_ld + col0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (col0 + i * W * 256 < a.cols) x[i].load_stream(p + i * W * 256);
+    const bool mod = NORM && (a.gate || a.scale || a.shift), mb = a.mod_bf16;
+    auto slot_of = [&](int b) { return s_ring + (size_t)(rc * NORM_RING + b) * (x_bytes + t_bytes); };
+    auto request = [&](long long row, int b) {              // by one lane of the row's warps
+        ptx::mbar_expect_tx(&s_full[rc][b], x_bytes + t_bytes);
+        ptx::bulk_load(slot_of(b), static_cast<const TX*>(a.x) + row * a.x_ld, x_bytes, &s_full[rc][b]);
+        if (t_bytes) ptx::bulk_load(slot_of(b) + x_bytes, static_cast<const TR*>(a.residual) + row * a.res_ld, t_bytes, &s_full[rc][b]);
+    };
+    auto request_index = [&](long long row) {
         if (mod) index = a.row_index ? a.row_index[row] : (int)row;
     };
-    auto request_t = [&](long long row) {
-        if constexpr (NORM) {
-            if (!a.residual) return;
-            const TR* p = static_cast<const TR*>(a.residual) + row * a.res_ld + col0;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (col0 + i * W * 256 < a.cols) t[i].load_stream(p + i * W * 256);
-        }
-    };
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        x[i].set(0.f);
-        if constexpr (NORM) t[i].set(0.f);
-    }
     long long row = (long long)blockIdx.x * RPC + rc;
-    if (row < rows) {
-        request_x(row);
-        request_t(row);
-    }
-    for (; row < rows; row += step) {
-        const long long next = row + step;
-        float v[NV][8];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) x[i].get(v[i]);
+    if (wr == 0 && lane == 0)
+        for (int b = 0; b < NORM_RING; ++b)
+            if (row + b * step < rows) request(row + b * step, b);
+    if (row < rows) request_index(row);
+    uint32_t it = 0;
+    bool ok = true;                                         // a thread whose wait ran out stores nothing more, but no thread leaves the loop
+    for (; row < rows; row += step, ++it) {
+        const int b = it % NORM_RING;
+        const long long ahead = row + NORM_RING * step;
+        // every warp of the row has read its slot: it may be filled again
+        auto release = [&]() {
+            if constexpr (W > 1) row_barrier<RPC, 32 * W>(rc);
+            else __syncwarp();
+            if (wr == 0 && lane == 0 && ahead < rows && ok) request(ahead, b);
+        };
         const int at = index;
-        if (next < rows) request_x(next);
+        if (row + step < rows) request_index(row + step);
+        ok = ok && ptx::mbar_wait(&s_full[rc][b], (it / NORM_RING) & 1, &s_abort);
         long long g = 0;
         if (mod) {
             if (at < 0 || at >= a.slots) {                  // (the same for every thread of the row)
                 if (wr == 0 && lane == 0) report_status(a.status, FD_ERR_STATE);
-                if (next < rows) request_t(next);
+                release();
                 continue;
             }
             g = (unsigned)at / (unsigned)a.rows_per_group;
         }
+        uint64_t v[NG][2];
+        const TX* xs = reinterpret_cast<const TX*>(slot_of(b)) + col0;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            Raw4<TX> x;
+            x.clear();
+            if (in(i)) x.load(xs + i * SPAN);
+            x.get(v[i]);
+        }
+        auto times = [&](uint64_t f) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) { v[i][0] = mul2(v[i][0], f); v[i][1] = mul2(v[i][1], f); }
+        };
         auto normalise = [&](int kind) {                    // v becomes its norm
             if (kind == FD_NORM_NONE) return;
             if (kind == FD_NORM_LAYER) {
-                float s = 0.f;
+                uint64_t s = v[0][0];
+                s = add2(s, v[0][1]);
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) s += v[i][k];
+                for (int i = 1; i < NG; ++i) s = add2(add2(s, v[i][0]), v[i][1]);
                 const float mean = row_sum(s) * inv_cols;
+                const uint64_t m = pair(-mean, -mean);
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (col0 + i * W * 256 < a.cols)        // (columns that are not there stay zeros)
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[i][k] -= mean;
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) { v[i][0] = add2(v[i][0], m); v[i][1] = add2(v[i][1], m); }      // (columns that are not there stay zeros)
             }
-            float ss = 0.f;
+            uint64_t ss = mul2(v[0][0], v[0][0]);
+            ss = fma2(v[0][1], v[0][1], ss);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 1; i < NG; ++i) ss = fma2(v[i][1], v[i][1], fma2(v[i][0], v[i][0], ss));
+            const float rstd = rsqrtf(fmaf(row_sum(ss), inv_cols, a.eps));
+            times(pair(rstd, rstd));
+        };
+        Raw4<TX> w[NORM ? NG : 1];
+        RawMod f0[NORM ? NG : 1], f1[NORM ? NG : 1];
+        auto fetch_weight = [&](const void* p) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) ss = fmaf(v[i][k], v[i][k], ss);
-            const float rstd = 1.0f / sqrtf(fmaf(row_sum(ss), inv_cols, a.eps));
+            for (int i = 0; i < NG; ++i)
+                if (in(i)) w[i].load(static_cast<const TX*>(p) + col0 + i * SPAN);
+        };
+        auto fetch_mod = [&](RawMod* f, const void* p, long long ld) {
+            const long long from = g * ld + col0;
+            if (mb) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) f[i].load(p, true, from + i * SPAN);
+            } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] *= rstd;
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) f[i].load(p, false, from + i * SPAN);
+            }
+        };
+        // v = op(v, values) for every group that is there
+        auto with_weight = [&]() {
+#pragma unroll
+            for (int i = 0; i < NG; ++i)
+                if (in(i)) {
+                    uint64_t f[2];
+                    w[i].get(f);
+                    v[i][0] = mul2(v[i][0], f[0]);
+                    v[i][1] = mul2(v[i][1], f[1]);
+                }
+        };
+        auto with_mod = [&](const RawMod* m, auto&& op) {
+            if (mb) {
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) {
+                        uint64_t f[2];
+                        m[i].get(true, f);
+                        v[i][0] = op(v[i][0], f[0]);
+                        v[i][1] = op(v[i][1], f[1]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) {
+                        uint64_t f[2];
+                        m[i].get(false, f);
+                        v[i][0] = op(v[i][0], f[0]);
+                        v[i][1] = op(v[i][1], f[1]);
+                    }
+            }
         };
         if constexpr (NORM) {
+            if (a.post_weight) fetch_weight(a.post_weight);
+            if (a.gate) fetch_mod(f0, a.gate, a.gate_ld);
             normalise(a.post);
+            if (a.post_weight) with_weight();
+            if (a.gate) with_mod(f0, [](uint64_t p, uint64_t f) { return attn::mul2(p, f); });
+            if (a.residual) {
+                const uint64_t alpha = pair(a.alpha, a.alpha);
+                const TR* ts = reinterpret_cast<const TR*>(slot_of(b) + x_bytes) + col0;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = col0 + i * W * 256;
-                if (c >= a.cols) continue;
-                float f[8];
-                if (a.post_weight) {
-                    Raw8<TX> w;
-                    w.load(static_cast<const TX*>(a.post_weight) + c);
-                    w.get(f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] *= f[k];
-                }
-                if (a.gate) {
-                    load8_mod(a.gate, a.mod_bf16, g * a.gate_ld + c, f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] *= f[k];
-                }
-                if (a.residual) {
-                    t[i].get(f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] = fmaf(a.alpha, f[k], v[i][k]);
-                }
-                if (a.residual_out) store8<TR>(static_cast<TR*>(a.residual_out) + row * a.res_out_ld + c, v[i]);
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) {
+                        Raw4<TR> t;
+                        uint64_t f[2];
+                        t.load(ts + i * SPAN);
+                        t.get(f);
+                        v[i][0] = fma2(alpha, f[0], v[i][0]);
+                        v[i][1] = fma2(alpha, f[1], v[i][1]);
+                    }
             }
-            if (next < rows) request_t(next);
-            if (!a.y && !a.y8) continue;
+            const bool more = a.y || a.y8;
+            if (more) {
+                if (a.pre_weight) fetch_weight(a.pre_weight);
+                if (a.scale) fetch_mod(f0, a.scale, a.scale_ld);
+                if (a.shift) fetch_mod(f1, a.shift, a.shift_ld);
+            }
+            release();
+            if (a.residual_out && ok) {
+                TR* p = static_cast<TR*>(a.residual_out) + row * a.res_out_ld + col0;
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) store4(p + i * SPAN, v[i]);
+            }
+            if (!more) continue;
             normalise(a.pre);
+            if (a.pre_weight) with_weight();
+            if (a.scale) with_mod(f0, [](uint64_t p, uint64_t f) { return attn::mul2(p, attn::add2(f, attn::pair(1.0f, 1.0f))); });
+            if (a.shift) with_mod(f1, [](uint64_t p, uint64_t f) { return attn::add2(p, f); });
+            if (a.y && ok) {
+                TX* p = static_cast<TX*>(a.y) + row * a.y_ld + col0;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = col0 + i * W * 256;
-                if (c >= a.cols) continue;
-                float f[8];
-                if (a.pre_weight) {
-                    Raw8<TX> w;
-                    w.load(static_cast<const TX*>(a.pre_weight) + c);
-                    w.get(f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] *= f[k];
-                }
-                if (a.scale) {
-                    load8_mod(a.scale, a.mod_bf16, g * a.scale_ld + c, f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] *= 1.0f + f[k];
-                }
-                if (a.shift) {
-                    load8_mod(a.shift, a.mod_bf16, g * a.shift_ld + c, f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] += f[k];
-                }
-                if (a.y) store8<TX>(static_cast<TX*>(a.y) + row * a.y_ld + c, v[i]);
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) store4(p + i * SPAN, v[i]);
             }
         }
-        if (a.y8 && a.y8_int) {
-            uint32_t m = 0;
+        if constexpr (!NORM) release();
+        if (!a.y8) continue;
+        uint8_t* y8 = a.y8 + row * a.y8_ld + col0;
+        if (a.y8_int) {
+            float m = 0.f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) m = max(m, abs_bits(v[i][k]));
-            const I8Scale i8 = i8_scale(row_max(m));
-            if (wr == 0 && lane == 0) a.y8_scale[row * a.sc_ld] = i8.scale;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = col0 + i * W * 256;
-                if (c < a.cols) *reinterpret_cast<uint2*>(a.y8 + row * a.y8_ld + c) = make_uint2(i8.code4(v[i]), i8.code4(v[i] + 4));
+            for (int i = 0; i < NG; ++i) {
+                float p[4];
+                unpair(v[i][0], p[0], p[1]);
+                unpair(v[i][1], p[2], p[3]);
+                m = max3_nan(max3_nan(m, p[0], p[1]), p[2], p[3]);
             }
-        } else if (NORM && a.y8) {
+            const I8Scale i8 = i8_scale(row_max(abs_bits(m)));
+            if (wr == 0 && lane == 0 && ok) a.y8_scale[row * a.sc_ld] = i8.scale;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = col0 + i * W * 256;
-                float amax = 0.f;
+            for (int i = 0; i < NG; ++i)
+                if (in(i) && ok) *reinterpret_cast<uint32_t*>(y8 + i * SPAN) = i8.code4(v[i]);
+        } else if (NORM) {
+            // lane i takes the divisions of the warp's group i (a NaN does not count for a block's scale)
+            float mine = 1.0f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) amax = fmaxf(amax, fabsf(v[i][k]));
+            for (int i = 0; i < NG; ++i) {
+                float p[4];
+                unpair(v[i][0], p[0], p[1]);
+                unpair(v[i][1], p[2], p[3]);
+                const float m = attn::max3(attn::max3(FP8_AMAX_FLOOR, fabsf(p[0]), fabsf(p[1])), fabsf(p[2]), fabsf(p[3]));
+                const float amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+                if (lane == i) mine = amax;
+            }
+            const float inv = E4M3_MAX / mine;
+            if (lane < NG && wr * 128 + lane * SPAN < a.cols && ok) a.y8_scale[row * a.sc_ld + wr + lane * W] = mine / E4M3_MAX;
 #pragma unroll
-                for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                amax = fmaxf(amax, FP8_AMAX_FLOOR);
-                const float inv = E4M3_MAX / amax;
-                if (c < a.cols) {
-                    uint2 q;
-                    q.x = pack4_e4m3(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-                    q.y = pack4_e4m3(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
-                    *reinterpret_cast<uint2*>(a.y8 + row * a.y8_ld + c) = q;
-                    if ((lane & 15) == 0) a.y8_scale[row * a.sc_ld + c / FP8_BLOCK] = amax / E4M3_MAX;
-                }
+            for (int i = 0; i < NG; ++i) {
+                const float f = __shfl_sync(0xffffffffu, inv, i);
+                float p[4];
+                unpair(v[i][0], p[0], p[1]);
+                unpair(v[i][1], p[2], p[3]);
+                if (in(i) && ok) *reinterpret_cast<uint32_t*>(y8 + i * SPAN) = pack4_e4m3(p[0] * f, p[1] * f, p[2] * f, p[3] * f);
             }
         }
+    }
+    if (!ok) {
+        report_status(a.status, FD_ERR_TIMEOUT);
+        gb_settle();                                        // copies under way land before the CTA leaves
     }
     ptx::pdl_trigger();
 }
@@ -368,49 +455,62 @@ gated_norm_any_kernel(NormArgs a) {
     ptx::pdl_trigger();
 }
 
-constexpr int NORM_CTAS = 8, NORM_MAX_NV = 6, NORM_MAX_W = 8;
+constexpr int NORM_CTAS = 8, NORM_MAX_NG = 6, NORM_MAX_W = 16;
+constexpr int NORM_RING_BYTES = 150 * 1024;     // of rings on an SM: the rest of its 228 KB caches the weights and conditioning vectors
+constexpr int NORM_MAX_SMEM = 200 * 1024;
+static_assert(NORM_RING * 128 * NORM_MAX_W * NORM_MAX_NG * 8 <= NORM_MAX_SMEM, "the widest fp32 rows fit the ring");
 
-template <typename TX, typename TR, int W, int NV, bool NORM>
+template <typename TX, typename TR, int W, int NG, bool NORM>
 cudaError_t launch_reg(const NormArgs& a, cudaStream_t st) {
     constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
-    const int grid = (int)min((a.rows + RPC - 1) / RPC, 148LL * NORM_CTAS);
-    return ptx::launch_kernel(gated_norm_kernel<TX, TR, W, NV, NORM>, grid, THREADS, 0, st, a.status == nullptr, a);
+    const int smem = RPC * NORM_RING * a.cols * (int)(sizeof(TX) + (NORM && a.residual ? sizeof(TR) : 0));
+    if (smem > 48 * 1024) {
+        static std::atomic<uint64_t> raised{0};             // devices on which the kernel may use as much
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = 1ull << (dev & 63);
+        if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
+            e = cudaFuncSetAttribute(gated_norm_kernel<TX, TR, W, NG, NORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MAX_SMEM);
+            if (e != cudaSuccess) return e;
+            raised.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    const int per_sm = max(1, min(NORM_CTAS, NORM_RING_BYTES / smem));
+    const int grid = (int)min((a.rows + RPC - 1) / RPC, 148LL * per_sm);
+    return ptx::launch_kernel(gated_norm_kernel<TX, TR, W, NG, NORM>, grid, THREADS, smem, st, a.status == nullptr, a);
 }
 
-// (fewer than NORM_MAX_W warps hold at most three vectors a lane: launch_typed)
-template <typename TX, typename TR, int W, bool NORM>
-cudaError_t launch_nv(const NormArgs& a, cudaStream_t st) {
-    const int nv = (a.cols + 256 * W - 1) / (256 * W);
-    if (nv == 1) return launch_reg<TX, TR, W, 1, NORM>(a, st);
-    if (nv == 2) return launch_reg<TX, TR, W, 2, NORM>(a, st);
-    if constexpr (W == NORM_MAX_W) {
-        if (nv == 4) return launch_reg<TX, TR, W, 4, NORM>(a, st);
-        if (nv == 5) return launch_reg<TX, TR, W, 5, NORM>(a, st);
-        if (nv == 6) return launch_reg<TX, TR, W, 6, NORM>(a, st);
-    }
-    return launch_reg<TX, TR, W, 3, NORM>(a, st);
+template <typename TX, typename TR, int W, bool NORM, int NG = NORM_MAX_NG>
+cudaError_t launch_ng(const NormArgs& a, cudaStream_t st) {
+    if constexpr (NG > 1)
+        if (a.cols <= 128 * W * (NG - 1)) return launch_ng<TX, TR, W, NORM, NG - 1>(a, st);
+    return launch_reg<TX, TR, W, NG, NORM>(a, st);
 }
 
 template <typename TX, typename TR, bool NORM>
 cudaError_t launch_typed(const NormArgs& a, cudaStream_t st) {
-    auto ok = [](const void* p, long long ld, int es) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0); };
-    const int ms = a.mod_bf16 ? 2 : 4;
-    const bool fast = a.cols % 8 == 0 && a.cols <= 256 * NORM_MAX_W * NORM_MAX_NV && ok(a.x, a.x_ld, sizeof(TX)) &&
-                      ok(a.residual, a.res_ld, sizeof(TR)) && ok(a.residual_out, a.res_out_ld, sizeof(TR)) && ok(a.post_weight, 16, 1) &&
-                      ok(a.pre_weight, 16, 1) && ok(a.gate, a.gate_ld, ms) && ok(a.scale, a.scale_ld, ms) && ok(a.shift, a.shift_ld, ms) &&
-                      ok(a.y, a.y_ld, sizeof(TX)) && (!a.y8 || ((reinterpret_cast<uintptr_t>(a.y8) & 7) == 0 && a.y8_ld % 8 == 0));
+    // four values at a time: rows start at multiples of four elements
+    auto ok = [](const void* p, long long ld, int es) { return !p || (reinterpret_cast<uintptr_t>(p) % (4 * es) == 0 && ld % 4 == 0); };
+    const int xs = sizeof(TX), rs = sizeof(TR), ms = a.mod_bf16 ? 2 : 4;
+    // and those that bulk copies fetch at whole 16-byte units
+    auto whole = [&](const void* p, long long ld, int es) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0 && a.cols * es % 16 == 0); };
+    const bool fast = a.cols % 4 == 0 && a.cols <= 128 * NORM_MAX_W * NORM_MAX_NG && whole(a.x, a.x_ld, xs) && whole(a.residual, a.res_ld, rs) &&
+                      ok(a.residual_out, a.res_out_ld, rs) && ok(a.post_weight, 0, xs) && ok(a.pre_weight, 0, xs) && ok(a.gate, a.gate_ld, ms) &&
+                      ok(a.scale, a.scale_ld, ms) && ok(a.shift, a.shift_ld, ms) && ok(a.y, a.y_ld, xs) && ok(a.y8, a.y8_ld, 1);
     if (!fast) {
         const int grid = (int)min(a.rows, 148LL * 16);
         return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 256>, grid, 256, 0, st, a.status == nullptr, a);
     }
-    // Warps per row: three vectors a lane where eight warps allow it; more warps when the rows alone would leave SMs idle.
+    // Warps per row: as few as hold it; more when the rows alone would leave SMs idle.
     int w = 1;
-    while (w < NORM_MAX_W && (a.cols > 256 * w * 3 || (a.cols > 256 * w && a.rows * w < 148 * 4))) w *= 2;
+    while (w < NORM_MAX_W && (a.cols > 128 * w * NORM_MAX_NG || (a.cols > 128 * w && a.rows * w < 148 * 4))) w *= 2;
     switch (w) {
-        case 1: return launch_nv<TX, TR, 1, NORM>(a, st);
-        case 2: return launch_nv<TX, TR, 2, NORM>(a, st);
-        case 4: return launch_nv<TX, TR, 4, NORM>(a, st);
-        default: return launch_nv<TX, TR, 8, NORM>(a, st);
+        case 1: return launch_ng<TX, TR, 1, NORM>(a, st);
+        case 2: return launch_ng<TX, TR, 2, NORM>(a, st);
+        case 4: return launch_ng<TX, TR, 4, NORM>(a, st);
+        case 8: return launch_ng<TX, TR, 8, NORM>(a, st);
+        default: return launch_ng<TX, TR, 16, NORM>(a, st);
     }
 }
 

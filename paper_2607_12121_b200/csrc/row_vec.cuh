@@ -1,5 +1,6 @@
-// Eight consecutive values of a row at a time, in 16-byte accesses.
+// Eight or four consecutive values of a row at a time, in accesses of up to 16 bytes.
 #pragma once
+#include "attn_common.cuh"
 #include "common.cuh"
 
 namespace fd {
@@ -63,6 +64,38 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16*
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Four consecutive values: as they lie in memory, and as two packed pairs of fp32
+template <typename T> struct Raw4;
+template <> struct Raw4<float> {
+    uint4 q;
+    __device__ __forceinline__ void load(const float* p) { q = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load_stream(const float* p) { q = load_once(p); }
+    __device__ __forceinline__ void clear() { q = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void get(uint64_t* v) const {
+        v[0] = attn::pair(__uint_as_float(q.x), __uint_as_float(q.y));
+        v[1] = attn::pair(__uint_as_float(q.z), __uint_as_float(q.w));
+    }
+};
+template <> struct Raw4<__nv_bfloat16> {
+    uint2 q;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { q = *reinterpret_cast<const uint2*>(p); }
+    __device__ __forceinline__ void load_stream(const __nv_bfloat16* p) {
+        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(q.x), "=r"(q.y) : "l"(p) : "memory");
+    }
+    __device__ __forceinline__ void clear() { q = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void get(uint64_t* v) const {
+        v[0] = attn::pair(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xffff0000u));
+        v[1] = attn::pair(__uint_as_float(q.y << 16), __uint_as_float(q.y & 0xffff0000u));
+    }
+};
+__device__ __forceinline__ void store4(float* p, const uint64_t* v) { *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(v[0], v[1]); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const uint64_t* v) {
+    float a, b, c, d;
+    attn::unpair(v[0], a, b);
+    attn::unpair(v[1], c, d);
+    *reinterpret_cast<uint2*>(p) = make_uint2(attn::pack_bf16(a, b), attn::pack_bf16(c, d));
 }
 
 }  // namespace fd
