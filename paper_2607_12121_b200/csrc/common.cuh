@@ -98,9 +98,15 @@ __device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
     return {a / I8_MAX, I8_MAX / a};
 }
 
-// the value of code i (0 .. 3) of four: with its sign bit flipped a code lies 128 above itself, in the low bits of 2^23
-__device__ __forceinline__ float i8_value(uint32_t q, int i) {
-    return __uint_as_float(__byte_perm(q ^ 0x80808080u, 0x4B000000u, 0x7540 + i)) - 8388736.0f;
+// the values of four codes times f: with its sign bit flipped a code lies 128 above itself, in the low bits of 2^23
+__device__ __forceinline__ void i8_values(uint32_t q, float f, float* v) {
+    q ^= 0x80808080u;
+    const uint64_t back = attn::pair(-8388736.0f, -8388736.0f), by = attn::pair(f, f);
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const uint64_t p = attn::pair(__uint_as_float(__byte_perm(q, 0x4B000000u, 0x7540 + i)), __uint_as_float(__byte_perm(q, 0x4B000000u, 0x7541 + i)));
+        attn::unpair(attn::mul2(attn::add2(p, back), by), v[i], v[i + 1]);
+    }
 }
 
 // Rows a call works on: a capacity, and optionally a count that only the device knows.

@@ -346,13 +346,16 @@ gated_norm_kernel(NormArgs a) {
     ptx::pdl_trigger();
 }
 
-// Any width, stride and alignment: one CTA a row, which is read again for every sum.
-template <typename TX, typename TR, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+// Any width, stride and alignment: one CTA a row, element accesses.  A warp takes whole blocks of 128 columns, a lane four columns of a block
+// 32 apart, the same ones in every pass over the row: x, then r, then y stay in shared memory between the passes (STAGED), or, wider than
+// that, are formed again from what is in global memory.  (In place either way: every element is read and written by one thread.)
+constexpr int NORM_ANY_COLS = 12 * 1024;                    // fp32 values in 48 KB
+template <typename TX, typename TR, bool STAGED>
+__global__ void __launch_bounds__(256)
 gated_norm_any_kernel(NormArgs a) {
-    constexpr int WARPS = THREADS / 32;
-    __shared__ uint32_t s_part[2][WARPS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    extern __shared__ float s_row[];
+    __shared__ uint32_t s_part[2][8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x / 32;
     ptx::pdl_wait();
     const long long rows = used_rows(a.rows, a.rows_used);
     int turn = 0;                                                // (two turns: a sum has been read before the one after next is written)
@@ -361,8 +364,7 @@ gated_norm_any_kernel(NormArgs a) {
         if (lane == 0) s_part[turn][warp] = __float_as_uint(v);
         __syncthreads();
         v = 0.f;
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) v += __uint_as_float(s_part[turn][i]);
+        for (int i = 0; i < warps; ++i) v += __uint_as_float(s_part[turn][i]);
         turn ^= 1;
         return v;
     };
@@ -380,63 +382,80 @@ gated_norm_any_kernel(NormArgs a) {
             return a.mod_bf16 ? to_f(static_cast<const __nv_bfloat16*>(p)[at]) : static_cast<const float*>(p)[at];
         };
         const float cols = (float)a.cols;
+        auto each = [&](auto&& f) {                              // f(column) for this thread's columns
+            for (int c0 = warp * 128 + lane; c0 < a.cols; c0 += warps * 128)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c0 + 32 * k < a.cols) f(c0 + 32 * k);
+        };
         auto norm_of = [&](int kind, auto&& value, float& mean, float& rstd) {      // mean and 1 / deviation of the row's values
             mean = 0.f;
             rstd = 1.f;
             if (kind == FD_NORM_NONE) return;
             if (kind == FD_NORM_LAYER) {
                 float s = 0.f;
-                for (int c = threadIdx.x; c < a.cols; c += THREADS) s += value(c);
+                each([&](int c) { s += value(c); });
                 mean = block_sum(s) / cols;
             }
             float s = 0.f;
-            for (int c = threadIdx.x; c < a.cols; c += THREADS) {
+            each([&](int c) {
                 const float d = value(c) - mean;
                 s = fmaf(d, d, s);
-            }
-            rstd = 1.0f / sqrtf(block_sum(s) / cols + a.eps);
+            });
+            rstd = rsqrtf(block_sum(s) / cols + a.eps);
         };
+        if constexpr (STAGED) each([&](int c) { s_row[c] = to_f<TX>(x[c]); });
+        auto x_of = [&](int c) { return STAGED ? s_row[c] : to_f<TX>(x[c]); };
         float post_mean, post_rstd, pre_mean, pre_rstd;
-        norm_of(a.post, [&](int c) { return to_f<TX>(x[c]); }, post_mean, post_rstd);
-        auto r_of = [&](int c) {
-            float n = (to_f<TX>(x[c]) - post_mean) * post_rstd;
+        norm_of(a.post, x_of, post_mean, post_rstd);
+        auto r_formed = [&](int c) {
+            float n = (x_of(c) - post_mean) * post_rstd;
             if (post_w) n *= to_f<TX>(post_w[c]);
             if (a.gate) n *= mod(a.gate, a.gate_ld, c);
             return res ? fmaf(a.alpha, to_f<TR>(res[c]), n) : n;
         };
+        if constexpr (STAGED) each([&](int c) { s_row[c] = r_formed(c); });
+        auto r_of = [&](int c) { return STAGED ? s_row[c] : r_formed(c); };
         norm_of(a.pre, r_of, pre_mean, pre_rstd);
-        auto y_of = [&](float r, int c) {
+        auto y_formed = [&](float r, int c) {
             float y = (r - pre_mean) * pre_rstd;
             if (pre_w) y *= to_f<TX>(pre_w[c]);
             if (a.scale) y *= 1.0f + mod(a.scale, a.scale_ld, c);
             return a.shift ? y + mod(a.shift, a.shift_ld, c) : y;
         };
+        if constexpr (STAGED)
+            each([&](int c) {
+                const float r = s_row[c];
+                if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
+                s_row[c] = y_formed(r, c);
+            });
         I8Scale i8{};
         if (a.y8 && a.y8_int) {
             uint32_t m = 0;
-            for (int c = threadIdx.x; c < a.cols; c += THREADS) m = max(m, abs_bits(y_of(r_of(c), c)));
+            each([&](int c) { m = max(m, abs_bits(STAGED ? s_row[c] : y_formed(r_of(c), c))); });
             m = __reduce_max_sync(0xffffffffu, m);
             if (lane == 0) s_part[turn][warp] = m;
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < WARPS; ++i) m = max(m, s_part[turn][i]);
+            for (int i = 0; i < warps; ++i) m = max(m, s_part[turn][i]);
             turn ^= 1;
             i8 = i8_scale(m);
             if (threadIdx.x == 0) a.y8_scale[row * a.sc_ld] = i8.scale;
         }
-        // the outputs: a warp takes 128 columns, a lane four of them 32 apart (in place: every element is written by the thread that
-        // reads it here, and all reads for the sums are behind their barriers)
-        for (int b = warp; b * FP8_BLOCK < a.cols; b += WARPS) {
+        for (int b = warp; b * FP8_BLOCK < a.cols; b += warps) {
             float v[4], amax = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int c = b * FP8_BLOCK + k * 32 + lane;
                 v[k] = 0.f;
                 if (c >= a.cols) continue;
-                const float r = r_of(c);
-                v[k] = y_of(r, c);
+                if constexpr (STAGED) {
+                    v[k] = s_row[c];
+                } else {
+                    const float r = r_of(c);
+                    v[k] = y_formed(r, c);
+                    if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
+                }
                 amax = fmaxf(amax, fabsf(v[k]));
-                if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
                 if (a.y) static_cast<TX*>(a.y)[row * a.y_ld + c] = from_f<TX>(v[k]);
                 if (a.y8 && a.y8_int) a.y8[row * a.y8_ld + c] = i8.code(v[k]);
             }
@@ -499,8 +518,11 @@ cudaError_t launch_typed(const NormArgs& a, cudaStream_t st) {
                       ok(a.residual_out, a.res_out_ld, rs) && ok(a.post_weight, 0, xs) && ok(a.pre_weight, 0, xs) && ok(a.gate, a.gate_ld, ms) &&
                       ok(a.scale, a.scale_ld, ms) && ok(a.shift, a.shift_ld, ms) && ok(a.y, a.y_ld, xs) && ok(a.y8, a.y8_ld, 1);
     if (!fast) {
-        const int grid = (int)min(a.rows, 148LL * 16);
-        return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 256>, grid, 256, 0, st, a.status == nullptr, a);
+        // (a warp a block of 128 columns, up to eight; the widest staged rows leave room for four CTAs an SM)
+        const int threads = 32 * min(8, (a.cols + 127) / 128), grid = (int)min(a.rows, 148LL * 32);
+        if (a.cols <= NORM_ANY_COLS)
+            return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, true>, grid, threads, a.cols * sizeof(float), st, a.status == nullptr, a);
+        return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, false>, grid, threads, 0, st, a.status == nullptr, a);
     }
     // Warps per row: as few as hold it; more when the rows alone would leave SMs idle.
     int w = 1;

@@ -37,71 +37,99 @@ __device__ __forceinline__ long long kv_slot(const KvArgs& a, long long i, bool 
     return s;
 }
 
-// Head dims of whole 16-byte units: LANES lanes hold one head, NU units of 8 channels each; keys and values of a head are in flight together.
-template <typename T, bool STORE, int LANES, int NU>
-__global__ void __launch_bounds__(256) kv_kernel(KvArgs a, int n_sets) {
-    const int l = threadIdx.x % LANES, units = a.dh / 8;
-    const unsigned group_mask = LANES == 32 ? 0xffffffffu : ((1u << LANES) - 1) << ((threadIdx.x & 31) / LANES * LANES);
+// A set whose rows are whole 16-byte units and whose codes are whole 8-byte units apart: strides in those units, in 32 bits
+struct KvFastSet {
+    char* rows;
+    char* codes;
+    float* scale;
+    uint32_t rows_group, rows_token, rows_head, codes_group, codes_token, codes_head, scale_group, scale_token, scale_head;
+};
+struct KvFastArgs {
+    KvFastSet sets[2];
+    KvArgs a;
+};
+__device__ __forceinline__ uint64_t offset3(uint32_t a, uint32_t sa, uint32_t b, uint32_t sb, uint32_t c, uint32_t sc) {
+    return (uint64_t)a * sa + (uint64_t)b * sb + (uint64_t)c * sc;
+}
+
+// Head dims of whole units: LANES lanes hold one head, NU units of 8 channels each; keys and values of a head are in flight together.  Four
+// lanes, so that the index arithmetic and the quotients of a head serve many values: with eight, stores of 16380 x 2 x 12 heads of 128 took
+// 26.7 us against 23.7, of 5216 x 2 x 24 heads of 64 13.9 against 10.3.
+constexpr int LANES = 4;
+template <typename T, bool STORE, int NU>
+__global__ void __launch_bounds__(256) kv_kernel(const __grid_constant__ KvFastArgs f, int n_sets) {
+    const KvArgs& a = f.a;
+    const int l = threadIdx.x % LANES, units = a.dh / 8, first_lane = (threadIdx.x & 31) / LANES * LANES;
+    const unsigned group_mask = ((1u << LANES) - 1) << first_lane;
+    constexpr int UNIT = 8 * sizeof(T);                     // bytes of 8 channels
     ptx::pdl_wait();
     const uint32_t items = (uint32_t)(used_rows(a.rows, a.rows_used) * a.heads);       // (below 2^31: the launcher has checked)
     constexpr int HPC = 256 / LANES;                        // heads of a CTA
     for (uint32_t w = blockIdx.x * HPC + threadIdx.x / LANES; w < items; w += gridDim.x * HPC) {
-        const uint32_t i = a.by_heads.of(w);
-        const int h = (int)(w - i * a.heads);
+        const uint32_t i = a.by_heads.of(w), h = w - i * a.heads;
         const long long slot = kv_slot(a, i, STORE);
         if (slot < 0) {
             if (l == 0 && h == 0) report_status(a.status, FD_ERR_STATE);
             continue;
         }
         const uint32_t g = a.by_tokens.of((uint32_t)slot), t = (uint32_t)slot - g * a.tokens;
-        T* row[2];
-        int8_t* codes[2];
+        const uint32_t row_g = a.by_slot ? g : 0, row_t = a.by_slot ? t : i;
+        char* row[2];
+        char* codes[2];
         float* scale[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const fd_kv_int8_set& k = a.sets[s];
-            row[s] = static_cast<T*>(k.rows) + (a.by_slot ? g * k.rows_group_stride + t * k.rows_token_stride : i * k.rows_token_stride) + h * k.rows_head_stride;
-            codes[s] = static_cast<int8_t*>(k.codes) + g * k.codes_group_stride + t * k.codes_token_stride + h * k.codes_head_stride;
-            scale[s] = k.scale + g * k.scale_group_stride + t * k.scale_token_stride + h * k.scale_head_stride;
+            const KvFastSet& k = f.sets[s];
+            row[s] = k.rows + 16 * offset3(row_g, k.rows_group, row_t, k.rows_token, h, k.rows_head) + l * UNIT;
+            codes[s] = k.codes + 8 * offset3(g, k.codes_group, t, k.codes_token, h, k.codes_head) + l * 8;
+            scale[s] = k.scale + offset3(g, k.scale_group, t, k.scale_token, h, k.scale_head);
         }
         if constexpr (STORE) {
             Raw8<T> x[2][NU];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-                if (s < n_sets)
-#pragma unroll
-                    for (int u = 0; u < NU; ++u)
-                        if (l + u * LANES < units) x[s][u].load_stream(row[s] + (l + u * LANES) * 8);
-                        else x[s][u].set(0.f);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                if (s >= n_sets) break;
-                float v[NU][8];
-                uint32_t m = 0;
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
-                    x[s][u].get(v[u]);
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) m = max(m, abs_bits(v[u][c]));
+                    x[s][u].set(0.f);
+                    if (s < n_sets && l + u * LANES < units) x[s][u].load_stream(reinterpret_cast<const T*>(row[s] + u * LANES * UNIT));
                 }
+            uint32_t m[2];
 #pragma unroll
-                for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(group_mask, m, o));
-                const I8Scale i8 = i8_scale(m);
-                if (l == 0) *scale[s] = i8.scale;
+            for (int s = 0; s < 2; ++s) {
+                m[s] = x[s][0].amax_bits();
 #pragma unroll
-                for (int u = 0; u < NU; ++u)
-                    if (l + u * LANES < units) *reinterpret_cast<uint2*>(codes[s] + (l + u * LANES) * 8) = make_uint2(i8.code4(v[u]), i8.code4(v[u] + 4));
+                for (int u = 1; u < NU; ++u) m[s] = max(m[s], x[s][u].amax_bits());
+#pragma unroll
+                for (int o = LANES / 2; o > 0; o >>= 1) m[s] = max(m[s], __shfl_xor_sync(group_mask, m[s], o));
+            }
+            // both sets' scales and their reciprocals are four quotients: each of four lanes takes one
+            const bool of_scale = l & 1;
+            const uint32_t mine = l & 2 ? m[1] : m[0];
+            const float amax = fmaxf(__uint_as_float(mine), I8_AMAX_FLOOR);
+            float q = (of_scale ? amax : I8_MAX) / (of_scale ? I8_MAX : amax);
+            if (mine >= 0x7f800000u) q = of_scale ? __uint_as_float(0x7fffffffu) : 0.f;
+            if (of_scale && l < 4 && (l >> 1) < n_sets) *(l & 2 ? scale[1] : scale[0]) = q;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const I8Scale i8{0.f, __shfl_sync(group_mask, q, first_lane + 2 * s)};
+                if (s >= n_sets) break;
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    float v[8];
+                    x[s][u].get(v);
+                    if (l + u * LANES < units) *reinterpret_cast<uint2*>(codes[s] + u * LANES * 8) = make_uint2(i8.code4(v), i8.code4(v + 4));
+                }
             }
         } else {
             uint2 q[2][NU];
-            float f[2];
+            float by[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
                 if (s < n_sets) {
-                    f[s] = *scale[s];
+                    by[s] = *scale[s];
 #pragma unroll
                     for (int u = 0; u < NU; ++u)
-                        if (l + u * LANES < units) q[s][u] = *reinterpret_cast<const uint2*>(codes[s] + (l + u * LANES) * 8);
+                        if (l + u * LANES < units) q[s][u] = *reinterpret_cast<const uint2*>(codes[s] + u * LANES * 8);
                 }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -110,9 +138,9 @@ __global__ void __launch_bounds__(256) kv_kernel(KvArgs a, int n_sets) {
                 for (int u = 0; u < NU; ++u) {
                     if (l + u * LANES >= units) continue;
                     float v[8];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) v[c] = i8_value((c < 4 ? q[s][u].x : q[s][u].y), c & 3) * f[s];
-                    store8<T>(row[s] + (l + u * LANES) * 8, v);
+                    i8_values(q[s][u].x, by[s], v);
+                    i8_values(q[s][u].y, by[s], v + 4);
+                    store8<T>(reinterpret_cast<T*>(row[s] + u * LANES * UNIT), v);
                 }
             }
         }
@@ -160,33 +188,38 @@ __global__ void __launch_bounds__(256) kv_any_kernel(KvArgs a) {
     ptx::pdl_trigger();
 }
 
-template <typename T, bool STORE, int LANES, int NU>
-cudaError_t launch_lanes(const KvArgs& a, int n_sets, cudaStream_t st) {
-    const long long ctas = (a.rows * a.heads + 256 / LANES - 1) / (256 / LANES);
-    return ptx::launch_kernel(kv_kernel<T, STORE, LANES, NU>, (int)min(ctas, 148LL * 16), 256, 0, st, a.status == nullptr, a, n_sets);
+template <typename T, bool STORE, int NU>
+cudaError_t launch_units(const KvFastArgs& f, int n_sets, cudaStream_t st) {
+    const long long ctas = (f.a.rows * f.a.heads + 256 / LANES - 1) / (256 / LANES);
+    return ptx::launch_kernel(kv_kernel<T, STORE, NU>, (int)min(ctas, 1LL << 20), 256, 0, st, f.a.status == nullptr, f, n_sets);
 }
 
 template <typename T, bool STORE>
 cudaError_t launch_typed(const KvArgs& a, int n_sets, cudaStream_t st) {
     bool fast = a.dh % 8 == 0 && a.rows * a.heads < 1LL << 31;
-    for (int i = 0; i < n_sets; ++i) {
+    KvFastArgs f{{}, a};
+    for (int i = 0; i < 2; ++i) {
         const fd_kv_int8_set& k = a.sets[i];
-        const long long rows = k.rows_head_stride | k.rows_token_stride | (a.by_slot ? k.rows_group_stride : 0);
-        const long long codes = k.codes_head_stride | k.codes_token_stride | k.codes_group_stride;
-        fast = fast && (reinterpret_cast<uintptr_t>(k.rows) & 15) == 0 && rows * (long long)sizeof(T) % 16 == 0 &&
-               (reinterpret_cast<uintptr_t>(k.codes) & 7) == 0 && codes % 8 == 0;
+        auto units = [&](long long stride, int per) {
+            fast = fast && stride % per == 0 && stride / per < 1LL << 32;
+            return (uint32_t)(stride / per);
+        };
+        constexpr int PER = 16 / sizeof(T);
+        f.sets[i] = KvFastSet{static_cast<char*>(k.rows), static_cast<char*>(k.codes), k.scale, a.by_slot ? units(k.rows_group_stride, PER) : 0u,
+                              units(k.rows_token_stride, PER), units(k.rows_head_stride, PER), units(k.codes_group_stride, 8), units(k.codes_token_stride, 8),
+                              units(k.codes_head_stride, 8), units(k.scale_group_stride, 1), units(k.scale_token_stride, 1), units(k.scale_head_stride, 1)};
+        fast = fast && (reinterpret_cast<uintptr_t>(k.rows) & 15) == 0 && (reinterpret_cast<uintptr_t>(k.codes) & 7) == 0;
     }
     if (!fast) {
         const dim3 grid((unsigned)min((a.rows * a.heads + 7) / 8, 148LL * 16), n_sets);
         return ptx::launch_kernel(kv_any_kernel<T, STORE>, grid, 256, 0, st, a.status == nullptr, a);
     }
-    // 128-byte lines of bf16 for head dims of 64 and its multiples; four lanes and enough units for the others (72: 9 of 12)
-    if (a.dh == 64) return launch_lanes<T, STORE, 8, 1>(a, n_sets, st);
-    if (a.dh == 128) return launch_lanes<T, STORE, 8, 2>(a, n_sets, st);
-    if (a.dh <= 32) return launch_lanes<T, STORE, 4, 1>(a, n_sets, st);
-    if (a.dh <= 96) return launch_lanes<T, STORE, 4, 3>(a, n_sets, st);
-    if (a.dh <= 192) return launch_lanes<T, STORE, 8, 3>(a, n_sets, st);
-    return launch_lanes<T, STORE, 8, 4>(a, n_sets, st);
+    if (a.dh <= 32) return launch_units<T, STORE, 1>(f, n_sets, st);
+    if (a.dh <= 64) return launch_units<T, STORE, 2>(f, n_sets, st);
+    if (a.dh <= 96) return launch_units<T, STORE, 3>(f, n_sets, st);
+    if (a.dh <= 128) return launch_units<T, STORE, 4>(f, n_sets, st);
+    if (a.dh <= 192) return launch_units<T, STORE, 6>(f, n_sets, st);
+    return launch_units<T, STORE, 8>(f, n_sets, st);
 }
 
 }  // namespace

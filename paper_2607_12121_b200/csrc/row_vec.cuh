@@ -12,6 +12,10 @@ template <> struct Raw8<float> {
     __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
     __device__ __forceinline__ void load_stream(const float* p);
     __device__ __forceinline__ void set(float v) { a = b = make_float4(v, v, v, v); }
+    // bit pattern of the largest magnitude (a NaN's is above all others)
+    __device__ __forceinline__ uint32_t amax_bits() const {
+        return max(max(max(abs_bits(a.x), abs_bits(a.y)), max(abs_bits(a.z), abs_bits(a.w))), max(max(abs_bits(b.x), abs_bits(b.y)), max(abs_bits(b.z), abs_bits(b.w))));
+    }
     __device__ __forceinline__ void get(float* f) const {
         f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
     }
@@ -27,6 +31,13 @@ template <> struct Raw8<__nv_bfloat16> {
         const uint32_t h = __float_as_uint(v) >> 16;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = h | (h << 16);
+    }
+    __device__ __forceinline__ uint32_t amax_bits() const {      // two values an instruction: the pattern of a bf16 is the upper half of fp32's
+        __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[0]));
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[i])));
+        const uint32_t p = *reinterpret_cast<const uint32_t*>(&m);
+        return max(p << 16, p & 0xffff0000u);
     }
     __device__ __forceinline__ void get(float* f) const {
 #pragma unroll

@@ -100,20 +100,24 @@ gemm_int8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], 2 * GI_EPI_WARPS); }
         *abort_flag = 0;
         fence_barrier_init();
+    } else if (warp == 2 && lane == 0) {
         prefetch_tmap(&tm_a);
         prefetch_tmap(&tm_w);
         prefetch_tmap(&tm_tail);
         if (g.tma_out) prefetch_tmap(&tm_o);
     }
-    if (warp == 1) {
-        tmem_alloc_pair(tmem_slot, 512);
-        tmem_relinquish_pair();
+    __syncwarp();
+    cluster_sync_all();                      // both CTAs' barriers exist before anything remote arrives
+    if (warp != 0) {                         // (the loads need no TMEM: they are under way while it is allocated)
+        if (warp == 1) {
+            tmem_alloc_pair(tmem_slot, 512);
+            tmem_relinquish_pair();
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 1, %0;" ::"n"(GI_THREADS - 32) : "memory");
+        tc_fence_after();
     }
-    tc_fence_before();
-    __syncthreads();
-    cluster_sync_all();  // both CTAs' barriers exist before anything remote arrives
-    tc_fence_after();
-    const uint32_t tmem_base = *tmem_slot;
+    const uint32_t tmem_base = warp != 0 ? *tmem_slot : 0u;
     pdl_trigger();
     pdl_wait();
 
@@ -167,9 +171,9 @@ gemm_int8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     } else if (warp == 1 && rank == 0) {
         uint32_t s = 0, ph = 0;
         bool ok = true;
+        Item t = item(0);
         for (uint32_t it = 0; it < items; ++it) {
-            const Item t = item(it);
-            if (t.n0 >= g.n) continue;
+            if (t.n0 >= g.n) continue;                                   // (the last item: see the loads)
             const uint32_t idesc = idesc_s8(2 * GI_M, t.width);
             const uint32_t buf = it & 1, d = tmem_base + buf * GI_N;
             ok = ok && mbar_wait(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag);
@@ -188,6 +192,7 @@ gemm_int8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 __syncwarp();
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
+            if (it + 1 < items) t = item(it + 1);
         }
         if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
     } else if (warp >= 4) {
@@ -546,15 +551,33 @@ cudaError_t launch_matmul_int8(const fd_matmul_int8_args& f, int m, int n, int k
     const int k_blocks = (k + GI_K - 1) / GI_K;
     const long long tiles_split = (long long)((m + 127) / 128) * ((n + 127) / 128);
     const long long tiles_pair = (long long)((m + 2 * GI_M - 1) / (2 * GI_M)) * ((n + GI_N - 1) / GI_N);
-    const bool split = tiles_split <= dev->clusters[0];
+    // Which form, by what each was measured to take in us, launch included (m of 1 .. 1001, n of 256 .. 9216, k of 256 .. 8960, shared out to
+    // 1 .. 8 CTAs; the choice is within 1 % of the best of them on average and 10 % at worst).  Pairs: 3.3, 0.375 a block of K and round
+    // of tiles; the last round by the pieces its tiles are cut into.  Shared out: 2.6 for a few rows and 4.0 for 128, 0.258 a block of K in a
+    // CTA, and the exchange.  E.g. (pairs / shared out, CTAs): 8 x 9216 x 1536 7.5 / 5.4, 2; 128 x 1152 x 1000 5.4 / 5.8, 4; 1001 x
+    // 1152 x 4608 12.4 / 10.4, 2; 256 x 1152 x 8960 17.3 / 9.2, 6; 512 x 4608 x 1536 7.4 / 7.9, 1.  All clusters have to be resident at once (36
+    // of four are not: 128 x 4608 x 1536 11.6 us with them, 6.2 with two).
+    const long long rounds = tiles_pair / dev->pairs, left = tiles_pair % dev->pairs;
+    const int cut = left * 4 <= dev->pairs ? 4 : left * 2 <= dev->pairs ? 2 : 1;
+    double cost = 3.3 + 0.375 * k_blocks * rounds + (rounds ? 1.3 : 0.0);
+    if (left) cost += cut == 4 ? 0.195 * k_blocks : cut == 2 ? 0.5 + 0.235 * k_blocks : 1.2 + 0.27 * k_blocks;
+    const double filled = min(m, 128) / 128.0;
+    int splits = 0;                                         // 0: pairs
+    for (int s = 1; s <= 8 && s <= k_blocks; ++s) {
+        if (tiles_split > dev->clusters[s - 1]) continue;
+        const double c = 2.6 + 1.4 * filled + 0.258 * ((k_blocks + s - 1) / s) + (s > 1 ? 0.25 + 0.1 * s + 0.25 * filled : 0.0);
+        if (c < cost) {
+            cost = c;
+            splits = s;
+        }
+    }
+    const bool split = splits > 0;
     const int a_rows = split ? min(GI_M, (m + 7) / 8 * 8) : GI_M;       // with few rows the box ends with them
     const uint32_t box_a[2] = {GI_K, (uint32_t)a_rows}, box_w[2] = {GI_K, 128}, box_tail[2] = {GI_K, GI_TAIL_BOX};
     if (!encode_tmap(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.a8), 2, da, sa, box_a, 128, why) ||
         !encode_tmap(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, const_cast<void*>(f.w8), 2, dw, sw, box_w, 128, why))
         return cudaErrorInvalidValue;
     if (split) {
-        int splits = 1;
-        while (splits < 8 && k_blocks / (splits + 1) >= 6 && tiles_split <= dev->clusters[splits]) ++splits;
         cudaLaunchConfig_t lc = {};
         cudaLaunchAttribute at[2];
         cluster_config(lc, at, splits, (int)(tiles_split * splits), GI_THREADS, GS_SMEM, st, pdl);
