@@ -75,17 +75,20 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 }
 
 // W warps hold one row, NG groups of 4 columns per lane: a warp's group is 128 columns, one block of the E4M3 form, and every access is whole
-// lines (128 W (NG - 1) < cols <= 128 W NG).  CTAs stay and walk the rows.  Rows of x and the residual come by bulk copies into a ring of
-// NORM_RING rows in shared memory, so that what is under way does not cost registers.  The weights and conditioning vectors are fetched ahead
-// of the sums that stand before their use, out of the first-level cache: rows pass it by.
-constexpr int NORM_RING = 2;
+// lines (128 W (NG - 1) < cols <= 128 W NG).  CTAs stay and walk the rows; each of a CTA's slots of W warps has room for a row of x and the
+// residual in shared memory, filled by bulk copies while the row before it, by then in registers, is finished.  The weights and conditioning
+// vectors are fetched ahead of the sums that stand before their use, out of the first-level cache: rows pass it by.
+//
+// What bounds it, beyond memory, is the way of one row: two to four sums over its warps, one after another.  Measured at 16380 x 1536 (bf16, fp32
+// residual, RMS twice, 302 MB): 51.9 us; rows in registers one ahead 62, a second row in shared memory 53.4, two rows at a time per slot 55.5,
+// weights and vectors as factors in registers 57 (fewer warps fit), in shared memory with one CTA an SM 58.
 template <typename TX, typename TR, int W, int NG, bool NORM>
 __global__ void __launch_bounds__(W < 4 ? 128 : 32 * W)
 gated_norm_kernel(NormArgs a) {
     using attn::add2; using attn::fma2; using attn::mul2; using attn::pair; using attn::unpair;
     constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W), SPAN = 128 * W;
-    extern __shared__ __align__(16) uint8_t s_ring[];
-    __shared__ uint64_t s_full[RPC][NORM_RING];
+    extern __shared__ __align__(16) uint8_t s_rows[];
+    __shared__ uint64_t s_full[RPC];
     __shared__ int s_abort;
     __shared__ uint32_t s_part[2][THREADS / 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -95,8 +98,7 @@ gated_norm_kernel(NormArgs a) {
     auto in = [&](int i) { return i < NG - 1 || last; };
     const uint32_t x_bytes = a.cols * (uint32_t)sizeof(TX), t_bytes = NORM && a.residual ? a.cols * (uint32_t)sizeof(TR) : 0u;
     if (threadIdx.x == 0) {
-        for (int r = 0; r < RPC; ++r)
-            for (int b = 0; b < NORM_RING; ++b) ptx::mbar_init(&s_full[r][b], 1);
+        for (int r = 0; r < RPC; ++r) ptx::mbar_init(&s_full[r], 1);
         s_abort = 0;
         ptx::fence_barrier_init();
     }
@@ -132,34 +134,32 @@ gated_norm_kernel(NormArgs a) {
     };
     int index = 0;
     const bool mod = NORM && (a.gate || a.scale || a.shift), mb = a.mod_bf16;
-    auto slot_of = [&](int b) { return s_ring + (size_t)(rc * NORM_RING + b) * (x_bytes + t_bytes); };
-    auto request = [&](long long row, int b) {              // by one lane of the row's warps
-        ptx::mbar_expect_tx(&s_full[rc][b], x_bytes + t_bytes);
-        ptx::bulk_load(slot_of(b), static_cast<const TX*>(a.x) + row * a.x_ld, x_bytes, &s_full[rc][b]);
-        if (t_bytes) ptx::bulk_load(slot_of(b) + x_bytes, static_cast<const TR*>(a.residual) + row * a.res_ld, t_bytes, &s_full[rc][b]);
+    uint8_t* s_row = s_rows + (size_t)rc * (x_bytes + t_bytes);
+    auto request = [&](long long row) {                     // by one lane of the row's warps
+        ptx::mbar_expect_tx(&s_full[rc], x_bytes + t_bytes);
+        ptx::bulk_load(s_row, static_cast<const TX*>(a.x) + row * a.x_ld, x_bytes, &s_full[rc]);
+        if (t_bytes) ptx::bulk_load(s_row + x_bytes, static_cast<const TR*>(a.residual) + row * a.res_ld, t_bytes, &s_full[rc]);
     };
     auto request_index = [&](long long row) {
         if (mod) index = a.row_index ? a.row_index[row] : (int)row;
     };
     long long row = (long long)blockIdx.x * RPC + rc;
-    if (wr == 0 && lane == 0)
-        for (int b = 0; b < NORM_RING; ++b)
-            if (row + b * step < rows) request(row + b * step, b);
-    if (row < rows) request_index(row);
+    if (row < rows) {
+        if (wr == 0 && lane == 0) request(row);
+        request_index(row);
+    }
     uint32_t it = 0;
     bool ok = true;                                         // a thread whose wait ran out stores nothing more, but no thread leaves the loop
     for (; row < rows; row += step, ++it) {
-        const int b = it % NORM_RING;
-        const long long ahead = row + NORM_RING * step;
-        // every warp of the row has read its slot: it may be filled again
+        // every warp has the row in its registers: the next one may come
         auto release = [&]() {
             if constexpr (W > 1) row_barrier<RPC, 32 * W>(rc);
             else __syncwarp();
-            if (wr == 0 && lane == 0 && ahead < rows && ok) request(ahead, b);
+            if (wr == 0 && lane == 0 && row + step < rows && ok) request(row + step);
         };
         const int at = index;
         if (row + step < rows) request_index(row + step);
-        ok = ok && ptx::mbar_wait(&s_full[rc][b], (it / NORM_RING) & 1, &s_abort);
+        ok = ok && ptx::mbar_wait(&s_full[rc], it & 1, &s_abort);
         long long g = 0;
         if (mod) {
             if (at < 0 || at >= a.slots) {                  // (the same for every thread of the row)
@@ -170,7 +170,7 @@ gated_norm_kernel(NormArgs a) {
             g = (unsigned)at / (unsigned)a.rows_per_group;
         }
         uint64_t v[NG][2];
-        const TX* xs = reinterpret_cast<const TX*>(slot_of(b)) + col0;
+        const TX* xs = reinterpret_cast<const TX*>(s_row) + col0;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             Raw4<TX> x;
@@ -185,21 +185,25 @@ gated_norm_kernel(NormArgs a) {
         auto normalise = [&](int kind) {                    // v becomes its norm
             if (kind == FD_NORM_NONE) return;
             if (kind == FD_NORM_LAYER) {
-                uint64_t s = v[0][0];
-                s = add2(s, v[0][1]);
+                uint64_t s[4] = {0, 0, 0, 0};               // (four chains: an addition waits for the one before it in its chain)
 #pragma unroll
-                for (int i = 1; i < NG; ++i) s = add2(add2(s, v[i][0]), v[i][1]);
-                const float mean = row_sum(s) * inv_cols;
+                for (int i = 0; i < NG; ++i) {
+                    s[2 * (i & 1)] = add2(s[2 * (i & 1)], v[i][0]);
+                    s[2 * (i & 1) + 1] = add2(s[2 * (i & 1) + 1], v[i][1]);
+                }
+                const float mean = row_sum(add2(add2(s[0], s[1]), add2(s[2], s[3]))) * inv_cols;
                 const uint64_t m = pair(-mean, -mean);
 #pragma unroll
                 for (int i = 0; i < NG; ++i)
                     if (in(i)) { v[i][0] = add2(v[i][0], m); v[i][1] = add2(v[i][1], m); }      // (columns that are not there stay zeros)
             }
-            uint64_t ss = mul2(v[0][0], v[0][0]);
-            ss = fma2(v[0][1], v[0][1], ss);
+            uint64_t ss[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 1; i < NG; ++i) ss = fma2(v[i][1], v[i][1], fma2(v[i][0], v[i][0], ss));
-            const float rstd = rsqrtf(fmaf(row_sum(ss), inv_cols, a.eps));
+            for (int i = 0; i < NG; ++i) {
+                ss[2 * (i & 1)] = fma2(v[i][0], v[i][0], ss[2 * (i & 1)]);
+                ss[2 * (i & 1) + 1] = fma2(v[i][1], v[i][1], ss[2 * (i & 1) + 1]);
+            }
+            const float rstd = rsqrtf(fmaf(row_sum(add2(add2(ss[0], ss[1]), add2(ss[2], ss[3]))), inv_cols, a.eps));
             times(pair(rstd, rstd));
         };
         Raw4<TX> w[NORM ? NG : 1];
@@ -261,7 +265,7 @@ gated_norm_kernel(NormArgs a) {
             if (a.gate) with_mod(f0, [](uint64_t p, uint64_t f) { return attn::mul2(p, f); });
             if (a.residual) {
                 const uint64_t alpha = pair(a.alpha, a.alpha);
-                const TR* ts = reinterpret_cast<const TR*>(slot_of(b) + x_bytes) + col0;
+                const TR* ts = reinterpret_cast<const TR*>(s_row + x_bytes) + col0;
 #pragma unroll
                 for (int i = 0; i < NG; ++i)
                     if (in(i)) {
@@ -349,7 +353,7 @@ gated_norm_kernel(NormArgs a) {
 // Any width, stride and alignment: one CTA a row, element accesses.  A warp takes whole blocks of 128 columns, a lane four columns of a block
 // 32 apart, the same ones in every pass over the row: x, then r, then y stay in shared memory between the passes (STAGED), or, wider than
 // that, are formed again from what is in global memory.  (In place either way: every element is read and written by one thread.)
-constexpr int NORM_ANY_COLS = 12 * 1024;                    // fp32 values in 48 KB
+constexpr int NORM_ANY_COLS = 11 * 1024;                    // fp32 values in 44 KB
 template <typename TX, typename TR, bool STAGED>
 __global__ void __launch_bounds__(256)
 gated_norm_any_kernel(NormArgs a) {
@@ -474,16 +478,16 @@ gated_norm_any_kernel(NormArgs a) {
     ptx::pdl_trigger();
 }
 
-constexpr int NORM_CTAS = 8, NORM_MAX_NG = 6, NORM_MAX_W = 16;
-constexpr int NORM_RING_BYTES = 150 * 1024;     // of rings on an SM: the rest of its 228 KB caches the weights and conditioning vectors
-constexpr int NORM_MAX_SMEM = 200 * 1024;
-static_assert(NORM_RING * 128 * NORM_MAX_W * NORM_MAX_NG * 8 <= NORM_MAX_SMEM, "the widest fp32 rows fit the ring");
+constexpr int NORM_MAX_NG = 6, NORM_MAX_W = 16;
+constexpr int NORM_ROW_BYTES = 150 * 1024;      // of rows on an SM: the rest of its 228 KB caches the weights and conditioning vectors
+constexpr int NORM_MAX_SMEM = 100 * 1024;
+static_assert(128 * NORM_MAX_W * NORM_MAX_NG * 8 <= NORM_MAX_SMEM, "the widest fp32 rows fit");
 
 template <typename TX, typename TR, int W, int NG, bool NORM>
 cudaError_t launch_reg(const NormArgs& a, cudaStream_t st) {
     constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
-    const int smem = RPC * NORM_RING * a.cols * (int)(sizeof(TX) + (NORM && a.residual ? sizeof(TR) : 0));
-    if (smem > 48 * 1024) {
+    const int smem = RPC * a.cols * (int)(sizeof(TX) + (NORM && a.residual ? sizeof(TR) : 0));
+    if (smem > 47 * 1024) {                                 // (48 KB without asking, the fixed part included)
         static std::atomic<uint64_t> raised{0};             // devices on which the kernel may use as much
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
@@ -495,7 +499,17 @@ cudaError_t launch_reg(const NormArgs& a, cudaStream_t st) {
             raised.fetch_or(bit, std::memory_order_relaxed);
         }
     }
-    const int per_sm = max(1, min(NORM_CTAS, NORM_RING_BYTES / smem));
+    // CTAs an SM: those that its registers hold, with at most NORM_ROW_BYTES of rows
+    static std::atomic<int> by_registers{0};
+    int per_sm = by_registers.load(std::memory_order_relaxed);
+    if (!per_sm) {
+        cudaFuncAttributes fa;
+        const cudaError_t e = cudaFuncGetAttributes(&fa, gated_norm_kernel<TX, TR, W, NG, NORM>);
+        if (e != cudaSuccess) return e;
+        per_sm = min(2048 / THREADS, 65536 / (THREADS * ((fa.numRegs + 7) / 8 * 8)));
+        by_registers.store(per_sm, std::memory_order_relaxed);
+    }
+    per_sm = max(1, min(per_sm, NORM_ROW_BYTES / smem));
     const int grid = (int)min((a.rows + RPC - 1) / RPC, 148LL * per_sm);
     return ptx::launch_kernel(gated_norm_kernel<TX, TR, W, NG, NORM>, grid, THREADS, smem, st, a.status == nullptr, a);
 }
