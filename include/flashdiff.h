@@ -486,7 +486,7 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* args, int m, int n, int
  *               (m of the product) is then their capacity.  Rows behind them are not read, and outputs there are left as they were.
  *               fd_regional_step leaves this number at cu_active_out + B.
  *   status_out  optional DEVICE int32 that receives, in stream order, 0, FD_ERR_STATE if an index was refused (its row is skipped:
- *               outputs as they were), or FD_ERR_TIMEOUT if a bounded wait of the product ran out (the result is then incomplete).
+ *               outputs as they were), or FD_ERR_TIMEOUT if a bounded wait of the kernel ran out (the result is then incomplete).
  *
  * 8-bit integers stand for v by a scale over a set of values (a row; a token's head):
  *   a = max(largest |v|, 2^-100),   scale = a / 127,   code = v * (127 / a) rounded to the nearest whole number, ties to even,

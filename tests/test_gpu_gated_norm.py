@@ -173,7 +173,7 @@ def test_strides_and_neighbours(rows, cols, pad, form):
             assert bool((t._base[:, cols:] == (77 if t.dtype in (torch.int8, torch.uint8) else 7.0)).all())
 
 
-@pytest.mark.parametrize("rows,cols", [(19, 512), (7, 333), (2, 9000)])
+@pytest.mark.parametrize("rows,cols", [(19, 512), (7, 333), (2, 9000), (6000, 512), (5000, 99), (2500, 2304)])
 @pytest.mark.parametrize("residual", ["f32", "bf16"])
 def test_in_place(rows, cols, residual):
     s = _case(rows, cols, residual=residual)
@@ -249,6 +249,26 @@ def test_quantise_rows_used_and_strides(used):
     fd.fd_quantize_int8_rows(x, store[:, :400], sc, rows_used=torch.tensor([used], dtype=torch.int32, device="cuda"))
     ref.check_codes(store[:used, :400], sc[:used], x[:used].double()) if used else None
     assert bool((store[used:] == 77).all()) and bool((store[:, 400:] == 77).all()) and bool((sc[used:] == 7.0).all())
+
+
+@pytest.mark.parametrize("form", ["both8", "fp8"])
+@pytest.mark.parametrize("rows,cols", [(6001, 1152), (4999, 256), (3001, 1028)])
+def test_many_rows_of_shuffled_groups(rows, cols, form):
+    """More rows than are held at once, neighbours of different groups, some refused, some behind the used ones."""
+    s, o = _case(rows, cols, groups=7), _outputs(rows, cols, "bf16", "f32", form)
+    bad = torch.arange(5, rows, 101, device="cuda")
+    s["row_index"][bad] = -7
+    used = rows - 300
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    fd.fd_gated_norm(**s, **o, rows_used=torch.tensor([used], dtype=torch.int32, device="cuda"), status_out=status)
+    assert int(status) == fd.FD_ERR_STATE
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[bad] = False
+    keep[used:] = False
+    s2 = dict(s, x=s["x"][keep], residual=s["residual"][keep], row_index=s["row_index"][keep])
+    _check({k: t[keep] for k, t in o.items()}, _want(s2))
+    for t in o.values():
+        assert bool((t[~keep] == (77 if t.dtype in (torch.int8, torch.uint8) else 7.0)).all())
 
 
 def test_rows_past_32_bits():

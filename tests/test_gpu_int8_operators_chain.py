@@ -160,3 +160,31 @@ def test_a_block_on_the_steps_active_rows(name):
         for t in (out, r1, r2):
             assert bool((t[n:] == 4.0).all())
     fd.fd_destroy(ctx)
+
+
+_FIRST_CAPTURED = """
+import torch, paper_2607_12121_b200 as fd
+x, r = torch.ones({rows}, {cols}, device="cuda"), torch.zeros({rows}, {cols}, device="cuda")
+y8, s = torch.zeros({rows}, {cols}, dtype=torch.int8, device="cuda"), torch.zeros({rows}, device="cuda")
+k8, ks = torch.zeros(1, {rows}, 2, 64, dtype=torch.int8, device="cuda"), torch.zeros(1, {rows}, 2, device="cuda")
+back = torch.zeros({rows}, 2, 64, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    fd.fd_gated_norm(x, residual=r, residual_out=r, eps=0.0, y8=y8, y8_scale=s)
+    fd.fd_kv_store_int8(x[:, :128].unflatten(1, (2, 64)), k8, ks)
+    fd.fd_kv_load_int8(k8, ks, back)
+g.replay()
+torch.cuda.synchronize()
+assert bool(((r - 1).abs() < 1e-5).all()) and bool((y8 == 127).all()) and bool(((back - 1).abs() < 1e-6).all())
+"""
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 256), (2000, 9000), (5, 12288), (4, 333)])
+def test_first_call_of_a_process_may_be_captured(rows, cols):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _FIRST_CAPTURED.format(rows=rows, cols=cols)], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
