@@ -1,0 +1,560 @@
+// The norms behind one branch of a block and in front of the next, with the gate and the residual addition between them, in one pass over
+// the rows:  n = post(x) * post_weight,  r = residual_scale * residual + gate[g] * n,  y = pre(r) * pre_weight * (1 + scale[g]) + shift[g],
+// y in the storage type and / or as 8-bit integers with a scale per row or E4M3 codes with a scale per 128 columns.
+// Bound by memory: every element of x and the residual is read once, r and y are written once.
+#pragma once
+#include <atomic>
+
+#include "common.cuh"
+#include "gemm_8bit.cuh"
+#include "ptx.cuh"
+#include "row_vec.cuh"
+
+namespace fd {
+
+// Arguments of the kernels, and the launchers by type of x (one file each: gated_norm.cu, gated_norm_f32.cu)
+struct NormArgs {
+    const void* x;
+    const void* residual;
+    void* residual_out;
+    const void* post_weight;
+    const void* pre_weight;
+    const void* gate;
+    const void* scale;
+    const void* shift;
+    void* y;
+    uint8_t* y8;
+    float* y8_scale;
+    const int32_t* row_index;
+    const int32_t* rows_used;
+    int32_t* status;
+    long long x_ld, res_ld, res_out_ld, gate_ld, scale_ld, shift_ld, y_ld, y8_ld, sc_ld;
+    long long rows, slots;                 // slots = groups * rows_per_group
+    int cols, rows_per_group;
+    int post, pre, y8_int, mod_bf16;       // y8_int: FD_I8, else FD_E4M3
+    float alpha, eps;
+};
+cudaError_t launch_gated_norm_bf16(const NormArgs& a, bool residual_bf16, bool codes_only, cudaStream_t st);
+cudaError_t launch_gated_norm_f32(const NormArgs& a, bool residual_bf16, bool codes_only, cudaStream_t st);
+
+namespace {
+
+// The row's group, or -1 where its index is refused.
+__device__ __forceinline__ int row_group(const NormArgs& a, long long row) {
+    if (!a.gate && !a.scale && !a.shift) return 0;
+    const long long i = a.row_index ? (long long)a.row_index[row] : row;
+    return i >= 0 && i < a.slots ? (int)(i / a.rows_per_group) : -1;
+}
+
+// Barrier of the warps that hold row `rc` of the CTA's RPC rows (barrier 0 is the whole CTA's)
+template <int RPC, int THREADS> __device__ __forceinline__ void row_barrier(int rc) {
+    static_assert(RPC <= 2, "barriers have fixed numbers");
+    if (RPC == 1 || rc == 0) asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+    else asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+}
+
+// Four values of a conditioning vector of either type
+struct RawMod {
+    uint4 q;                                                // bf16: the first half
+    __device__ __forceinline__ void load(const void* p, bool bf16, long long at) {
+        if (bf16) {
+            const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + at);
+            q.x = h.x;
+            q.y = h.y;
+        } else {
+            q = *reinterpret_cast<const uint4*>(static_cast<const float*>(p) + at);
+        }
+    }
+    __device__ __forceinline__ void get(bool bf16, uint64_t* v) const {
+        if (bf16) Raw4<__nv_bfloat16>{make_uint2(q.x, q.y)}.get(v);
+        else Raw4<float>{q}.get(v);
+    }
+};
+
+// magnitudes: the larger of three, NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+    return d;
+}
+
+// W warps hold one row, NG groups of 4 columns per lane: a warp's group is 128 columns, one block of the E4M3 form, and every access is whole
+// lines (128 W (NG - 1) < cols <= 128 W NG).  CTAs stay and walk the rows; each of a CTA's slots of W warps has room for a row of x and the
+// residual in shared memory, filled by bulk copies while the row before it, by then in registers, is finished.  The weights and conditioning
+// vectors are fetched ahead of the sums that stand before their use, out of the first-level cache: rows pass it by.
+//
+// What bounds it, beyond memory, is the way of one row: two to four sums over its warps, one after another.  Measured at 16380 x 1536 (bf16, fp32
+// residual, RMS twice, 302 MB): 51.9 us; rows in registers one ahead 62, a second row in shared memory 53.4, two rows at a time per slot 55.5,
+// weights and vectors as factors in registers 57 (fewer warps fit), in shared memory with one CTA an SM 58.
+template <typename TX, typename TR, int W, int NG, bool NORM>
+__global__ void __launch_bounds__(W < 4 ? 128 : 32 * W)
+gated_norm_kernel(NormArgs a) {
+    using attn::add2; using attn::fma2; using attn::mul2; using attn::pair; using attn::unpair;
+    constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W), SPAN = 128 * W;
+    extern __shared__ __align__(16) uint8_t s_rows[];
+    __shared__ uint64_t s_full[RPC];
+    __shared__ int s_abort;
+    __shared__ uint32_t s_part[2][THREADS / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int wr = warp % W, rc = warp / W;                 // warp within its row, row within the CTA
+    const int col0 = wr * 128 + lane * 4;
+    const bool last = col0 + SPAN * (NG - 1) < a.cols;      // this lane's last group is there
+    auto in = [&](int i) { return i < NG - 1 || last; };
+    const uint32_t x_bytes = a.cols * (uint32_t)sizeof(TX), t_bytes = NORM && a.residual ? a.cols * (uint32_t)sizeof(TR) : 0u;
+    if (threadIdx.x == 0) {
+        for (int r = 0; r < RPC; ++r) ptx::mbar_init(&s_full[r], 1);
+        s_abort = 0;
+        ptx::fence_barrier_init();
+    }
+    __syncthreads();
+    const float inv_cols = 1.0f / (float)a.cols;
+    ptx::pdl_wait();
+    const long long rows = used_rows(a.rows, a.rows_used), step = (long long)gridDim.x * RPC;
+    int turn = 0;                                           // (two turns: a sum has been read before the one after next is written)
+    auto row_sum = [&](uint64_t p) {
+        float v, w;
+        unpair(p, v, w);
+        v = warp_sum(v + w);
+        if constexpr (W > 1) {
+            if (lane == 0) s_part[turn][warp] = __float_as_uint(v);
+            row_barrier<RPC, 32 * W>(rc);
+            v = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) v += __uint_as_float(s_part[turn][rc * W + i]);
+            turn ^= 1;
+        }
+        return v;
+    };
+    auto row_max = [&](uint32_t v) {
+        v = __reduce_max_sync(0xffffffffu, v);
+        if constexpr (W > 1) {
+            if (lane == 0) s_part[turn][warp] = v;
+            row_barrier<RPC, 32 * W>(rc);
+#pragma unroll
+            for (int i = 0; i < W; ++i) v = max(v, s_part[turn][rc * W + i]);
+            turn ^= 1;
+        }
+        return v;
+    };
+    int index = 0;
+    const bool mod = NORM && (a.gate || a.scale || a.shift), mb = a.mod_bf16;
+    uint8_t* s_row = s_rows + (size_t)rc * (x_bytes + t_bytes);
+    auto request = [&](long long row) {                     // by one lane of the row's warps
+        ptx::mbar_expect_tx(&s_full[rc], x_bytes + t_bytes);
+        ptx::bulk_load(s_row, static_cast<const TX*>(a.x) + row * a.x_ld, x_bytes, &s_full[rc]);
+        if (t_bytes) ptx::bulk_load(s_row + x_bytes, static_cast<const TR*>(a.residual) + row * a.res_ld, t_bytes, &s_full[rc]);
+    };
+    auto request_index = [&](long long row) {
+        if (mod) index = a.row_index ? a.row_index[row] : (int)row;
+    };
+    long long row = (long long)blockIdx.x * RPC + rc;
+    if (row < rows) {
+        if (wr == 0 && lane == 0) request(row);
+        request_index(row);
+    }
+    uint32_t it = 0;
+    bool ok = true;                                         // a thread whose wait ran out stores nothing more, but no thread leaves the loop
+    for (; row < rows; row += step, ++it) {
+        // every warp has the row in its registers: the next one may come
+        auto release = [&]() {
+            if constexpr (W > 1) row_barrier<RPC, 32 * W>(rc);
+            else __syncwarp();
+            if (wr == 0 && lane == 0 && row + step < rows && ok) request(row + step);
+        };
+        const int at = index;
+        if (row + step < rows) request_index(row + step);
+        ok = ok && ptx::mbar_wait(&s_full[rc], it & 1, &s_abort);
+        long long g = 0;
+        if (mod) {
+            if (at < 0 || at >= a.slots) {                  // (the same for every thread of the row)
+                if (wr == 0 && lane == 0) report_status(a.status, FD_ERR_STATE);
+                release();
+                continue;
+            }
+            g = (unsigned)at / (unsigned)a.rows_per_group;
+        }
+        uint64_t v[NG][2];
+        const TX* xs = reinterpret_cast<const TX*>(s_row) + col0;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            Raw4<TX> x;
+            x.clear();
+            if (in(i)) x.load(xs + i * SPAN);
+            x.get(v[i]);
+        }
+        auto times = [&](uint64_t f) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) { v[i][0] = mul2(v[i][0], f); v[i][1] = mul2(v[i][1], f); }
+        };
+        auto normalise = [&](int kind) {                    // v becomes its norm
+            if (kind == FD_NORM_NONE) return;
+            if (kind == FD_NORM_LAYER) {
+                uint64_t s[4] = {0, 0, 0, 0};               // (four chains: an addition waits for the one before it in its chain)
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    s[2 * (i & 1)] = add2(s[2 * (i & 1)], v[i][0]);
+                    s[2 * (i & 1) + 1] = add2(s[2 * (i & 1) + 1], v[i][1]);
+                }
+                const float mean = row_sum(add2(add2(s[0], s[1]), add2(s[2], s[3]))) * inv_cols;
+                const uint64_t m = pair(-mean, -mean);
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) { v[i][0] = add2(v[i][0], m); v[i][1] = add2(v[i][1], m); }      // (columns that are not there stay zeros)
+            }
+            uint64_t ss[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                ss[2 * (i & 1)] = fma2(v[i][0], v[i][0], ss[2 * (i & 1)]);
+                ss[2 * (i & 1) + 1] = fma2(v[i][1], v[i][1], ss[2 * (i & 1) + 1]);
+            }
+            const float rstd = rsqrtf(fmaf(row_sum(add2(add2(ss[0], ss[1]), add2(ss[2], ss[3]))), inv_cols, a.eps));
+            times(pair(rstd, rstd));
+        };
+        Raw4<TX> w[NORM ? NG : 1];
+        RawMod f0[NORM ? NG : 1], f1[NORM ? NG : 1];
+        auto fetch_weight = [&](const void* p) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i)
+                if (in(i)) w[i].load(static_cast<const TX*>(p) + col0 + i * SPAN);
+        };
+        auto fetch_mod = [&](RawMod* f, const void* p, long long ld) {
+            const long long from = g * ld + col0;
+            if (mb) {
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) f[i].load(p, true, from + i * SPAN);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) f[i].load(p, false, from + i * SPAN);
+            }
+        };
+        // v = op(v, values) for every group that is there
+        auto with_weight = [&]() {
+#pragma unroll
+            for (int i = 0; i < NG; ++i)
+                if (in(i)) {
+                    uint64_t f[2];
+                    w[i].get(f);
+                    v[i][0] = mul2(v[i][0], f[0]);
+                    v[i][1] = mul2(v[i][1], f[1]);
+                }
+        };
+        auto with_mod = [&](const RawMod* m, auto&& op) {
+            if (mb) {
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) {
+                        uint64_t f[2];
+                        m[i].get(true, f);
+                        v[i][0] = op(v[i][0], f[0]);
+                        v[i][1] = op(v[i][1], f[1]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) {
+                        uint64_t f[2];
+                        m[i].get(false, f);
+                        v[i][0] = op(v[i][0], f[0]);
+                        v[i][1] = op(v[i][1], f[1]);
+                    }
+            }
+        };
+        if constexpr (NORM) {
+            if (a.post_weight) fetch_weight(a.post_weight);
+            if (a.gate) fetch_mod(f0, a.gate, a.gate_ld);
+            normalise(a.post);
+            if (a.post_weight) with_weight();
+            if (a.gate) with_mod(f0, [](uint64_t p, uint64_t f) { return attn::mul2(p, f); });
+            if (a.residual) {
+                const uint64_t alpha = pair(a.alpha, a.alpha);
+                const TR* ts = reinterpret_cast<const TR*>(s_row + x_bytes) + col0;
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) {
+                        Raw4<TR> t;
+                        uint64_t f[2];
+                        t.load(ts + i * SPAN);
+                        t.get(f);
+                        v[i][0] = fma2(alpha, f[0], v[i][0]);
+                        v[i][1] = fma2(alpha, f[1], v[i][1]);
+                    }
+            }
+            const bool more = a.y || a.y8;
+            if (more) {
+                if (a.pre_weight) fetch_weight(a.pre_weight);
+                if (a.scale) fetch_mod(f0, a.scale, a.scale_ld);
+                if (a.shift) fetch_mod(f1, a.shift, a.shift_ld);
+            }
+            release();
+            if (a.residual_out && ok) {
+                TR* p = static_cast<TR*>(a.residual_out) + row * a.res_out_ld + col0;
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) store4(p + i * SPAN, v[i]);
+            }
+            if (!more) continue;
+            normalise(a.pre);
+            if (a.pre_weight) with_weight();
+            if (a.scale) with_mod(f0, [](uint64_t p, uint64_t f) { return attn::mul2(p, attn::add2(f, attn::pair(1.0f, 1.0f))); });
+            if (a.shift) with_mod(f1, [](uint64_t p, uint64_t f) { return attn::add2(p, f); });
+            if (a.y && ok) {
+                TX* p = static_cast<TX*>(a.y) + row * a.y_ld + col0;
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+                    if (in(i)) store4(p + i * SPAN, v[i]);
+            }
+        }
+        if constexpr (!NORM) release();
+        if (!a.y8) continue;
+        uint8_t* y8 = a.y8 + row * a.y8_ld + col0;
+        if (a.y8_int) {
+            float m = 0.f;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                float p[4];
+                unpair(v[i][0], p[0], p[1]);
+                unpair(v[i][1], p[2], p[3]);
+                m = max3_nan(max3_nan(m, p[0], p[1]), p[2], p[3]);
+            }
+            const I8Scale i8 = i8_scale(row_max(abs_bits(m)));
+            if (wr == 0 && lane == 0 && ok) a.y8_scale[row * a.sc_ld] = i8.scale;
+#pragma unroll
+            for (int i = 0; i < NG; ++i)
+                if (in(i) && ok) *reinterpret_cast<uint32_t*>(y8 + i * SPAN) = i8.code4(v[i]);
+        } else if (NORM) {
+            // lane i takes the divisions of the warp's group i (a NaN does not count for a block's scale)
+            float mine = 1.0f;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                float p[4];
+                unpair(v[i][0], p[0], p[1]);
+                unpair(v[i][1], p[2], p[3]);
+                const float m = attn::max3(attn::max3(FP8_AMAX_FLOOR, fabsf(p[0]), fabsf(p[1])), fabsf(p[2]), fabsf(p[3]));
+                const float amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+                if (lane == i) mine = amax;
+            }
+            const float inv = E4M3_MAX / mine;
+            if (lane < NG && wr * 128 + lane * SPAN < a.cols && ok) a.y8_scale[row * a.sc_ld + wr + lane * W] = mine / E4M3_MAX;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float f = __shfl_sync(0xffffffffu, inv, i);
+                float p[4];
+                unpair(v[i][0], p[0], p[1]);
+                unpair(v[i][1], p[2], p[3]);
+                if (in(i) && ok) *reinterpret_cast<uint32_t*>(y8 + i * SPAN) = pack4_e4m3(p[0] * f, p[1] * f, p[2] * f, p[3] * f);
+            }
+        }
+    }
+    if (!ok) {
+        report_status(a.status, FD_ERR_TIMEOUT);
+        gb_settle();                                        // copies under way land before the CTA leaves
+    }
+    ptx::pdl_trigger();
+}
+
+// Any width, stride and alignment: one CTA a row, element accesses.  A warp takes whole blocks of 128 columns, a lane four columns of a block
+// 32 apart, the same ones in every pass over the row: x, then r, then y stay in shared memory between the passes (STAGED), or, wider than
+// that, are formed again from what is in global memory.  (In place either way: every element is read and written by one thread.)
+constexpr int NORM_ANY_COLS = 11 * 1024;                    // fp32 values in 44 KB
+template <typename TX, typename TR, bool STAGED>
+__global__ void __launch_bounds__(256)
+gated_norm_any_kernel(NormArgs a) {
+    extern __shared__ float s_row[];
+    __shared__ uint32_t s_part[2][8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x / 32;
+    ptx::pdl_wait();
+    const long long rows = used_rows(a.rows, a.rows_used);
+    int turn = 0;                                                // (two turns: a sum has been read before the one after next is written)
+    auto block_sum = [&](float v) {
+        v = warp_sum(v);
+        if (lane == 0) s_part[turn][warp] = __float_as_uint(v);
+        __syncthreads();
+        v = 0.f;
+        for (int i = 0; i < warps; ++i) v += __uint_as_float(s_part[turn][i]);
+        turn ^= 1;
+        return v;
+    };
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+        const int g = row_group(a, row);
+        if (g < 0) {
+            if (threadIdx.x == 0) report_status(a.status, FD_ERR_STATE);
+            continue;
+        }
+        const TX* x = static_cast<const TX*>(a.x) + row * a.x_ld;
+        const TR* res = a.residual ? static_cast<const TR*>(a.residual) + row * a.res_ld : nullptr;
+        const TX *post_w = static_cast<const TX*>(a.post_weight), *pre_w = static_cast<const TX*>(a.pre_weight);
+        auto mod = [&](const void* p, long long ld, int c) {
+            const long long at = g * ld + c;
+            return a.mod_bf16 ? to_f(static_cast<const __nv_bfloat16*>(p)[at]) : static_cast<const float*>(p)[at];
+        };
+        const float cols = (float)a.cols;
+        auto each = [&](auto&& f) {                              // f(column) for this thread's columns
+            for (int c0 = warp * 128 + lane; c0 < a.cols; c0 += warps * 128)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c0 + 32 * k < a.cols) f(c0 + 32 * k);
+        };
+        auto norm_of = [&](int kind, auto&& value, float& mean, float& rstd) {      // mean and 1 / deviation of the row's values
+            mean = 0.f;
+            rstd = 1.f;
+            if (kind == FD_NORM_NONE) return;
+            if (kind == FD_NORM_LAYER) {
+                float s = 0.f;
+                each([&](int c) { s += value(c); });
+                mean = block_sum(s) / cols;
+            }
+            float s = 0.f;
+            each([&](int c) {
+                const float d = value(c) - mean;
+                s = fmaf(d, d, s);
+            });
+            rstd = rsqrtf(block_sum(s) / cols + a.eps);
+        };
+        if constexpr (STAGED) each([&](int c) { s_row[c] = to_f<TX>(x[c]); });
+        auto x_of = [&](int c) { return STAGED ? s_row[c] : to_f<TX>(x[c]); };
+        float post_mean, post_rstd, pre_mean, pre_rstd;
+        norm_of(a.post, x_of, post_mean, post_rstd);
+        auto r_formed = [&](int c) {
+            float n = (x_of(c) - post_mean) * post_rstd;
+            if (post_w) n *= to_f<TX>(post_w[c]);
+            if (a.gate) n *= mod(a.gate, a.gate_ld, c);
+            return res ? fmaf(a.alpha, to_f<TR>(res[c]), n) : n;
+        };
+        if constexpr (STAGED) each([&](int c) { s_row[c] = r_formed(c); });
+        auto r_of = [&](int c) { return STAGED ? s_row[c] : r_formed(c); };
+        norm_of(a.pre, r_of, pre_mean, pre_rstd);
+        auto y_formed = [&](float r, int c) {
+            float y = (r - pre_mean) * pre_rstd;
+            if (pre_w) y *= to_f<TX>(pre_w[c]);
+            if (a.scale) y *= 1.0f + mod(a.scale, a.scale_ld, c);
+            return a.shift ? y + mod(a.shift, a.shift_ld, c) : y;
+        };
+        if constexpr (STAGED)
+            each([&](int c) {
+                const float r = s_row[c];
+                if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
+                s_row[c] = y_formed(r, c);
+            });
+        I8Scale i8{};
+        if (a.y8 && a.y8_int) {
+            uint32_t m = 0;
+            each([&](int c) { m = max(m, abs_bits(STAGED ? s_row[c] : y_formed(r_of(c), c))); });
+            m = __reduce_max_sync(0xffffffffu, m);
+            if (lane == 0) s_part[turn][warp] = m;
+            __syncthreads();
+            for (int i = 0; i < warps; ++i) m = max(m, s_part[turn][i]);
+            turn ^= 1;
+            i8 = i8_scale(m);
+            if (threadIdx.x == 0) a.y8_scale[row * a.sc_ld] = i8.scale;
+        }
+        for (int b = warp; b * FP8_BLOCK < a.cols; b += warps) {
+            float v[4], amax = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = b * FP8_BLOCK + k * 32 + lane;
+                v[k] = 0.f;
+                if (c >= a.cols) continue;
+                if constexpr (STAGED) {
+                    v[k] = s_row[c];
+                } else {
+                    const float r = r_of(c);
+                    v[k] = y_formed(r, c);
+                    if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
+                }
+                amax = fmaxf(amax, fabsf(v[k]));
+                if (a.y) static_cast<TX*>(a.y)[row * a.y_ld + c] = from_f<TX>(v[k]);
+                if (a.y8 && a.y8_int) a.y8[row * a.y8_ld + c] = i8.code(v[k]);
+            }
+            if (a.y8 && !a.y8_int) {
+                amax = fmaxf(warp_max(amax), FP8_AMAX_FLOOR);
+                const float inv = E4M3_MAX / amax;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = b * FP8_BLOCK + k * 32 + lane;
+                    if (c < a.cols) a.y8[row * a.y8_ld + c] = __nv_cvt_float_to_fp8(v[k] * inv, __NV_SATFINITE, __NV_E4M3);
+                }
+                if (lane == 0) a.y8_scale[row * a.sc_ld + b] = amax / E4M3_MAX;
+            }
+        }
+    }
+    ptx::pdl_trigger();
+}
+
+constexpr int NORM_MAX_NG = 9, NORM_MAX_W = 16, NORM_MAX_COLS = 12 * 1024;
+constexpr int NORM_ROW_BYTES = 150 * 1024;      // of rows on an SM: the rest of its 228 KB caches the weights and conditioning vectors
+constexpr int NORM_MAX_SMEM = 100 * 1024;
+static_assert(NORM_MAX_COLS * 8 <= NORM_MAX_SMEM && NORM_MAX_COLS <= 128 * 16 * 6, "the widest fp32 rows fit");
+
+template <typename TX, typename TR, int W, int NG, bool NORM>
+cudaError_t launch_reg(const NormArgs& a, cudaStream_t st) {
+    constexpr int THREADS = W < 4 ? 128 : 32 * W, RPC = THREADS / (32 * W);
+    const int smem = RPC * a.cols * (int)(sizeof(TX) + (NORM && a.residual ? sizeof(TR) : 0));
+    if (smem > 47 * 1024) {                                 // (48 KB without asking, the fixed part included)
+        static std::atomic<uint64_t> raised{0};             // devices on which the kernel may use as much
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = 1ull << (dev & 63);
+        if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
+            e = cudaFuncSetAttribute(gated_norm_kernel<TX, TR, W, NG, NORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MAX_SMEM);
+            if (e != cudaSuccess) return e;
+            raised.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    // CTAs an SM: those that its registers hold, with at most NORM_ROW_BYTES of rows
+    static std::atomic<int> by_registers{0};
+    int per_sm = by_registers.load(std::memory_order_relaxed);
+    if (!per_sm) {
+        cudaFuncAttributes fa;
+        const cudaError_t e = cudaFuncGetAttributes(&fa, gated_norm_kernel<TX, TR, W, NG, NORM>);
+        if (e != cudaSuccess) return e;
+        per_sm = min(2048 / THREADS, 65536 / (THREADS * ((fa.numRegs + 7) / 8 * 8)));
+        by_registers.store(per_sm, std::memory_order_relaxed);
+    }
+    per_sm = max(1, min(per_sm, NORM_ROW_BYTES / smem));
+    const int grid = (int)min((a.rows + RPC - 1) / RPC, 148LL * per_sm);
+    return ptx::launch_kernel(gated_norm_kernel<TX, TR, W, NG, NORM>, grid, THREADS, smem, st, a.status == nullptr, a);
+}
+
+template <typename TX, typename TR, int W, bool NORM, int NG = NORM_MAX_NG>
+cudaError_t launch_ng(const NormArgs& a, cudaStream_t st) {
+    if constexpr (NG > 1)
+        if (a.cols <= 128 * W * (NG - 1)) return launch_ng<TX, TR, W, NORM, NG - 1>(a, st);
+    return launch_reg<TX, TR, W, NG, NORM>(a, st);
+}
+
+template <typename TX, typename TR, bool NORM>
+cudaError_t launch_typed(const NormArgs& a, cudaStream_t st) {
+    // four values at a time: rows start at multiples of four elements
+    auto ok = [](const void* p, long long ld, int es) { return !p || (reinterpret_cast<uintptr_t>(p) % (4 * es) == 0 && ld % 4 == 0); };
+    const int xs = sizeof(TX), rs = sizeof(TR), ms = a.mod_bf16 ? 2 : 4;
+    // and those that bulk copies fetch at whole 16-byte units
+    auto whole = [&](const void* p, long long ld, int es) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0 && a.cols * es % 16 == 0); };
+    const bool fast = a.cols % 4 == 0 && a.cols <= NORM_MAX_COLS && whole(a.x, a.x_ld, xs) && whole(a.residual, a.res_ld, rs) &&
+                      ok(a.residual_out, a.res_out_ld, rs) && ok(a.post_weight, 0, xs) && ok(a.pre_weight, 0, xs) && ok(a.gate, a.gate_ld, ms) &&
+                      ok(a.scale, a.scale_ld, ms) && ok(a.shift, a.shift_ld, ms) && ok(a.y, a.y_ld, xs) && ok(a.y8, a.y8_ld, 1);
+    if (!fast) {
+        // (a warp a block of 128 columns, up to eight; the widest staged rows leave room for four CTAs an SM)
+        const int threads = 32 * min(8, (a.cols + 127) / 128), grid = (int)min(a.rows, 148LL * 32);
+        if (a.cols <= NORM_ANY_COLS)
+            return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, true>, grid, threads, a.cols * sizeof(float), st, a.status == nullptr, a);
+        return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, false>, grid, threads, 0, st, a.status == nullptr, a);
+    }
+    // Warps per row: as few as hold it in nine groups a lane (with six: 3997 x 1152 bf16 to 8-bit integers 13.4 us against 12.0, 5000 x 4608
+    // 48.6 against 39.4; with twelve 16380 x 1536 55 against 51); more when the rows alone would leave SMs idle.
+    int w = 1;
+    while (w < NORM_MAX_W && (a.cols > 128 * w * NORM_MAX_NG || (a.cols > 128 * w && a.rows * w < 148 * 4))) w *= 2;
+    switch (w) {
+        case 1: return launch_ng<TX, TR, 1, NORM>(a, st);
+        case 2: return launch_ng<TX, TR, 2, NORM>(a, st);
+        case 4: return launch_ng<TX, TR, 4, NORM>(a, st);
+        case 8: return launch_ng<TX, TR, 8, NORM>(a, st);
+        default: return launch_ng<TX, TR, 16, NORM, 6>(a, st);        // (NORM_MAX_COLS)
+    }
+}
+
+}  // namespace
+
+}  // namespace fd
