@@ -502,13 +502,13 @@ def _type_code(t, name: str) -> int:
 
 def _rows(t, name: str, shape, device: int) -> int:
     """Row stride of the 2-D tensor ``t`` of the wanted shape (rows, columns) on the device, columns contiguous."""
+    if t.is_contiguous() and t.shape == shape and t.get_device() == device and len(shape) == 2:
+        return shape[1]
     if len(shape) != 2:
         _op_fail("%s must have two dimensions, not %s" % (name, list(shape)))
     if t.shape != shape or t.get_device() != device:
         _op_fail("%s must be %s on device %d, not %s on %s" % (name, list(shape), device, list(t.shape), t.device))
     rows, cols = shape
-    if t.is_contiguous():
-        return cols
     stride = t.stride()
     if stride[1] != 1 and cols > 1:
         _op_fail("%s must have contiguous columns" % name)
@@ -846,19 +846,23 @@ def fd_selftest_matmul_int8_wait(a8, a_scale, w8, w_scale, out, status_out, stre
     fd_matmul_int8(a8, a_scale, w8, w_scale, out, None, False, None, status_out, stream, _call_matmul_int8_selftest)
 
 
-def _kv_set(rows, codes, scale, shape, dtype, count: int, device: int):
+def _kv_set(rows, codes, scale, shape, shape_scale, shape_rows, dtype, device: int):
     """A set's addresses and strides: rows [rows, heads, head_dim] or [groups, tokens, heads, head_dim]."""
-    groups, tokens, heads, dh = shape
     if codes.dtype is not _int8 or codes.shape != shape or codes.get_device() != device:
         _op_fail("codes must be int8 %s on device %d" % (list(shape), device))
-    if scale.dtype is not _float32 or scale.shape != shape[:3] or scale.get_device() != device:
-        _op_fail("scales must be float32 %s on device %d" % (list(shape[:3]), device))
-    if rows.dtype is not dtype or rows.get_device() != device or rows.shape[-2:] != shape[2:] or (rows.shape != shape if rows.dim() == 4 else rows.shape[0] != count):
-        _op_fail("rows must be [rows, %d, %d] or %s, of one type and the codes' device" % (heads, dh, list(shape)))
-    rs, cs, ss = rows.stride(), codes.stride(), scale.stride()
-    if dh > 1 and (rs[-1] != 1 or cs[3] != 1):
+    if scale.dtype is not _float32 or scale.shape != shape_scale or scale.get_device() != device:
+        _op_fail("scales must be float32 %s on device %d" % (list(shape_scale), device))
+    if rows.dtype is not dtype or rows.shape != shape_rows or rows.get_device() != device:
+        _op_fail("rows must be %s, of one type and on device %d" % (list(shape_rows), device))
+    c0, c1, c2, c3 = codes.stride()
+    s0, s1, s2 = scale.stride()
+    if len(shape_rows) == 4:
+        r0, r1, r2, r3 = rows.stride()
+    else:
+        r0, (r1, r2, r3) = 0, rows.stride()
+    if (r3 != 1 or c3 != 1) and shape[3] > 1:
         _op_fail("channels must be contiguous")
-    return rows.data_ptr(), codes.data_ptr(), scale.data_ptr(), rs[0] if len(rs) == 4 else 0, rs[-3], rs[-2], cs[0], cs[1], cs[2], ss[0], ss[1], ss[2]
+    return rows.data_ptr(), codes.data_ptr(), scale.data_ptr(), r0, r1, r2, c0, c1, c2, s0, s1, s2
 
 
 def _kv(call, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stream) -> None:
@@ -867,24 +871,29 @@ def _kv(call, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stre
     device, shape, dims = k8.get_device(), k8.shape, k.dim()
     if len(shape) != 4 or dims not in (3, 4):
         _op_fail("codes must be [groups, tokens, heads, head_dim], rows [rows, heads, head_dim] or the codes' shape")
+    groups, tokens, heads, dh = shape
     idx = used = status = 0
     if dims == 3:
         rows = k.shape[0]
+        shape_rows = (rows, heads, dh)
     else:
-        rows = shape[0] * shape[1] if index is None else index.shape[0] if index.dim() == 1 else -1
+        rows = groups * tokens if index is None else index.shape[0] if index.dim() == 1 else -1
+        shape_rows = shape
     if index is not None:
         idx = _index(index, "index", rows, device)
-    if (v is None) != (v8 is None) or (v is None) != (v_scale is None) or (v is not None and v.dim() != dims):
-        _op_fail("v, v8 and v_scale come together, with k's number of dimensions")
-    first = _kv_set(k, k8, k_scale, shape, k.dtype, rows, device)
-    second = first if v is None else _kv_set(v, v8, v_scale, shape, k.dtype, rows, device)
+    dtype, shape_scale = k.dtype, (groups, tokens, heads)
+    first = second = _kv_set(k, k8, k_scale, shape, shape_scale, shape_rows, dtype, device)
+    if v is not None and v8 is not None and v_scale is not None:
+        second = _kv_set(v, v8, v_scale, shape, shape_scale, shape_rows, dtype, device)
+    elif v is not None or v8 is not None or v_scale is not None:
+        _op_fail("v, v8 and v_scale come together")
     if rows_used is not None:
         used = _word(rows_used, "rows_used", device)
     if status_out is not None:
         status = _word(status_out, "status_out", device)
-    if shape.numel() and (rows or status):
-        _op_call(device, stream, call, _pack_kv(*first, *second, idx, used, status, 1 if v is None else 2, shape[2], shape[3], _type_code(k, "rows"),
-                                                shape[0], shape[1], 1 if dims == 4 else 0), rows)
+    if (rows and groups and tokens and heads and dh) or status:
+        _op_call(device, stream, call, _pack_kv(*first, *second, idx, used, status, 1 if v is None else 2, heads, dh, _type_code(k, "rows"), groups, tokens,
+                                                1 if dims == 4 else 0), rows)
 
 
 def fd_kv_store_int8(k, k8, k_scale, v=None, v8=None, v_scale=None, index=None, rows_used=None, status_out=None, stream=None) -> None:
