@@ -54,13 +54,14 @@ struct GiArgs {
     int starve;                                // self-test: no copy is issued, so that every wait for one runs out
 };
 
-// Scale and bias of column col + i for i < 4 (zeros behind n: nothing of those columns is stored)
+// Scale and bias of column col + i for i < 4 (zeros behind n: nothing of those columns is stored).  Plain loads, not those for data that
+// stays the same throughout a launch: the launch before this one, beside which this one may have started, can have written them.
 __device__ __forceinline__ void gi_columns(const GiArgs& g, int col, float* scale, float* bias) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const bool in = col + i < g.n;
-        scale[i] = in ? __ldg(g.w_scale + col + i) : 0.f;
-        bias[i] = !in || !g.bias ? 0.f : g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[col + i]) : __ldg(static_cast<const float*>(g.bias) + col + i);
+        scale[i] = in ? g.w_scale[col + i] : 0.f;
+        bias[i] = !in || !g.bias ? 0.f : g.bias_bf16 ? to_f(static_cast<const __nv_bfloat16*>(g.bias)[col + i]) : static_cast<const float*>(g.bias)[col + i];
     }
 }
 
@@ -247,7 +248,7 @@ gemm_int8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             const uint32_t buf = it & 1, parity = (it >> 1) & 1;
             float sc[4], bi[4];
             gi_columns(g, col0 + 4 * lane, sc, bi);
-            const float a_s = row_base + lane < m_used ? __ldg(g.a_scale + row_base + lane) : 0.f;
+            const float a_s = row_base + lane < m_used ? g.a_scale[row_base + lane] : 0.f;
             __syncwarp();                                        // (the last tile's columns have been read)
             *reinterpret_cast<float4*>(cols + 4 * lane) = make_float4(sc[0], sc[1], sc[2], sc[3]);
             *reinterpret_cast<float4*>(cols + 128 + 4 * lane) = make_float4(bi[0], bi[1], bi[2], bi[3]);
@@ -345,7 +346,7 @@ __device__ __forceinline__ void gs_finish(const GiArgs& g, uint32_t part, int ra
     for (int j = 0; j < ROWS; ++j) {
         const int r = rank * SLICE + 8 * j + w;
         const bool in = r < GI_M && m0 + r < m_used;
-        a_s[j] = in ? __ldg(g.a_scale + m0 + r) : 0.f;
+        a_s[j] = in ? g.a_scale[m0 + r] : 0.f;
 #pragma unroll
         for (int s = 0; s < S; ++s) p[j][s] = in ? load_cluster4(base[s] + gs_unit(r, lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
     }

@@ -162,6 +162,64 @@ def test_a_block_on_the_steps_active_rows(name):
     fd.fd_destroy(ctx)
 
 
+@pytest.mark.parametrize("m,captured", [(20, False), (300, False), (3000, False), (300, True)])
+def test_every_call_reads_what_the_call_before_it_wrote(m, captured):
+    """Scales, codes, conditioning vectors and residual rows that one launch writes and the next reads, over and over in the same memory without
+    a wait between: operands quantised, their product, conditioning vectors out of a product, a norm that uses them, its rows into a cache
+    and back."""
+    k, n, H, B = 512, 384, 256, 2
+    g = torch.Generator(device="cuda").manual_seed(m)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")          # noqa: E731
+    steps = 12
+    xs, ws, conds = [rnd(m, k) * (i + 1) for i in range(steps)], [rnd(n, k) / (i + 1) for i in range(steps)], [rnd(B, k) * (1 + i % 3) for i in range(steps)]
+    x, w, cond = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda"), torch.empty(B, k, device="cuda")
+    a8, a_s = torch.empty(m, k, dtype=torch.int8, device="cuda"), torch.empty(m, device="cuda")
+    w8, w_s = torch.empty(n, k, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+    c8, c_s = torch.empty(B, k, dtype=torch.int8, device="cuda"), torch.empty(B, device="cuda")
+    wm, wm_s = ref.quantise(rnd(3 * H, k) * 0.02)
+    out, mod = torch.empty(m, n, device="cuda"), torch.empty(B, 3 * H, device="cuda")
+    y, r = torch.empty(m, H, device="cuda"), torch.empty(m, H, device="cuda")
+    k8, ks, back = torch.empty(1, m, 4, 64, dtype=torch.int8, device="cuda"), torch.empty(1, m, 4, device="cuda"), torch.empty(m, 4, 64, device="cuda")
+
+    def work():
+        fd.fd_quantize_int8_rows(x, a8, a_s)
+        fd.fd_quantize_int8_rows(w, w8, w_s)
+        fd.fd_matmul_int8(a8, a_s, w8, w_s, out)
+        fd.fd_quantize_int8_rows(cond, c8, c_s)
+        fd.fd_matmul_int8(c8, c_s, wm, wm_s, mod)
+        fd.fd_gated_norm(out[:, :H], residual=out[:, n - H:], residual_out=r, gate=mod[:, :H], scale=mod[:, H: 2 * H], shift=mod[:, 2 * H:], y=y)
+        fd.fd_kv_store_int8(y.unflatten(1, (4, 64)), k8, ks)
+        fd.fd_kv_load_int8(k8, ks, back)
+
+    graph = None
+    if captured:
+        x.copy_(xs[0]), w.copy_(ws[0]), cond.copy_(conds[0])
+        work()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            work()
+    kept = []
+    for i in range(steps):
+        x.copy_(xs[i]), w.copy_(ws[i]), cond.copy_(conds[i])
+        graph.replay() if captured else work()
+        kept.append([t.clone() for t in (a8, a_s, w8, w_s, out, c8, c_s, mod, r, y, k8, ks, back)])
+    group = torch.arange(m, device="cuda") // -(-m // B)
+    for i, (a8_, a_s_, w8_, w_s_, out_, c8_, c_s_, mod_, r_, y_, k8_, ks_, back_) in enumerate(kept):
+        ref.check_codes(a8_, a_s_, xs[i].double())
+        ref.check_codes(w8_, w_s_, ws[i].double())
+        ref.near(out_, *ref.matmul(a8_, a_s_, w8_, w_s_))
+        ref.check_codes(c8_, c_s_, conds[i].double())
+        ref.near(mod_, *ref.matmul(c8_, c_s_, wm, wm_s))
+        (want_r, r_err), (want_y, y_err) = ref.gated_norm(out_[:, :H], out_[:, n - H:], 1.0, "rms", None, mod_[:, :H], "rms", None, mod_[:, H: 2 * H],
+                                                          mod_[:, 2 * H:], group=group)
+        ref.near(r_, want_r, r_err)
+        ref.near(y_, want_y, y_err)
+        ref.check_codes(k8_[0], ks_[0], y_.double().unflatten(1, (4, 64)))
+        value = k8_[0].double() * ks_[0].double()[..., None]
+        ref.near(back_, value, ref.U32 * value.abs())
+
+
 _FIRST_CAPTURED = """
 import torch, paper_2607_12121_b200 as fd
 x, r = torch.ones({rows}, {cols}, device="cuda"), torch.zeros({rows}, {cols}, device="cuda")
