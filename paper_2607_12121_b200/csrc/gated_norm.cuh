@@ -6,6 +6,7 @@
 // (88 MB) 19.9; 3997 x 1152, all bf16, to 8-bit integers 12.0; 8500 x 1536 quantised alone (39 MB) 8.3; one token 3.1.
 #pragma once
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "gemm_8bit.cuh"
@@ -357,13 +358,144 @@ gated_norm_kernel(NormArgs a) {
 }
 
 // Any width, stride and alignment: one CTA a row, element accesses.  A warp takes whole blocks of 128 columns, a lane four columns of a block
-// 32 apart, the same ones in every pass over the row: x, then r, then y stay in shared memory between the passes (STAGED), or, wider than
-// that, are formed again from what is in global memory.  (In place either way: every element is read and written by one thread.)
-constexpr int NORM_ANY_COLS = 11 * 1024;                    // fp32 values in 44 KB
-template <typename TX, typename TR, bool STAGED>
-__global__ void __launch_bounds__(256)
+// 32 apart, and keeps its MB blocks' values in registers from x over r to y; vectors are applied one after another, so that a vector's loads
+// are under way together.  Bound by accesses of single elements: 5000 x 1333 in 37.7 us (62 with the row in shared memory and all vectors'
+// elements looked up one by one), quantised alone 18.5.
+template <typename TX, typename TR, int WARPS, int MB>
+__global__ void __launch_bounds__(32 * WARPS)
 gated_norm_any_kernel(NormArgs a) {
-    extern __shared__ float s_row[];
+    constexpr int N = 4 * MB;                                    // values of a lane
+    __shared__ uint32_t s_part[2][WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col0 = warp * 128 + lane;
+    auto off = [](int i) { return (i >> 2) * WARPS * 128 + (i & 3) * 32; };
+    ptx::pdl_wait();
+    const long long rows = used_rows(a.rows, a.rows_used);
+    const float cols = (float)a.cols;
+    int turn = 0;                                                // (two turns: a sum has been read before the one after next is written)
+    auto block_sum = [&](float v) {
+        v = warp_sum(v);
+        if (lane == 0) s_part[turn][warp] = __float_as_uint(v);
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) v += __uint_as_float(s_part[turn][i]);
+        turn ^= 1;
+        return v;
+    };
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+        const int g = row_group(a, row);
+        if (g < 0) {
+            if (threadIdx.x == 0) report_status(a.status, FD_ERR_STATE);
+            continue;
+        }
+        float v[N];                                              // (columns that are not there are zeros)
+        auto in = [&](int i) { return col0 + off(i) < a.cols; };
+        auto load = [&](auto* p, float* f) {                     // a row or a vector of values
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = in(i) ? to_f(p[off(i)]) : 0.f;
+        };
+        auto load_mod = [&](const void* p, long long ld, float* f) {
+            if (a.mod_bf16) load(static_cast<const __nv_bfloat16*>(p) + g * ld + col0, f);
+            else load(static_cast<const float*>(p) + g * ld + col0, f);
+        };
+        auto normalise = [&](int kind) {                         // v becomes its norm
+            if (kind == FD_NORM_NONE) return;
+            if (kind == FD_NORM_LAYER) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum += v[i];
+                const float mean = block_sum(sum) / cols;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (in(i)) v[i] -= mean;
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum = fmaf(v[i], v[i], sum);
+            const float rstd = rsqrtf(block_sum(sum) / cols + a.eps);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= rstd;
+        };
+        float f[N];
+        load(static_cast<const TX*>(a.x) + row * a.x_ld + col0, v);
+        normalise(a.post);
+        if (a.post_weight) {
+            load(static_cast<const TX*>(a.post_weight) + col0, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= f[i];
+        }
+        if (a.gate) {
+            load_mod(a.gate, a.gate_ld, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= f[i];
+        }
+        if (a.residual) {
+            load(static_cast<const TR*>(a.residual) + row * a.res_ld + col0, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = fmaf(a.alpha, f[i], v[i]);
+        }
+        auto store = [&](auto* p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (in(i)) p[off(i)] = from_f<typename std::remove_pointer<decltype(p)>::type>(v[i]);
+        };
+        if (a.residual_out) store(static_cast<TR*>(a.residual_out) + row * a.res_out_ld + col0);
+        if (!a.y && !a.y8) continue;
+        normalise(a.pre);
+        if (a.pre_weight) {
+            load(static_cast<const TX*>(a.pre_weight) + col0, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= f[i];
+        }
+        if (a.scale) {
+            load_mod(a.scale, a.scale_ld, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= 1.0f + f[i];
+        }
+        if (a.shift) {
+            load_mod(a.shift, a.shift_ld, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += f[i];
+        }
+        if (a.y) store(static_cast<TX*>(a.y) + row * a.y_ld + col0);
+        if (!a.y8) continue;
+        uint8_t* y8 = a.y8 + row * a.y8_ld + col0;
+        if (a.y8_int) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) m = max(m, abs_bits(v[i]));
+            m = __reduce_max_sync(0xffffffffu, m);
+            if (lane == 0) s_part[turn][warp] = m;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) m = max(m, s_part[turn][i]);
+            turn ^= 1;
+            const I8Scale i8 = i8_scale(m);
+            if (threadIdx.x == 0) a.y8_scale[row * a.sc_ld] = i8.scale;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (in(i)) y8[off(i)] = i8.code(v[i]);
+        } else {
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                if ((b * WARPS + warp) * FP8_BLOCK >= a.cols) break;
+                const float m = fmaxf(fmaxf(fabsf(v[4 * b]), fabsf(v[4 * b + 1])), fmaxf(fabsf(v[4 * b + 2]), fabsf(v[4 * b + 3])));
+                const float amax = fmaxf(warp_max(m), FP8_AMAX_FLOOR), inv = E4M3_MAX / amax;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (in(4 * b + k)) y8[off(4 * b + k)] = __nv_cvt_float_to_fp8(v[4 * b + k] * inv, __NV_SATFINITE, __NV_E4M3);
+                if (lane == 0) a.y8_scale[row * a.sc_ld + b * WARPS + warp] = amax / E4M3_MAX;
+            }
+        }
+    }
+    ptx::pdl_trigger();
+}
+
+// Rows of any kind that are wider than registers hold: each is read again for every sum.  A lane's columns are the same ones in every pass, so
+// that the in-place forms hold: every element is read and written by one thread.
+template <typename TX, typename TR>
+__global__ void __launch_bounds__(256)
+gated_norm_wide_kernel(NormArgs a) {
     __shared__ uint32_t s_part[2][8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x / 32;
     ptx::pdl_wait();
@@ -414,18 +546,15 @@ gated_norm_any_kernel(NormArgs a) {
             });
             rstd = rsqrtf(block_sum(s) / cols + a.eps);
         };
-        if constexpr (STAGED) each([&](int c) { s_row[c] = to_f<TX>(x[c]); });
-        auto x_of = [&](int c) { return STAGED ? s_row[c] : to_f<TX>(x[c]); };
+        auto x_of = [&](int c) { return to_f<TX>(x[c]); };
         float post_mean, post_rstd, pre_mean, pre_rstd;
         norm_of(a.post, x_of, post_mean, post_rstd);
-        auto r_formed = [&](int c) {
+        auto r_of = [&](int c) {
             float n = (x_of(c) - post_mean) * post_rstd;
             if (post_w) n *= to_f<TX>(post_w[c]);
             if (a.gate) n *= mod(a.gate, a.gate_ld, c);
             return res ? fmaf(a.alpha, to_f<TR>(res[c]), n) : n;
         };
-        if constexpr (STAGED) each([&](int c) { s_row[c] = r_formed(c); });
-        auto r_of = [&](int c) { return STAGED ? s_row[c] : r_formed(c); };
         norm_of(a.pre, r_of, pre_mean, pre_rstd);
         auto y_formed = [&](float r, int c) {
             float y = (r - pre_mean) * pre_rstd;
@@ -433,16 +562,10 @@ gated_norm_any_kernel(NormArgs a) {
             if (a.scale) y *= 1.0f + mod(a.scale, a.scale_ld, c);
             return a.shift ? y + mod(a.shift, a.shift_ld, c) : y;
         };
-        if constexpr (STAGED)
-            each([&](int c) {
-                const float r = s_row[c];
-                if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
-                s_row[c] = y_formed(r, c);
-            });
         I8Scale i8{};
         if (a.y8 && a.y8_int) {
             uint32_t m = 0;
-            each([&](int c) { m = max(m, abs_bits(STAGED ? s_row[c] : y_formed(r_of(c), c))); });
+            each([&](int c) { m = max(m, abs_bits(y_formed(r_of(c), c))); });
             m = __reduce_max_sync(0xffffffffu, m);
             if (lane == 0) s_part[turn][warp] = m;
             __syncthreads();
@@ -458,13 +581,9 @@ gated_norm_any_kernel(NormArgs a) {
                 const int c = b * FP8_BLOCK + k * 32 + lane;
                 v[k] = 0.f;
                 if (c >= a.cols) continue;
-                if constexpr (STAGED) {
-                    v[k] = s_row[c];
-                } else {
-                    const float r = r_of(c);
-                    v[k] = y_formed(r, c);
-                    if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
-                }
+                const float r = r_of(c);
+                v[k] = y_formed(r, c);
+                if (a.residual_out) static_cast<TR*>(a.residual_out)[row * a.res_out_ld + c] = from_f<TR>(r);
                 amax = fmaxf(amax, fabsf(v[k]));
                 if (a.y) static_cast<TX*>(a.y)[row * a.y_ld + c] = from_f<TX>(v[k]);
                 if (a.y8 && a.y8_int) a.y8[row * a.y8_ld + c] = i8.code(v[k]);
@@ -538,11 +657,14 @@ cudaError_t launch_typed(const NormArgs& a, cudaStream_t st) {
                       ok(a.residual_out, a.res_out_ld, rs) && ok(a.post_weight, 0, xs) && ok(a.pre_weight, 0, xs) && ok(a.gate, a.gate_ld, ms) &&
                       ok(a.scale, a.scale_ld, ms) && ok(a.shift, a.shift_ld, ms) && ok(a.y, a.y_ld, xs) && ok(a.y8, a.y8_ld, 1);
     if (!fast) {
-        // (a warp a block of 128 columns, up to eight; 5000 x 1333 in 62 us: bound by accesses of single elements)
-        const int threads = 32 * min(8, (a.cols + 127) / 128), grid = (int)min(a.rows, 148LL * 32);
-        if (a.cols <= NORM_ANY_COLS)
-            return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, true>, grid, threads, a.cols * sizeof(float), st, a.status == nullptr, a);
-        return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, false>, grid, threads, 0, st, a.status == nullptr, a);
+        const int grid = (int)min(a.rows, 148LL * 64), blocks = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
+        const bool pdl = a.status == nullptr;
+        if (blocks <= 4) return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 4, 1>, grid, 128, 0, st, pdl, a);
+        if (blocks <= 8) return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 4, 2>, grid, 128, 0, st, pdl, a);
+        if (blocks <= 16) return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 4, 4>, grid, 128, 0, st, pdl, a);
+        if (blocks <= 32) return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 8, 4>, grid, 256, 0, st, pdl, a);
+        if (blocks <= 64) return ptx::launch_kernel(gated_norm_any_kernel<TX, TR, 8, 8>, grid, 256, 0, st, pdl, a);
+        return ptx::launch_kernel(gated_norm_wide_kernel<TX, TR>, grid, 256, 0, st, pdl, a);
     }
     // Warps per row: as few as hold it in nine groups a lane (with six: 3997 x 1152 bf16 to 8-bit integers 13.4 us against 12.0, 5000 x 4608
     // 48.6 against 39.4; with twelve 16380 x 1536 55 against 51); more when the rows alone would leave SMs idle.

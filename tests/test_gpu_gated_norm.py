@@ -94,10 +94,10 @@ def test_types_and_norms(rows, cols, form, post, pre, x, residual, mod):
     _check(o, _want(s, post_norm=post, pre_norm=pre))
 
 
-@pytest.mark.parametrize("cols", [8000, 8192, 8200, 11263, 11264, 11265, 12281, 12288, 12296])
+@pytest.mark.parametrize("cols", [511, 513, 1023, 1025, 2047, 2049, 4095, 4097, 8000, 8191, 8192, 8193, 8200, 11265, 12281, 12288, 12296])
 @pytest.mark.parametrize("x,residual", [("bf16", "f32"), ("f32", "f32"), ("bf16", "bf16")])
-def test_widest_rows(cols, x, residual):
-    """Rows around the largest that are held in one piece, whole units or not, with and without a residual."""
+def test_widths_between_forms(cols, x, residual):
+    """Rows around the largest that each form holds, whole units or not, with and without a residual."""
     s, o = _case(3, cols, x, residual), _outputs(3, cols, x, residual, "both8")
     fd.fd_gated_norm(**s, **o)
     _check(o, _want(s))
