@@ -1,0 +1,126 @@
+"""GPU: lists of a store that are not strictly ascending.  No slot is written by two rows, whatever the list: a row counts only if its index is a
+slot above the index before it and above every slot named before it, in rows that do not count too."""
+import pytest
+import torch
+
+import int8_ref as ref
+import paper_2607_12121_b200 as fd
+
+pytestmark = pytest.mark.gpu
+
+
+def _kept(index, slots):
+    """The rows that the rule keeps; no slot comes twice, and a list that ascends keeps them all."""
+    top, kept = -1, []
+    for i, s in enumerate(index):
+        if 0 <= s < slots:
+            if s > top and not (i > 0 and index[i - 1] >= s):
+                kept.append(i)
+            top = max(top, s)
+    named = [index[i] for i in kept]
+    assert len(set(named)) == len(named)
+    assert len(kept) == len(index) or not (sorted(set(index)) == list(index) and 0 <= index[0] and index[-1] < slots)
+    return kept
+
+
+def _run(index, slots, heads, dh, source="rows", used=None, sets=2, dt=torch.bfloat16, replay=False):
+    n = len(index)
+    count = n if used is None else used
+    g = torch.Generator(device="cuda").manual_seed(n + heads + dh)
+    rows = torch.randn(2, n if source == "rows" else slots, heads, dh, generator=g, device="cuda").to(dt)
+    codes = torch.full((2, 1, slots, heads, dh), 55, dtype=torch.int8, device="cuda")
+    scale = torch.full((2, 1, slots, heads), 9.0, device="cuda")
+    idx, status = torch.tensor(index, dtype=torch.int32, device="cuda"), torch.full((1,), 5, dtype=torch.int32, device="cuda")
+    word = None if used is None else torch.tensor([used], dtype=torch.int32, device="cuda")
+    src = [t if source == "rows" else t[None] for t in rows]
+    second = (src[1], codes[1], scale[1]) if sets == 2 else ()
+
+    def store(**kw):
+        fd.fd_kv_store_int8(src[0], codes[0], scale[0], *second, index=idx, rows_used=word, **kw)
+
+    if replay:
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            store(status_out=status)
+        graph.replay()
+    else:
+        store(status_out=status)
+    kept = _kept(index[:count], slots)
+    assert int(status) == (0 if len(kept) == count else fd.FD_ERR_STATE)
+    at = idx[torch.tensor(kept, dtype=torch.long, device="cuda")].long()
+    rest = torch.ones(slots, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    for half in range(2):
+        c, s = codes[half, 0], scale[half, 0]
+        if half < sets and kept:
+            ref.check_codes(c[at], s[at], rows[half][kept if source == "rows" else at].double())
+        untouched = rest if half < sets else torch.ones_like(rest)
+        assert bool((c[untouched] == 55).all()) and bool((s[untouched] == 9.0).all())
+    before = codes.clone(), scale.clone()                       # the same again, without the word: the same slots get the same
+    store()
+    assert torch.equal(codes, before[0]) and torch.equal(scale, before[1])
+
+
+@pytest.mark.parametrize("index", [[5, 3, 5], [5, -1, 5], [0, 1, 2, 0, 1, 2], [3, 5, 3, 4, 5], [7, 50, 7], [2 ** 31 - 1, 4, 6, 4, 6], [9, 9, 9], [4, 3, 2, 1, 0],
+                                   [-2 ** 31, 0, -1, 0, 1], [0], [49], [50], [-1]])
+@pytest.mark.parametrize("heads,dh", [(1, 8), (3, 64), (16, 72), (5, 50), (12, 128), (2, 250)])
+def test_short_lists(index, heads, dh):
+    _run(index, 50, heads, dh)
+    _run(index, 50, heads, dh, "slots", sets=1, dt=torch.float32)
+
+
+def _long(n, slots, kind):
+    g = torch.Generator().manual_seed(n + len(kind))
+    up = torch.randperm(slots, generator=g)[:n].sort().values
+    if kind == "two numberings":                                # of two requests, each from zero
+        up = torch.cat([torch.arange(n // 2), torch.arange(n - n // 2)])
+    elif kind == "random":
+        up = torch.randint(-2, slots + 2, (n,), generator=g)
+    elif kind == "one returns":                                 # the first slot once more, far behind
+        up[n - 2] = up[0]
+    elif kind == "repeats":
+        up = torch.arange(n) // 2 % slots
+    elif kind == "a hole":
+        up[n // 3] = -1
+    elif kind == "swaps":                                       # every 97th pair of neighbours the wrong way round
+        for i in range(5, n - 1, 97):
+            up[[i, i + 1]] = up[[i + 1, i]]
+    elif kind == "first is last":
+        up[0] = slots - 1
+    elif kind == "holes":                                       # every 256th row, a run of rows, and the end name no slot
+        up[256::256] = -1
+        up[n // 2: n // 2 + 300] = -1
+        up[n - n // 3:] = -1
+    elif kind == "halves swapped":
+        up = torch.cat([up[n // 2:], up[: n // 2]])
+    return up.tolist()
+
+
+@pytest.mark.parametrize("kind", ["ascending", "two numberings", "random", "one returns", "repeats", "a hole", "swaps", "first is last", "holes", "halves swapped"])
+@pytest.mark.parametrize("n,slots,heads,dh", [(4099, 6000, 12, 128), (3001, 3300, 1, 64), (20011, 40000, 2, 40), (2500, 5000, 65, 16), (3001, 4000, 3, 50), (700, 900, 24, 96)])
+def test_long_lists(n, slots, heads, dh, kind):
+    """Lists over many CTAs, heads that leave a row to two of them among them."""
+    _run(_long(n, slots, kind), slots, heads, dh)
+
+
+@pytest.mark.parametrize("used", [0, 1, 77, 999, 1000])
+@pytest.mark.parametrize("kind", ["ascending", "random", "one returns"])
+def test_rows_behind_the_used_ones_do_not_count(used, kind):
+    index = _long(1000, 1500, kind)
+    _run(index, 1500, 4, 64, used=used, replay=True)
+    _run(index, 1500, 3, 30, used=used, source="slots")
+
+
+@pytest.mark.parametrize("offset", [0, 1, 2, 3])
+def test_lists_that_begin_anywhere(offset):
+    """The list as a slice of a longer one, at every alignment of its address."""
+    whole = torch.tensor([7] * offset + _long(2003, 2500, "one returns"), dtype=torch.int32, device="cuda")
+    k = torch.randn(2003, 2, 64, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    k8, ks = torch.full((1, 2500, 2, 64), 55, dtype=torch.int8, device="cuda"), torch.full((1, 2500, 2), 9.0, device="cuda")
+    fd.fd_kv_store_int8(k, k8, ks, index=whole[offset:])
+    index = whole[offset:].tolist()
+    kept = _kept(index, 2500)
+    assert len(kept) == 2002                                    # (all but the row whose slot returns)
+    at = torch.tensor([index[i] for i in kept], device="cuda")
+    ref.check_codes(k8[0, at], ks[0, at], k[kept].double())
