@@ -614,6 +614,13 @@ fd_status fd_selftest_matmul_wait(const fd_matmul_fp8_args* args, int m, int n, 
 /* The same for fd_matmul_int8. */
 fd_status fd_selftest_matmul_int8_wait(const fd_matmul_int8_args* args, int m, int n, int k, void* cuda_stream);
 
+/*
+ * The same for fd_gated_norm (and fd_quantize_int8_rows, whose kernel is that of FD_NORM_NONE twice with y8 alone): no row is fetched, status_out
+ * receives FD_ERR_TIMEOUT, and the outputs stay as they were.  FD_ERR_SHAPE where the kernel for these rows waits for nothing (rows
+ * that are not whole 16-byte units, or wider than 12288 columns).
+ */
+fd_status fd_selftest_gated_norm_wait(const fd_gated_norm_args* args, int64_t rows, int cols, void* cuda_stream);
+
 /* Number of kernels the library has launched through this context so far (host counter). */
 int64_t fd_launch_count(const fd_ctx* ctx);
 

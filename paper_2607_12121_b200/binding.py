@@ -30,7 +30,7 @@ EXPORTS = ["fd_workspace_bytes", "fd_create", "fd_partition_regions", "fd_region
            "fd_set_text_stream", "fd_set_cross_attention", "fd_set_fp8_operands", "fd_debug_buffer", "fd_set_fp8_text_stream",
            "fd_rope_axes", "fd_rope_axes_tables", "fd_add_rmsnorm", "fd_quantize_fp8_blocks", "fd_matmul_fp8_blocks",
            "fd_selftest_matmul_wait", "fd_gated_norm", "fd_quantize_int8_rows", "fd_matmul_int8", "fd_kv_store_int8", "fd_kv_load_int8",
-           "fd_selftest_matmul_int8_wait"]
+           "fd_selftest_matmul_int8_wait", "fd_selftest_gated_norm_wait"]
 FD_NOALLOC_MAX_REGION_SLOTS = 16384
 PROF_GROUPS = ["activity", "compact", "adaln", "ln_modulate", "gemm_qkv", "attention", "gemm_out", "gemm_fc1",
                "gemm_fc2", "partition", "sampler", "qk_variants", "cross_attention"]
@@ -198,8 +198,9 @@ def _load() -> ctypes.CDLL:
     lib.fd_matmul_fp8_blocks.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
     lib.fd_selftest_matmul_wait.restype = i32
     lib.fd_selftest_matmul_wait.argtypes = [ctypes.POINTER(FdMatmulFp8Args), i32, i32, i32, vp]
-    lib.fd_gated_norm.restype = i32
-    lib.fd_gated_norm.argtypes = [ctypes.POINTER(FdGatedNormArgs), i64, i32, vp]
+    for name in ("fd_gated_norm", "fd_selftest_gated_norm_wait"):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [ctypes.POINTER(FdGatedNormArgs), i64, i32, vp]
     lib.fd_quantize_int8_rows.restype = i32
     lib.fd_quantize_int8_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, vp, vp]
     lib.fd_matmul_int8.restype = i32
@@ -482,6 +483,7 @@ def _packed(name: str, *argtypes):
 _call_rmsnorm = _packed("fd_add_rmsnorm", ctypes.c_int64, ctypes.c_int)
 _call_matmul = _packed("fd_matmul_fp8_blocks", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 _call_gated_norm = _packed("fd_gated_norm", ctypes.c_int64, ctypes.c_int)
+_call_gated_norm_selftest = _packed("fd_selftest_gated_norm_wait", ctypes.c_int64, ctypes.c_int)
 _call_matmul_int8 = _packed("fd_matmul_int8", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 _call_matmul_int8_selftest = _packed("fd_selftest_matmul_int8_wait", ctypes.c_int, ctypes.c_int, ctypes.c_int)
 _call_kv_store = _packed("fd_kv_store_int8", ctypes.c_int64)
@@ -723,12 +725,13 @@ def _int8_rows(t, name: str, shape, device: int) -> int:
 
 def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1.0, post_norm="rms", post_weight=None, gate=None, pre_norm="rms",
                   pre_weight=None, scale=None, shift=None, eps: float = 1e-6, rows_per_group=None, row_index=None, rows_used=None, y=None, y8=None,
-                  y8_scale=None, status_out=None, stream=None) -> None:
+                  y8_scale=None, status_out=None, stream=None, _call=_call_gated_norm) -> None:
     """n = post(x) * post_weight, r = residual_scale * residual + gate[g] * n (kept in residual_out), y = pre(r) * pre_weight * (1 + scale[g]) +
     shift[g], on rows [rows, cols].  Norms: "rms", "layer" or None.  gate, scale, shift [groups, cols]: one type, any row stride; the row's g is
     (row_index or the row's own number) // rows_per_group (default: rows over groups, rounded up).  Outputs y in x's type and / or y8: int8 with
     y8_scale [rows], or E4M3 codes with y8_scale [rows, ceil(cols / 128)].  rows_used, status_out: int32 device scalars, the number of
-    rows in use and what receives 0 or FD_ERR_STATE (a row_index that is no row of any group)."""
+    rows in use and what receives 0, FD_ERR_STATE (a row_index that is no row of any group) or FD_ERR_TIMEOUT (a bounded wait of the kernel ran
+    out; without it an incomplete result goes unreported)."""
     if _float32 is None:
         _torch_names()
     shape, device, dtype = x.shape, x.get_device(), x.dtype
@@ -792,10 +795,16 @@ def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1
     if not 0.0 <= eps < 3.0e38 or not abs(residual_scale) < 3.0e38:
         _op_fail("eps must be non-negative and finite, residual_scale finite")
     if rows or status:
-        _op_call(device, stream, _call_gated_norm, _pack_gated_norm(
+        _op_call(device, stream, _call, _pack_gated_norm(
             x.data_ptr(), r, ro, w1, w2, pg, psc, psh, py, p8, ps, idx, used, status, x_stride, r_stride, ro_stride, g_stride, sc_stride, sh_stride,
             y_stride, y8_stride, s_stride, _type_code(x, "x"), r_type, mod_type, y8_type, _NORMS[post_norm], _NORMS[pre_norm], groups, per_group,
             residual_scale, eps), rows, cols)
+
+
+def fd_selftest_gated_norm_wait(x, status_out, stream=None, **kw) -> None:
+    """fd_gated_norm (its other arguments by name) without its rows' copies: every wait runs out, status_out receives FD_ERR_TIMEOUT and
+    the outputs stay as they were."""
+    fd_gated_norm(x, status_out=status_out, stream=stream, _call=_call_gated_norm_selftest, **kw)
 
 
 def fd_quantize_int8_rows(x, y8, y8_scale, rows_used=None, stream=None) -> None:

@@ -1020,7 +1020,7 @@ fd_status op_no_rows(const char* who, int32_t* status_out, void* cuda_stream) {
 }
 bool norm_kind(int k) { return k == FD_NORM_NONE || k == FD_NORM_RMS || k == FD_NORM_LAYER; }
 
-fd_status gated_norm_call(const char* who, const fd_gated_norm_args& a, int64_t rows, int cols, void* cuda_stream) {
+fd_status gated_norm_call(const char* who, const fd_gated_norm_args& a, int64_t rows, int cols, bool starve, void* cuda_stream) {
     if (rows < 0 || rows >= MAX_ROWS || cols < 1 || cols > (1 << 30)) return op_fail(FD_ERR_SHAPE, "%s: rows in [0, 2^31), cols in [1, 2^30]", who);
     const bool any = rows > 0;                               // (tensors of no rows may have no memory)
     if (any && !a.x) return op_fail(FD_ERR_INVALID_ARG, "%s: x is null", who);
@@ -1059,13 +1059,21 @@ fd_status gated_norm_call(const char* who, const fd_gated_norm_args& a, int64_t 
         (a.y8 && (a.y8 == a.x || a.y8 == a.residual)))
         return op_fail(FD_ERR_SHAPE, "%s: an output shares rows with another tensor", who);
     if (rows == 0) return op_no_rows(who, a.status_out, cuda_stream);
-    return op_launched(who, launch_gated_norm(a, rows, cols, static_cast<cudaStream_t>(cuda_stream)));
+    const cudaError_t e = launch_gated_norm(a, rows, cols, starve, static_cast<cudaStream_t>(cuda_stream));
+    if (starve && e == cudaErrorNotSupported) return op_fail(FD_ERR_SHAPE, "%s: the kernel for these rows waits for nothing", who);
+    return op_launched(who, e);
 }
 }  // namespace
 
 fd_status fd_gated_norm(const fd_gated_norm_args* args, int64_t rows, int cols, void* cuda_stream) {
     if (!args) return op_fail(FD_ERR_INVALID_ARG, "fd_gated_norm: args is null");
-    return gated_norm_call("fd_gated_norm", *args, rows, cols, cuda_stream);
+    return gated_norm_call("fd_gated_norm", *args, rows, cols, false, cuda_stream);
+}
+
+fd_status fd_selftest_gated_norm_wait(const fd_gated_norm_args* args, int64_t rows, int cols, void* cuda_stream) {
+    const char* who = "fd_selftest_gated_norm_wait";
+    if (!args || !args->status_out) return op_fail(FD_ERR_INVALID_ARG, "%s: args or status_out is null", who);
+    return gated_norm_call(who, *args, rows, cols, true, cuda_stream);
 }
 
 fd_status fd_quantize_int8_rows(const void* x, int64_t x_stride, int x_dtype, int64_t rows, int cols, void* y8, int64_t y8_stride,
@@ -1080,7 +1088,7 @@ fd_status fd_quantize_int8_rows(const void* x, int64_t x_stride, int x_dtype, in
     a.y8_scale = y8_scale;
     a.y8_scale_stride = 1;
     a.rows_used = rows_used;
-    return gated_norm_call("fd_quantize_int8_rows", a, rows, cols, cuda_stream);
+    return gated_norm_call("fd_quantize_int8_rows", a, rows, cols, false, cuda_stream);
 }
 
 namespace {

@@ -274,8 +274,9 @@ cudaError_t launch_row_blocks(const fd_rmsnorm_args& a, int64_t rows, int cols, 
 // tc_gemm_blocks.cu (starve: the self-test's form, which issues no copies)
 cudaError_t launch_matmul_fp8_blocks(const fd_matmul_fp8_args& a, int m, int n, int k, bool starve, cudaStream_t st, std::string* why);
 
-// gated_norm.cu: norm, gate, residual addition, norm, modulation; 8-bit integers of rows (quantize_int8: no norm, no addition)
-cudaError_t launch_gated_norm(const fd_gated_norm_args& a, int64_t rows, int cols, cudaStream_t st);
+// gated_norm.cu: norm, gate, residual addition, norm, modulation; 8-bit integers of rows (no norm, no addition).  starve: the self-test's form,
+// which fetches no rows; cudaErrorNotSupported where no row is waited for
+cudaError_t launch_gated_norm(const fd_gated_norm_args& a, int64_t rows, int cols, bool starve, cudaStream_t st);
 
 // kv_int8.cu
 cudaError_t launch_kv_int8(const fd_kv_int8_args& a, int64_t rows, bool store, cudaStream_t st);

@@ -3,11 +3,11 @@
 
 namespace fd {
 
-cudaError_t launch_gated_norm(const fd_gated_norm_args& f, int64_t rows, int cols, cudaStream_t st) {
+cudaError_t launch_gated_norm(const fd_gated_norm_args& f, int64_t rows, int cols, bool starve, cudaStream_t st) {
     NormArgs a{f.x, f.residual, f.residual_out, f.post_weight, f.pre_weight, f.gate, f.scale, f.shift, f.y, static_cast<uint8_t*>(f.y8), f.y8_scale,
                f.row_index, f.rows_used, f.status_out, f.x_stride, f.residual_stride, f.residual_out_stride, f.gate_stride, f.scale_stride,
                f.shift_stride, f.y_stride, f.y8_stride, f.y8_scale_stride, rows, (long long)f.groups * f.rows_per_group, cols, f.rows_per_group,
-               f.post_norm, f.pre_norm, f.y8_dtype == FD_I8, f.mod_dtype == FD_BF16, f.residual_scale, f.eps};
+               f.post_norm, f.pre_norm, f.y8_dtype == FD_I8, f.mod_dtype == FD_BF16, f.residual_scale, f.eps, starve};
     if (f.status_out) {
         const cudaError_t e = cudaMemsetAsync(f.status_out, 0, sizeof(int32_t), st);
         if (e != cudaSuccess) return e;

@@ -36,6 +36,7 @@ struct NormArgs {
     int cols, rows_per_group;
     int post, pre, y8_int, mod_bf16;       // y8_int: FD_I8, else FD_E4M3
     float alpha, eps;
+    int starve;                            // self-test: no row is fetched, so that every wait for one runs out
 };
 cudaError_t launch_gated_norm_bf16(const NormArgs& a, bool residual_bf16, bool codes_only, cudaStream_t st);
 cudaError_t launch_gated_norm_f32(const NormArgs& a, bool residual_bf16, bool codes_only, cudaStream_t st);
@@ -143,6 +144,7 @@ gated_norm_kernel(NormArgs a) {
     const bool mod = NORM && (a.gate || a.scale || a.shift), mb = a.mod_bf16;
     uint8_t* s_row = s_rows + (size_t)rc * (x_bytes + t_bytes);
     auto request = [&](long long row) {                     // by one lane of the row's warps
+        if (a.starve) return;
         ptx::mbar_expect_tx(&s_full[rc], x_bytes + t_bytes);
         ptx::bulk_load(s_row, static_cast<const TX*>(a.x) + row * a.x_ld, x_bytes, &s_full[rc]);
         if (t_bytes) ptx::bulk_load(s_row + x_bytes, static_cast<const TR*>(a.residual) + row * a.res_ld, t_bytes, &s_full[rc]);
@@ -656,6 +658,7 @@ cudaError_t launch_typed(const NormArgs& a, cudaStream_t st) {
     const bool fast = a.cols % 4 == 0 && a.cols <= NORM_MAX_COLS && whole(a.x, a.x_ld, xs) && whole(a.residual, a.res_ld, rs) &&
                       ok(a.residual_out, a.res_out_ld, rs) && ok(a.post_weight, 0, xs) && ok(a.pre_weight, 0, xs) && ok(a.gate, a.gate_ld, ms) &&
                       ok(a.scale, a.scale_ld, ms) && ok(a.shift, a.shift_ld, ms) && ok(a.y, a.y_ld, xs) && ok(a.y8, a.y8_ld, 1);
+    if (!fast && a.starve) return cudaErrorNotSupported;    // (the kernels below wait for nothing)
     if (!fast) {
         const int grid = (int)min(a.rows, 148LL * 64), blocks = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
         const bool pdl = a.status == nullptr;
