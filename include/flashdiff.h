@@ -504,8 +504,9 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* args, int m, int n, int
  *   ceil(cols / 128)], the block form of fd_add_rmsnorm.  At least one of residual_out, y, y8 is given.
  *   residual_out may be residual, y may be x (same strides).  A row_index outside [0, groups * rows_per_group) is refused.
  * Sums, norms and r are fp32; r is rounded only where it is stored (the norm in front reads it unrounded).  Squares are fp32 too, with
- * the consequences that fd_add_rmsnorm has.
- * fd_quantize_int8_rows: the codes and scales (y8_scale [rows], contiguous) of a tensor as it is.
+ * the consequences that fd_add_rmsnorm has.  Rows of 8-bit outputs that a time-out left unfinished have the scale NaN.
+ * fd_quantize_int8_rows: the codes and scales (y8_scale [rows], contiguous) of a tensor as it is.  It has no status word; fd_gated_norm with
+ *   FD_NORM_NONE twice and y8 alone is the same call with one.
  */
 typedef enum { FD_NORM_NONE = 0, FD_NORM_RMS = 1, FD_NORM_LAYER = 2 } fd_norm_kind;
 typedef struct {
@@ -616,7 +617,7 @@ fd_status fd_selftest_matmul_int8_wait(const fd_matmul_int8_args* args, int m, i
 
 /*
  * The same for fd_gated_norm (and fd_quantize_int8_rows, whose kernel is that of FD_NORM_NONE twice with y8 alone): no row is fetched, status_out
- * receives FD_ERR_TIMEOUT, and the outputs stay as they were.  FD_ERR_SHAPE where the kernel for these rows waits for nothing (rows
+ * receives FD_ERR_TIMEOUT, y8_scale NaN, and the other outputs stay as they were.  FD_ERR_SHAPE where the kernel for these rows waits for nothing (rows
  * that are not whole 16-byte units, or wider than 12288 columns).
  */
 fd_status fd_selftest_gated_norm_wait(const fd_gated_norm_args* args, int64_t rows, int cols, void* cuda_stream);

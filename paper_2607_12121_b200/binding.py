@@ -802,15 +802,20 @@ def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1
 
 
 def fd_selftest_gated_norm_wait(x, status_out, stream=None, **kw) -> None:
-    """fd_gated_norm (its other arguments by name) without its rows' copies: every wait runs out, status_out receives FD_ERR_TIMEOUT and
-    the outputs stay as they were."""
+    """fd_gated_norm (its other arguments by name) without its rows' copies: every wait runs out, status_out receives FD_ERR_TIMEOUT,
+    y8_scale NaN, and the other outputs stay as they were."""
     fd_gated_norm(x, status_out=status_out, stream=stream, _call=_call_gated_norm_selftest, **kw)
 
 
-def fd_quantize_int8_rows(x, y8, y8_scale, rows_used=None, stream=None) -> None:
-    """int8 codes y8 and scales y8_scale [rows] of x [rows, cols] (float32 or bfloat16), the first rows_used rows of them if given."""
+def fd_quantize_int8_rows(x, y8, y8_scale, rows_used=None, stream=None, status_out=None) -> None:
+    """int8 codes y8 and scales y8_scale [rows] of x [rows, cols] (float32 or bfloat16), the first rows_used rows of them if given.  status_out: int32
+    device scalar that receives 0, or FD_ERR_TIMEOUT if a bounded wait of the kernel ran out; rows it left unfinished have the scale NaN."""
     if _float32 is None:
         _torch_names()
+    if status_out is not None:                          # (the same kernel)
+        _int8_rows(y8, "y8", x.shape, x.get_device())
+        fd_gated_norm(x, post_norm=None, pre_norm=None, y8=y8, y8_scale=y8_scale, rows_used=rows_used, status_out=status_out, stream=stream)
+        return
     shape, device = x.shape, x.get_device()
     x_stride = _rows(x, "x", shape, device)
     rows, cols = shape

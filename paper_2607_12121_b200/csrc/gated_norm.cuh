@@ -57,6 +57,17 @@ template <int RPC, int THREADS> __device__ __forceinline__ void row_barrier(int 
     else asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
+// The same, and whether `all` holds for every one of their threads
+template <int RPC, int THREADS> __device__ __forceinline__ bool row_barrier_all(int rc, bool all) {
+    static_assert(RPC <= 2, "barriers have fixed numbers");
+    uint32_t r;
+    if (RPC == 1 || rc == 0)
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)all), "n"(THREADS) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 2, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)all), "n"(THREADS) : "memory");
+    return r != 0;
+}
+
 // Four values of a conditioning vector of either type
 struct RawMod {
     uint4 q;                                                // bf16: the first half
@@ -158,12 +169,15 @@ gated_norm_kernel(NormArgs a) {
         request_index(row);
     }
     uint32_t it = 0;
-    bool ok = true;                                         // a thread whose wait ran out stores nothing more, but no thread leaves the loop
+    // A row one of whose threads' wait ran out is not stored, nor are those behind it; their 8-bit forms get the scale NaN, so that codes which
+    // were there before do not pass for the row's.  No thread leaves the loop.
+    bool ok = true;
+    const float lost = __uint_as_float(0x7fffffffu);
     for (; row < rows; row += step, ++it) {
-        // every warp has the row in its registers: the next one may come
+        // every warp has the row in its registers: the next one may come; from here on the row's threads agree on `ok`
         auto release = [&]() {
-            if constexpr (W > 1) row_barrier<RPC, 32 * W>(rc);
-            else __syncwarp();
+            if constexpr (W > 1) ok = row_barrier_all<RPC, 32 * W>(rc, ok);
+            else ok = __all_sync(0xffffffffu, ok);
             if (wr == 0 && lane == 0 && row + step < rows && ok) request(row + step);
         };
         const int at = index;
@@ -324,7 +338,7 @@ gated_norm_kernel(NormArgs a) {
                 m = max3_nan(max3_nan(m, p[0], p[1]), p[2], p[3]);
             }
             const I8Scale i8 = i8_scale(row_max(abs_bits(m)));
-            if (wr == 0 && lane == 0 && ok) a.y8_scale[row * a.sc_ld] = i8.scale;
+            if (wr == 0 && lane == 0) a.y8_scale[row * a.sc_ld] = ok ? i8.scale : lost;
 #pragma unroll
             for (int i = 0; i < NG; ++i)
                 if (in(i) && ok) *reinterpret_cast<uint32_t*>(y8 + i * SPAN) = i8.code4(v[i]);
@@ -341,7 +355,7 @@ gated_norm_kernel(NormArgs a) {
                 if (lane == i) mine = amax;
             }
             const float inv = E4M3_MAX / mine;
-            if (lane < NG && wr * 128 + lane * SPAN < a.cols && ok) a.y8_scale[row * a.sc_ld + wr + lane * W] = mine / E4M3_MAX;
+            if (lane < NG && wr * 128 + lane * SPAN < a.cols) a.y8_scale[row * a.sc_ld + wr + lane * W] = ok ? mine / E4M3_MAX : lost;
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
                 const float f = __shfl_sync(0xffffffffu, inv, i);
