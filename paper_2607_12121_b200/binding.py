@@ -728,7 +728,8 @@ def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1
                   y8_scale=None, status_out=None, stream=None, _call=_call_gated_norm) -> None:
     """n = post(x) * post_weight, r = residual_scale * residual + gate[g] * n (kept in residual_out), y = pre(r) * pre_weight * (1 + scale[g]) +
     shift[g], on rows [rows, cols].  Norms: "rms", "layer" or None.  gate, scale, shift [groups, cols]: one type, any row stride; the row's g is
-    (row_index or the row's own number) // rows_per_group (default: rows over groups, rounded up).  Outputs y in x's type and / or y8: int8 with
+    (row_index or the row's own number) // rows_per_group; without an index the default is rows over groups, rounded up, with one it has to be
+    given (the tokens of a group, of which the rows may be a few).  Outputs y in x's type and / or y8: int8 with
     y8_scale [rows], or E4M3 codes with y8_scale [rows, ceil(cols / 128)].  rows_used, status_out: int32 device scalars, the number of
     rows in use and what receives 0, FD_ERR_STATE (a row_index that is no row of any group) or FD_ERR_TIMEOUT (a bounded wait of the kernel ran
     out; without it an incomplete result goes unreported)."""
@@ -770,6 +771,8 @@ def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1
             psc, sc_stride = scale.data_ptr(), _rows(scale, "scale", mod_shape, device)
         if shift is not None:
             psh, sh_stride = shift.data_ptr(), _rows(shift, "shift", mod_shape, device)
+        if rows_per_group is None and row_index is not None:
+            _op_fail("row_index needs rows_per_group")
         per_group = max(1, -(-rows // groups)) if rows_per_group is None else rows_per_group
         if not 0 < per_group < 2 ** 31:
             _op_fail("rows_per_group must be positive")
