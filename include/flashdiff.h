@@ -483,8 +483,9 @@ fd_status fd_matmul_fp8_blocks(const fd_matmul_fp8_args* args, int m, int n, int
  * models, the 8-bit conventions are this library's).  They are row operators like the ones above (no context, no workspace, nothing kept
  * between calls; strides in elements; errors to fd_last_error(NULL)), and take a row count that only the device knows:
  *   rows_used   optional DEVICE int32, read in stream order: the call works on the first min(rows, max(0, *rows_used)) rows; `rows`
- *               (m of the product) is then their capacity.  Rows behind them are not read, and outputs there are left as they were.
- *               fd_regional_step leaves this number at cu_active_out + B.
+ *               (m of the product) is then their capacity.  What stands in rows behind them has no influence, and outputs there are left as they
+ *               were.  The product may fetch rows of its last tile in use (up to 255 behind the count, within the capacity) and of its first
+ *               one; the other calls do not read rows behind the count.  fd_regional_step leaves this number at cu_active_out + B.
  *   status_out  optional DEVICE int32 that receives, in stream order, 0, FD_ERR_STATE if an index was refused (its row is skipped:
  *               outputs as they were), or FD_ERR_TIMEOUT if a bounded wait of the kernel ran out (the result is then incomplete).
  *

@@ -396,7 +396,10 @@ gemm_int8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
     const int k_blocks = (g.k + GI_K - 1) / GI_K;
     const int kb0 = (int)((long long)k_blocks * rank / splits), blocks = (int)((long long)k_blocks * (rank + 1) / splits) - kb0;
 
-    const int loads = g.starve ? 0 : blocks;
+    // A tile behind the used rows fetches and multiplies nothing.  The first row tile does not wait for the count before its loads (a count of
+    // none is rare, and few rows are one tile).
+    auto idle = [&](int m_used) { return m0 > 0 && m0 >= m_used; };
+    int loads = g.starve ? 0 : blocks;
     auto load_stage = [&](int it, bool ok) { // whole warp 0
         const int s = it % GS_STAGES;
         if (elect_one() && ok) {
@@ -416,6 +419,7 @@ gemm_int8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
         }
         __syncwarp();
         pdl_wait();
+        if (m0 > 0 && idle((int)used_rows(g.m, g.rows_used))) loads = 0;
         for (int it = 0; it < min(loads, GS_STAGES); ++it) load_stage(it, true);
     } else if (warp == 1) {
         tmem_alloc(tmem_slot, GS_N);
@@ -428,7 +432,7 @@ gemm_int8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
     pdl_trigger();
     pdl_wait();
     const int m_used = (int)used_rows(g.m, g.rows_used);
-    float scale[4], bias[4];                 // of columns n0 + 4 lane ..: fetched ahead of their use
+    float scale[4] = {}, bias[4] = {};       // of columns n0 + 4 lane ..: fetched ahead of their use
 
     if (warp == 0) {
         bool ok = true;
@@ -446,7 +450,7 @@ gemm_int8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
     } else if (warp == 1) {
         constexpr uint32_t idesc = idesc_s8(GI_M, GS_N);
         bool ok = true;
-        for (int it = 0; it < blocks; ++it) {
+        for (int it = 0; it < blocks && !idle(m_used); ++it) {
             const int s = it % GS_STAGES;
             ok = ok && mbar_wait(&full[s], (it / GS_STAGES) & 1, abort_flag);
             tc_fence_after();
@@ -461,7 +465,7 @@ gemm_int8_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
             __syncwarp();
         }
         if (!ok) gb_report(g.status, FD_ERR_TIMEOUT);
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && !idle(m_used)) {
         const int quad = warp & 3, half = (warp - 4) >> 2;      // TMEM lane quadrant, 64-column half
         gi_columns(g, n0 + lane * 4, scale, bias);
         const bool ok = mbar_wait(tfull, 0, abort_flag);        // all products of this CTA: its stages have been read, too
