@@ -519,11 +519,11 @@ typedef void (*GsKernel)(const CUtensorMap, const CUtensorMap, GiArgs, int, int)
 constexpr GsKernel GS_KERNELS[4] = {gemm_int8_split_kernel<FD_F32, false>, gemm_int8_split_kernel<FD_F32, true>, gemm_int8_split_kernel<FD_BF16, false>,
                                     gemm_int8_split_kernel<FD_BF16, true>};
 
-// Per-device set-up, done once: shared-memory attributes, the number of SMs and of CTA pairs the device keeps resident.
+// Per-device set-up, done once: shared-memory attributes, the numbers of CTA pairs and clusters the device keeps resident.
 struct GiDevice {
     std::mutex set_up;                          // held while the fields below are written
     std::atomic<bool> ready{false};             // they do not change any more
-    int sms = 0, pairs = 0, clusters[8] = {};   // clusters of 1 .. 8 CTAs of the split kernel resident at once
+    int pairs = 0, clusters[8] = {};            // clusters of 1 .. 8 CTAs of the split kernel resident at once
 };
 constexpr int GI_MAX_DEVICES = 64;
 GiDevice g_devices[GI_MAX_DEVICES];
@@ -548,7 +548,6 @@ cudaError_t gi_set_up(GiDevice& d, int dev) {
         e = cudaOccupancyMaxActiveClusters(&d.clusters[i], GS_KERNELS[0], &lc);
         if (e != cudaSuccess) return e;
     }
-    d.sms = n;
     return cudaSuccess;
 }
 
