@@ -570,8 +570,8 @@ fd_status fd_matmul_int8(const fd_matmul_int8_args* args, int m, int n, int k, v
  * (a slice of a fused projection's output); rows_by_slot = 1: at its slot's g * rows_group_stride + t * rows_token_stride (the step's
  * kv_cache itself); head h at h * rows_head_stride from there, channels contiguous.
  *   index [rows] int32 or NULL (rows is then at most the number of slots).  A row whose index is no slot is refused; fd_kv_store_int8 also refuses
- *   one whose index is not above the index before it and above every slot that the list names before it, in refused rows too: no slot is
- *   written twice.  A strictly ascending list, as the step leaves it, keeps every row.
+ *   one whose index is not above the index before it.  Where rows that are not refused name one slot all the same (a list that starts anew: 5, 3,
+ *   5), it holds the last one's values.
  *   sets: one or two (keys and values; HOST array inside the struct) with the same shape;  head_dim 1 .. 256
  * Slots and rows that are written must not overlap one another: FD_ERR_SHAPE unless every stride, from the smallest up, spans what is inside.
  */

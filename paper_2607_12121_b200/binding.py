@@ -916,8 +916,8 @@ def _kv(call, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stre
 def fd_kv_store_int8(k, k8, k_scale, v=None, v8=None, v_scale=None, index=None, rows_used=None, status_out=None, stream=None) -> None:
     """Quantises keys (and values) into a cache k8 [groups, tokens, heads, head_dim] int8 with k_scale [groups, tokens, heads] float32.  k: rows
     [rows, heads, head_dim], row i for slot index[i] (slot i without an index), or [groups, tokens, heads, head_dim], of which the index's slots
-    are taken.  index: strictly ascending int32, group * tokens + token; a row whose index is no slot, or not above the index before it and
-    above every slot named before it, is refused.  rows_used, status_out: int32 device scalars, the number of rows in use and what receives
+    are taken.  index: ascending int32, group * tokens + token; a row whose index is no slot, or not above the index before it, is refused, and a
+    slot that several others name holds the last one's values.  rows_used, status_out: int32 device scalars, the number of rows in use and what receives
     0 or FD_ERR_STATE (a refused index)."""
     _kv(_call_kv_store, k, k8, k_scale, v, v8, v_scale, index, rows_used, status_out, stream)
 

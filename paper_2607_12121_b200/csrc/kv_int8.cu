@@ -1,7 +1,7 @@
 // Keys and values in 8-bit integers with a scale for every token and head: rows of the storage type into slots of a cache, and back.
-// Bound by memory: 3 bytes a bf16 value either way, and 4 bytes a head for its scale; a store with a list also by the look at the list that precedes
-// it.  Measured: 16380 tokens x 2 x 12 heads of 128 stored in 26.8 us (5.7 TB/s; without the look 24.4), 32760 loaded in 47.0 (6.5 TB/s); 5216 x 2 x 24
-// heads of 64 stored in 10.2; 997 x 2 x 16 heads of 72 in 3.9.
+// Bound by memory: 3 bytes a bf16 value either way, and 4 bytes a head for its scale; a store with a list has a second, small launch behind it.
+// Measured: 16380 tokens x 2 x 12 heads of 128 stored in 26.4 us (5.8 TB/s), of which 2.0 are the second launch, 32760 loaded in 47.0 (6.5 TB/s); 5216 x
+// 2 x 24 heads of 64 stored in 11.0 (1.6); 997 x 2 x 16 heads of 72 in 4.2 (0.7).
 #include "common.cuh"
 #include "ptx.cuh"
 #include "row_vec.cuh"
@@ -31,60 +31,12 @@ struct KvArgs {
     Divisor by_heads, by_tokens;
 };
 
-// The slot that row i names, or -1.
-__device__ __forceinline__ int named_slot(const KvArgs& a, uint32_t i) {
-    if (!a.index) return (int)i;
-    const int s = a.index[i];
-    return s >= 0 && s < (int)a.slots ? s : -1;
-}
-
-// A store's list.  A slot that the list names twice would be written by two CTAs at once, so a row counts only if its index is a slot above the
-// index before it and above every slot named before it.  A CTA looks once at the whole list; where it ascends, as the step's lists do,
-// every row counts, else the rows of each turn are looked at.  Nothing may be written before that, which costs 2.4 us at 16380 rows (26.8 against
-// 24.4) and 0.4 at 997.  Dropped: a look in runs of consecutive rows (the same, and 3.5 at a handful), turn by turn at blocks of the list (29.1), by the
-// CTAs of a cluster together (36), one CTA an SM (27.3), the first rows fetched meanwhile (27.5).
-constexpr int KV_THREADS = 256, KV_WARPS = KV_THREADS / 32;
-
-// Whether index[0 .. rows) are slots in ascending order; the whole CTA.
-__device__ __forceinline__ bool list_ascends(const KvArgs& a, uint32_t rows) {
-    const int32_t* p = a.index;
-    const int slots = (int)a.slots;
-    const uint32_t head = min(rows, (uint32_t)(-(reinterpret_cast<uintptr_t>(p) >> 2) & 3)), quads = (rows - head) / 4, tail = head + 4 * quads;
-    auto above = [&](uint32_t i) { return p[i] > (i > 0 ? p[i - 1] : -1) && p[i] < slots; };
-    bool up = true;
-#pragma unroll 4
-    for (uint32_t j0 = 0; j0 < quads; j0 += KV_THREADS) {
-        const uint32_t j = j0 + threadIdx.x;
-        const bool in = j < quads;
-        const int4 v = in ? reinterpret_cast<const int4*>(p + head)[j] : make_int4(0, 0, 0, 0);
-        int before = __shfl_up_sync(0xffffffffu, v.w, 1);
-        if ((threadIdx.x & 31) == 0) before = in && head + j > 0 ? p[head + 4 * j - 1] : -1;
-        up = up && (!in || (before < v.x && v.x < v.y && v.y < v.z && v.z < v.w && v.w < slots));
-    }
-    if (threadIdx.x < head) up = up && above(threadIdx.x);
-    if (threadIdx.x < rows - tail) up = up && above(tail + threadIdx.x);
-    return __syncthreads_and(up);
-}
-
-// For a list that does not ascend: the largest slot that rows 0 .. to - 1 name, `top` being that of rows 0 .. from - 1; the whole CTA.
-__device__ __noinline__ int list_top(const KvArgs& a, uint32_t from, uint32_t to, int top) {
-    __shared__ int s_top[KV_WARPS];
-    for (uint32_t i = from + threadIdx.x; i < to; i += KV_THREADS) top = max(top, named_slot(a, i));
-    top = __reduce_max_sync(0xffffffffu, top);
-    __syncthreads();                                        // (the turn before has read its result)
-    if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
-    __syncthreads();
-    for (int i = 0; i < KV_WARPS; ++i) top = max(top, s_top[i]);
-    return top;
-}
-
-// Whether row i counts, `top` being the largest slot that rows 0 .. from - 1 name (from <= i).
-__device__ __noinline__ bool row_counts(const KvArgs& a, uint32_t i, uint32_t from, int top) {
-    const int s = named_slot(a, i);
-    if (s <= top || (i > 0 && a.index[i - 1] >= s)) return false;
-    for (uint32_t j = from; j < i; ++j)
-        if (named_slot(a, j) >= s) return false;
-    return true;
+// The slot of row i, or -1 where its index is refused.
+__device__ __forceinline__ long long kv_slot(const KvArgs& a, long long i, bool ascending) {
+    if (!a.index) return i;
+    const long long s = a.index[i];
+    if (s < 0 || s >= a.slots || (ascending && i > 0 && a.index[i - 1] >= s)) return -1;
+    return s;
 }
 
 // A set whose rows are whole 16-byte units and whose codes are whole 8-byte units apart: strides in those units, in 32 bits
@@ -104,29 +56,21 @@ __device__ __forceinline__ uint64_t offset3(uint32_t a, uint32_t sa, uint32_t b,
 
 // Head dims of whole units: LANES lanes hold one head, NU units of 8 channels each; keys and values of a head are in flight together.  Four
 // lanes, so that the index arithmetic and the quotients of a head serve many values: with eight, stores of 16380 x 2 x 12 heads of 128 took
-// 26.7 us against 23.7, of 5216 x 2 x 24 heads of 64 13.9 against 10.3 (all without a look at the list).
-constexpr int LANES = 4, KV_TURN = KV_THREADS / LANES;       // (heads that a CTA takes at a time)
+// 26.7 us against 23.7, of 5216 x 2 x 24 heads of 64 13.9 against 10.3 (the first launch alone).
+constexpr int LANES = 4;
 template <typename T, bool STORE, int NU>
-__global__ void __launch_bounds__(KV_THREADS) kv_kernel(const __grid_constant__ KvFastArgs f, int n_sets) {
+__global__ void __launch_bounds__(256) kv_kernel(const __grid_constant__ KvFastArgs f, int n_sets) {
     const KvArgs& a = f.a;
     const int l = threadIdx.x % LANES, units = a.dh / 8, first_lane = (threadIdx.x & 31) / LANES * LANES;
     const unsigned group_mask = ((1u << LANES) - 1) << first_lane;
     constexpr int UNIT = 8 * sizeof(T);                     // bytes of 8 channels
     ptx::pdl_wait();
-    const uint32_t rows = (uint32_t)used_rows(a.rows, a.rows_used), items = rows * a.heads;       // (below 2^31: the launcher has checked)
-    const bool every = !STORE || !a.index || list_ascends(a, rows);                              // every row counts
-    uint32_t seen = 0;                                      // else: `top` is the largest slot that the rows before this one name
-    int top = -1;
-    for (uint32_t w0 = blockIdx.x * KV_TURN; w0 < items; w0 += gridDim.x * KV_TURN) {
-        if (STORE && !every) {
-            const uint32_t i0 = a.by_heads.of(w0);
-            top = list_top(a, seen, i0, top);
-            seen = i0;
-        }
-        const uint32_t w = w0 + threadIdx.x / LANES;
-        if (w >= items) continue;
+    if (STORE && a.index) ptx::pdl_trigger();               // (see kv_settle_kernel)
+    const uint32_t items = (uint32_t)(used_rows(a.rows, a.rows_used) * a.heads);       // (below 2^31: the launcher has checked)
+    constexpr int HPC = 256 / LANES;                        // heads of a CTA
+    for (uint32_t w = blockIdx.x * HPC + threadIdx.x / LANES; w < items; w += gridDim.x * HPC) {
         const uint32_t i = a.by_heads.of(w), h = w - i * a.heads;
-        const int slot = !STORE || every || row_counts(a, i, seen, top) ? named_slot(a, i) : -1;
+        const long long slot = kv_slot(a, i, STORE);
         if (slot < 0) {
             if (l == 0 && h == 0) report_status(a.status, FD_ERR_STATE);
             continue;
@@ -207,65 +151,134 @@ __global__ void __launch_bounds__(KV_THREADS) kv_kernel(const __grid_constant__ 
     ptx::pdl_trigger();
 }
 
+// Where a head lies that belongs to row i and to a slot
+template <typename T> struct KvHead {
+    T* row;
+    int8_t* codes;
+    float* scale;
+    __device__ __forceinline__ KvHead(const KvArgs& a, const fd_kv_int8_set& s, long long i, long long slot, int h) {
+        const long long g = slot / a.tokens, t = slot % a.tokens;
+        row = static_cast<T*>(s.rows) + (a.by_slot ? g * s.rows_group_stride + t * s.rows_token_stride : i * s.rows_token_stride) + h * s.rows_head_stride;
+        codes = static_cast<int8_t*>(s.codes) + g * s.codes_group_stride + t * s.codes_token_stride + h * s.codes_head_stride;
+        scale = s.scale + g * s.scale_group_stride + t * s.scale_token_stride + h * s.scale_head_stride;
+    }
+};
+
+// One head stored by a warp, any head dim, stride and alignment
+template <typename T>
+__device__ __forceinline__ void kv_store_head(const KvArgs& a, const fd_kv_int8_set& s, long long i, long long slot, int h) {
+    const int lane = threadIdx.x & 31;
+    const KvHead<T> p(a, s, i, slot, h);
+    float v[8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        v[k] = k * 32 + lane < a.dh ? to_f<T>(p.row[k * 32 + lane]) : 0.f;
+        m = max(m, abs_bits(v[k]));
+    }
+    const I8Scale i8 = i8_scale(__reduce_max_sync(0xffffffffu, m));
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k * 32 + lane < a.dh) p.codes[k * 32 + lane] = (int8_t)i8.code(v[k]);
+    if (lane == 0) *p.scale = i8.scale;
+}
+
 // Any head dim, stride and alignment: a warp a head, four channels a lane and turn.
 template <typename T, bool STORE>
-__global__ void __launch_bounds__(KV_THREADS) kv_any_kernel(const __grid_constant__ KvArgs a) {
+__global__ void __launch_bounds__(256) kv_any_kernel(KvArgs a) {
     const int lane = threadIdx.x & 31;
     ptx::pdl_wait();
-    const uint32_t rows = (uint32_t)used_rows(a.rows, a.rows_used);
-    const long long items = (long long)rows * a.heads;
+    if (STORE && a.index) ptx::pdl_trigger();               // (see kv_settle_kernel)
+    const long long rows = used_rows(a.rows, a.rows_used), items = rows * a.heads;
     const fd_kv_int8_set& s = a.sets[blockIdx.y];
-    const bool every = !STORE || !a.index || list_ascends(a, rows);
-    uint32_t seen = 0;                                      // else: `top` is the largest slot that the rows before this one name
-    int top = -1;
-    for (long long w0 = (long long)blockIdx.x * KV_WARPS; w0 < items; w0 += (long long)gridDim.x * KV_WARPS) {
-        if (STORE && !every) {
-            const uint32_t i0 = (uint32_t)(w0 / a.heads);
-            top = list_top(a, seen, i0, top);
-            seen = i0;
-        }
-        const long long w = w0 + (threadIdx.x >> 5);
-        if (w >= items) continue;
-        const uint32_t i = (uint32_t)(w / a.heads);
+    for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < items; w += gridDim.x * 8LL) {
+        const long long i = w / a.heads;
         const int h = (int)(w % a.heads);
-        const long long slot = !STORE || every || row_counts(a, i, seen, top) ? named_slot(a, i) : -1;
+        const long long slot = kv_slot(a, i, STORE);
         if (slot < 0) {
             if (lane == 0) report_status(a.status, FD_ERR_STATE);
             continue;
         }
-        const long long g = slot / a.tokens, t = slot % a.tokens;
-        T* row = static_cast<T*>(s.rows) + (a.by_slot ? g * s.rows_group_stride + t * s.rows_token_stride : i * s.rows_token_stride) + h * s.rows_head_stride;
-        int8_t* codes = static_cast<int8_t*>(s.codes) + g * s.codes_group_stride + t * s.codes_token_stride + h * s.codes_head_stride;
-        float* scale = s.scale + g * s.scale_group_stride + t * s.scale_token_stride + h * s.scale_head_stride;
         if constexpr (STORE) {
-            float v[8];
-            uint32_t m = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[k] = k * 32 + lane < a.dh ? to_f<T>(row[k * 32 + lane]) : 0.f;
-                m = max(m, abs_bits(v[k]));
-            }
-            const I8Scale i8 = i8_scale(__reduce_max_sync(0xffffffffu, m));
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k * 32 + lane < a.dh) codes[k * 32 + lane] = (int8_t)i8.code(v[k]);
-            if (lane == 0) *scale = i8.scale;
+            kv_store_head<T>(a, s, i, slot, h);
         } else {
-            const float f = *scale;
-            for (int c = lane; c < a.dh; c += 32) row[c] = from_f<T>((float)codes[c] * f);
+            const KvHead<T> p(a, s, i, slot, h);
+            const float f = *p.scale;
+            for (int c = lane; c < a.dh; c += 32) p.row[c] = from_f<T>((float)p.codes[c] * f);
         }
     }
     ptx::pdl_trigger();
 }
 
+// Behind a store with a list.  A list that does not ascend may name a slot twice (5, 3, 5: only the 3 is refused), and then two CTAs have written
+// it at once.  Here every slot belongs to one CTA, and every element of it to one thread, which writes the rows that name it in the list's
+// order: the last one's values stay.  A list that ascends names no slot twice, and nothing is done.
+// A launch of its own: a look at the list by every CTA ahead of its writes leaves memory idle meanwhile, and wants CTAs that stay.  16380 x 2 x 12
+// heads of 128 stored and 32760 loaded 75.6 us (79.9 with a look ahead, 73.3 with neither); 997 x 2 x 16 heads of 72 stored 4.2 (4.0, 3.5), 150000 x 2 x
+// 12 heads of 128 239 (290, 226).
+constexpr int SETTLE_CTAS = 32, SETTLE_THREADS = 512;
+
+// Whether index[0 .. rows) ascends strictly; the whole CTA.
+__device__ __forceinline__ bool list_ascends(const int32_t* p, uint32_t rows) {
+    const uint32_t head = min(rows, (uint32_t)(-(reinterpret_cast<uintptr_t>(p) >> 2) & 3)), quads = (rows - head) / 4, tail = head + 4 * quads;
+    auto above = [&](uint32_t i) { return i == 0 || __ldcg(p + i) > __ldcg(p + i - 1); };
+    bool up = true;
+#pragma unroll 8
+    for (uint32_t j0 = 0; j0 < quads; j0 += SETTLE_THREADS) {
+        const uint32_t j = j0 + threadIdx.x;
+        const bool in = j < quads;
+        const int4 v = in ? __ldcg(reinterpret_cast<const int4*>(p + head) + j) : make_int4(0, 1, 2, 3);
+        int before = __shfl_up_sync(0xffffffffu, v.w, 1);
+        const bool edge = (threadIdx.x & 31) == 0, first = edge && head + j == 0;
+        if (edge && in && !first) before = __ldcg(p + head + 4 * j - 1);
+        up = up && v.x < v.y && v.y < v.z && v.z < v.w && (!in || first || before < v.x);
+    }
+    if (threadIdx.x < head) up = up && above(threadIdx.x);
+    if (threadIdx.x < rows - tail) up = up && above(tail + threadIdx.x);
+    return __syncthreads_and(up);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(SETTLE_THREADS) kv_settle_kernel(const __grid_constant__ KvArgs a, int n_sets) {
+    constexpr int WARPS = SETTLE_THREADS / 32;
+    __shared__ uint32_t s_rows[SETTLE_THREADS], s_named[WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // The list and its length were there before the store began (its CTAs let this launch begin when they have waited for what is before them), so
+    // they are looked at, past the first-level cache, while the store ends.
+    const uint32_t rows = a.rows_used ? (uint32_t)min(a.rows, (long long)max(0, __ldcg(a.rows_used))) : (uint32_t)a.rows;
+    const bool up = list_ascends(a.index, rows);
+    ptx::pdl_wait();
+    ptx::pdl_trigger();
+    if (up) return;
+    for (uint32_t i0 = 0; i0 < rows; i0 += SETTLE_THREADS) {
+        // this CTA's rows among the next ones, in order
+        const uint32_t i = i0 + threadIdx.x;
+        const long long slot = i < rows ? kv_slot(a, i, true) : -1;
+        const bool mine = slot >= 0 && (uint32_t)slot % SETTLE_CTAS == blockIdx.x;
+        const uint32_t named = __ballot_sync(0xffffffffu, mine);
+        if (lane == 0) s_named[warp] = __popc(named);
+        __syncthreads();
+        uint32_t at = __popc(named & ((1u << lane) - 1)), count = 0;
+        for (int w = 0; w < WARPS; ++w) {
+            if (w < warp) at += s_named[w];
+            count += s_named[w];
+        }
+        if (mine) s_rows[at] = i;
+        __syncthreads();
+        // (head w of a slot is always the same warp's)
+        for (uint32_t r = 0; r < count; ++r)
+            for (int w = warp; w < n_sets * a.heads; w += WARPS) {
+                const int set = w >= a.heads;
+                kv_store_head<T>(a, a.sets[set], s_rows[r], a.index[s_rows[r]], w - set * a.heads);
+            }
+        __syncthreads();                                    // (the rows have been read)
+    }
+}
+
 template <typename T, bool STORE, int NU>
 cudaError_t launch_units(const KvFastArgs& f, int n_sets, cudaStream_t st) {
-    const long long turns = (f.a.rows * f.a.heads + KV_TURN - 1) / KV_TURN;
-    // Without a list a CTA a turn.  With one, at which every CTA looks, as many CTAs as an SM holds: what its registers leave, by the 16-byte
-    // units of a set that a lane holds.
-    constexpr int HELD = NU * (int)sizeof(T) / 2, RESIDENT = HELD <= 1 ? 6 : HELD == 2 ? 5 : HELD <= 4 ? 4 : HELD <= 6 ? 3 : HELD <= 8 ? 2 : 1;
-    const long long most = STORE && f.a.index ? 148LL * RESIDENT : 1LL << 20;
-    return ptx::launch_kernel(kv_kernel<T, STORE, NU>, (int)min(turns, most), KV_THREADS, 0, st, f.a.status == nullptr, f, n_sets);
+    const long long ctas = (f.a.rows * f.a.heads + 256 / LANES - 1) / (256 / LANES);
+    return ptx::launch_kernel(kv_kernel<T, STORE, NU>, (int)min(ctas, 1LL << 20), 256, 0, st, f.a.status == nullptr, f, n_sets);
 }
 
 template <typename T, bool STORE>
@@ -285,8 +298,8 @@ cudaError_t launch_typed(const KvArgs& a, int n_sets, cudaStream_t st) {
         fast = fast && (reinterpret_cast<uintptr_t>(k.rows) & 15) == 0 && (reinterpret_cast<uintptr_t>(k.codes) & 7) == 0;
     }
     if (!fast) {
-        const dim3 grid((unsigned)min((a.rows * a.heads + KV_WARPS - 1) / KV_WARPS, 148LL * (STORE && a.index ? 8 / n_sets : 16)), n_sets);
-        return ptx::launch_kernel(kv_any_kernel<T, STORE>, grid, KV_THREADS, 0, st, a.status == nullptr, a);
+        const dim3 grid((unsigned)min((a.rows * a.heads + 7) / 8, 148LL * 16), n_sets);
+        return ptx::launch_kernel(kv_any_kernel<T, STORE>, grid, 256, 0, st, a.status == nullptr, a);
     }
     if (a.dh <= 32) return launch_units<T, STORE, 1>(f, n_sets, st);
     if (a.dh <= 64) return launch_units<T, STORE, 2>(f, n_sets, st);
@@ -306,8 +319,11 @@ cudaError_t launch_kv_int8(const fd_kv_int8_args& f, int64_t rows, bool store, c
         if (e != cudaSuccess) return e;
     }
     using bf = __nv_bfloat16;
-    if (f.dtype == FD_BF16) return store ? launch_typed<bf, true>(a, f.n_sets, st) : launch_typed<bf, false>(a, f.n_sets, st);
-    return store ? launch_typed<float, true>(a, f.n_sets, st) : launch_typed<float, false>(a, f.n_sets, st);
+    const bool wide = f.dtype == FD_F32;
+    if (!store) return wide ? launch_typed<float, false>(a, f.n_sets, st) : launch_typed<bf, false>(a, f.n_sets, st);
+    const cudaError_t e = wide ? launch_typed<float, true>(a, f.n_sets, st) : launch_typed<bf, true>(a, f.n_sets, st);
+    if (e != cudaSuccess || !f.index || rows == 1) return e;
+    return ptx::launch_kernel(wide ? kv_settle_kernel<float> : kv_settle_kernel<bf>, SETTLE_CTAS, SETTLE_THREADS, 0, st, true, a, f.n_sets);
 }
 
 }  // namespace fd

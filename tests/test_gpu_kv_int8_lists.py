@@ -1,5 +1,5 @@
-"""GPU: lists of a store that are not strictly ascending.  No slot is written by two rows, whatever the list: a row counts only if its index is a
-slot above the index before it and above every slot named before it, in rows that do not count too."""
+"""GPU: lists of a store that are not strictly ascending.  A row counts if its index is a slot above the index before it; a slot that several such
+rows name holds the last one's codes and scales, all of them."""
 import pytest
 import torch
 
@@ -9,18 +9,11 @@ import paper_2607_12121_b200 as fd
 pytestmark = pytest.mark.gpu
 
 
-def _kept(index, slots):
-    """The rows that the rule keeps; no slot comes twice, and a list that ascends keeps them all."""
-    top, kept = -1, []
-    for i, s in enumerate(index):
-        if 0 <= s < slots:
-            if s > top and not (i > 0 and index[i - 1] >= s):
-                kept.append(i)
-            top = max(top, s)
-    named = [index[i] for i in kept]
-    assert len(set(named)) == len(named)
-    assert len(kept) == len(index) or not (sorted(set(index)) == list(index) and 0 <= index[0] and index[-1] < slots)
-    return kept
+def _last(index, slots):
+    """How many rows count, and the slots that they name with the last row that does, in the order of the slots."""
+    count = [i for i, s in enumerate(index) if 0 <= s < slots and not (i > 0 and index[i - 1] >= s)]
+    last = {index[i]: i for i in count}
+    return len(count), sorted(last), [last[s] for s in sorted(last)]
 
 
 def _run(index, slots, heads, dh, source="rows", used=None, sets=2, dt=torch.bfloat16, replay=False):
@@ -46,15 +39,15 @@ def _run(index, slots, heads, dh, source="rows", used=None, sets=2, dt=torch.bfl
         graph.replay()
     else:
         store(status_out=status)
-    kept = _kept(index[:count], slots)
-    assert int(status) == (0 if len(kept) == count else fd.FD_ERR_STATE)
-    at = idx[torch.tensor(kept, dtype=torch.long, device="cuda")].long()
+    counted, named, last = _last(index[:count], slots)
+    assert int(status) == (0 if counted == count else fd.FD_ERR_STATE)
+    at = torch.tensor(named, dtype=torch.long, device="cuda")
     rest = torch.ones(slots, dtype=torch.bool, device="cuda")
     rest[at] = False
     for half in range(2):
         c, s = codes[half, 0], scale[half, 0]
-        if half < sets and kept:
-            ref.check_codes(c[at], s[at], rows[half][kept if source == "rows" else at].double())
+        if half < sets and named:
+            ref.check_codes(c[at], s[at], rows[half][last if source == "rows" else at].double())
         untouched = rest if half < sets else torch.ones_like(rest)
         assert bool((c[untouched] == 55).all()) and bool((s[untouched] == 9.0).all())
     before = codes.clone(), scale.clone()                       # the same again, without the word: the same slots get the same
@@ -94,13 +87,15 @@ def _long(n, slots, kind):
         up[n - n // 3:] = -1
     elif kind == "halves swapped":
         up = torch.cat([up[n // 2:], up[: n // 2]])
+    elif kind == "thrice":                                      # the same slots three times over
+        up = torch.cat([up[: n // 3]] * 3 + [up[n // 3: n // 3 + n - n // 3 * 3]])
     return up.tolist()
 
 
-@pytest.mark.parametrize("kind", ["ascending", "two numberings", "random", "one returns", "repeats", "a hole", "swaps", "first is last", "holes", "halves swapped"])
+@pytest.mark.parametrize("kind", ["ascending", "two numberings", "random", "one returns", "repeats", "a hole", "swaps", "first is last", "holes", "halves swapped", "thrice"])
 @pytest.mark.parametrize("n,slots,heads,dh", [(4099, 6000, 12, 128), (3001, 3300, 1, 64), (20011, 40000, 2, 40), (2500, 5000, 65, 16), (3001, 4000, 3, 50), (700, 900, 24, 96)])
 def test_long_lists(n, slots, heads, dh, kind):
-    """Lists over many CTAs, heads that leave a row to two of them among them."""
+    """Lists over many CTAs, with slots that come back near and far."""
     _run(_long(n, slots, kind), slots, heads, dh)
 
 
@@ -119,8 +114,7 @@ def test_lists_that_begin_anywhere(offset):
     k = torch.randn(2003, 2, 64, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
     k8, ks = torch.full((1, 2500, 2, 64), 55, dtype=torch.int8, device="cuda"), torch.full((1, 2500, 2), 9.0, device="cuda")
     fd.fd_kv_store_int8(k, k8, ks, index=whole[offset:])
-    index = whole[offset:].tolist()
-    kept = _kept(index, 2500)
-    assert len(kept) == 2002                                    # (all but the row whose slot returns)
-    at = torch.tensor([index[i] for i in kept], device="cuda")
-    ref.check_codes(k8[0, at], ks[0, at], k[kept].double())
+    counted, named, last = _last(whole[offset:].tolist(), 2500)
+    assert counted == 2002 and len(named) == 2002               # (all but the row that names the first slot again)
+    at = torch.tensor(named, device="cuda")
+    ref.check_codes(k8[0, at], ks[0, at], k[last].double())
