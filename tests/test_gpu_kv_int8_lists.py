@@ -118,3 +118,49 @@ def test_lists_that_begin_anywhere(offset):
     assert counted == 2002 and len(named) == 2002               # (all but the row that names the first slot again)
     at = torch.tensor(named, device="cuda")
     ref.check_codes(k8[0, at], ks[0, at], k[last].double())
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_lists_written_just_before(captured):
+    """Lists and their lengths that change from call to call in the same memory without a wait between, ascending and not; other calls of the library
+    stand before and behind."""
+    n, slots, heads, dh, steps = 3000, 4000, 6, 64, 24
+    g = torch.Generator(device="cuda").manual_seed(3)
+    kinds = ["ascending", "two numberings", "thrice", "ascending", "repeats", "one returns"]
+    lists = [torch.tensor(_long(n, slots, kinds[i % len(kinds)]), dtype=torch.int32, device="cuda") for i in range(steps)]
+    lengths = [torch.tensor([n - 100 * i], dtype=torch.int32, device="cuda") for i in range(steps)]
+    xs = [torch.randn(n, 2 * heads * dh, generator=g, device="cuda").bfloat16() for _ in range(3)]
+    x, y8, y_s = torch.empty_like(xs[0]), torch.empty(n, 2 * heads * dh, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+    index, used = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    codes = torch.empty(2, 1, slots, heads, dh, dtype=torch.int8, device="cuda")
+    scale, back = torch.empty(2, 1, slots, heads, device="cuda"), torch.empty(2, 1, slots, heads, dh, device="cuda")
+    k, v = (x[:, i * heads * dh: (i + 1) * heads * dh].unflatten(1, (heads, dh)) for i in (0, 1))
+
+    def work():
+        fd.fd_quantize_int8_rows(x, y8, y_s, rows_used=used)
+        fd.fd_kv_store_int8(k, codes[0], scale[0], v, codes[1], scale[1], index=index, rows_used=used)
+        fd.fd_kv_load_int8(codes[0], scale[0], back[0], codes[1], scale[1], back[1])
+
+    graph = None
+    if captured:
+        x.copy_(xs[0]), index.copy_(lists[0]), used.copy_(lengths[0]), codes.fill_(55), scale.fill_(9.0)
+        work()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            work()
+    kept = []
+    for i in range(steps):
+        x.copy_(xs[i % 3]), codes.fill_(55), scale.fill_(9.0), index.copy_(lists[i]), used.copy_(lengths[i])
+        graph.replay() if captured else work()
+        kept.append((codes.clone(), scale.clone(), back.clone()))
+    for i, (codes_, scale_, back_) in enumerate(kept):
+        counted, named, last = _last(lists[i].tolist()[: n - 100 * i], slots)
+        at, rest = torch.tensor(named, device="cuda"), torch.ones(slots, dtype=torch.bool, device="cuda")
+        rest[at] = False
+        rows = xs[i % 3].unflatten(1, (2, heads, dh))
+        for half in range(2):
+            ref.check_codes(codes_[half, 0, at], scale_[half, 0, at], rows[last, half].double())
+            assert bool((codes_[half, 0, rest] == 55).all()) and bool((scale_[half, 0, rest] == 9.0).all())
+        value = codes_.double() * scale_.double()[..., None]
+        ref.near(back_, value, ref.U32 * value.abs())
