@@ -727,7 +727,7 @@ def fd_gated_norm(x, residual=None, residual_out=None, residual_scale: float = 1
                   pre_weight=None, scale=None, shift=None, eps: float = 1e-6, rows_per_group=None, row_index=None, rows_used=None, y=None, y8=None,
                   y8_scale=None, status_out=None, stream=None, _call=_call_gated_norm) -> None:
     """n = post(x) * post_weight, r = residual_scale * residual + gate[g] * n (kept in residual_out), y = pre(r) * pre_weight * (1 + scale[g]) +
-    shift[g], on rows [rows, cols].  Norms: "rms", "layer" or None.  gate, scale, shift [groups, cols]: one type, any row stride; the row's g is
+    shift[g], on rows [rows, cols].  Norms: "rms", "layer" or None.  gate, scale, shift [groups, cols]: one type, row strides of at least cols; the row's g is
     (row_index or the row's own number) // rows_per_group; without an index the default is rows over groups, rounded up, with one it has to be
     given (the tokens of a group, of which the rows may be a few).  Outputs y in x's type and / or y8: int8 with
     y8_scale [rows], or E4M3 codes with y8_scale [rows, ceil(cols / 128)].  rows_used, status_out: int32 device scalars, the number of

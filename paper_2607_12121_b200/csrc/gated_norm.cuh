@@ -2,8 +2,8 @@
 // the rows:  n = post(x) * post_weight,  r = residual_scale * residual + gate[g] * n,  y = pre(r) * pre_weight * (1 + scale[g]) + shift[g],
 // y in the storage type and / or as 8-bit integers with a scale per row or E4M3 codes with a scale per 128 columns.
 // Every element of x and the residual is read once, r and y are written once; sums, norms and r are fp32, rounded where they are stored.
-// Measured: 16380 x 1536, bf16 + fp32 residual, RMS on both sides (302 MB) 51.3 us, 5.9 TB/s; 5216 x 1536, layer norm with scale and shift to E4M3
-// (88 MB) 19.9; 3997 x 1152, all bf16, to 8-bit integers 12.0; 8500 x 1536 quantised alone (39 MB) 8.3; one token 3.1.
+// Measured: 16380 x 1536, bf16 + fp32 residual, RMS on both sides (302 MB) 51.7 us, 5.8 TB/s; 5216 x 1536, layer norm with scale and shift to E4M3
+// (88 MB) 20.4; 3997 x 1152, all bf16, to 8-bit integers 12.0; 8500 x 1536 quantised alone (39 MB) 8.5; one token 3.3.
 #pragma once
 #include <atomic>
 #include <type_traits>
@@ -98,7 +98,8 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 // residual in shared memory, filled by bulk copies while the row before it, by then in registers, is finished.  The weights and conditioning
 // vectors are fetched ahead of the sums that stand before their use, out of the first-level cache: rows pass it by.
 //
-// What bounds it, beyond memory, is the way of one row: two to four sums over its warps, one after another.  16380 x 1536 took 62 us with rows one
+// What bounds it, beyond memory, is the way of one row, two to four sums over its warps one after another, and how many rows the registers let
+// an SM hold at once: of 1152 columns, all bf16, twelve (164 registers, 72 of them for vectors fetched ahead), of 1536 eight.  16380 x 1536 took 62 us with rows one
 // ahead in registers, 53.4 with a second row in shared memory, 55.5 with two rows at a time per slot, 57 with the weights and vectors as
 // factors in registers (fewer warps fit), 58 with these in shared memory and one CTA an SM.
 template <typename TX, typename TR, int W, int NG, bool NORM>

@@ -7,8 +7,8 @@
 // the other; the last, partly filled round's tiles are cut along the columns so that every pair has a piece.  For few tiles, 128 x 128
 // tiles with K shared out to a cluster.  No load is multicast.
 //
-// Measured: 16380 x 8960 x 1536 with GELU 163 us (2760 TOP/s, tensor cores 83 % busy), 16380 x 4608 x 1536 79.5, 5216 x 4608 x 1536 29.5, 8192 x 8192 x
-// 8192 362 (3030 TOP/s); 1001 x 1152 x 4608 11.4, eight rows x 9216 x 1536 5.8.  What bounds it, in clocks of one pair: a tile of K = 1536 takes 6950,
+// Measured: 16380 x 8960 x 1536 with GELU 165 us (2730 TOP/s, tensor cores 83 % busy), 16380 x 4608 x 1536 79.5, 5216 x 4608 x 1536 29.9, 8192 x 8192 x
+// 8192 362 (3030 TOP/s); 1001 x 1152 x 4608 11.7 (8.0 with 8 rows in use), eight rows x 9216 x 1536 6.0.  What bounds it, in clocks of one pair: a tile of K = 1536 takes 6950,
 // its products alone 6144; the difference is the epilogue of the tile before it (3700, hidden but for this), whose staging and stores
 // share shared memory and the way to L2 with the operands.  A launch adds 4.7 us: set-up, first operands (2000), last epilogue.  One
 // CTA a tile of 128 x 256 needs 48 KB a block of K and took 33.1 us for the 5216 rows.
